@@ -17,6 +17,15 @@
  *   6. ultraep_grad_reduce    local half of the gradient reduction: replica
  *                             gradients accumulated into main gradients
  *
+ * and the operators of the MoE layer around it:
+ *
+ *   7. ultraep_route          router: top-k ids, gates, per-expert counts and
+ *      ultraep_balance_loss   score sums; the balance loss over them
+ *      ultraep_route_grad     and the logits' gradient from both
+ *   8. ultraep_combine_grad   backward pass of the combine
+ *   9. ultraep_quant_rows     rows to 8-bit integers with a scale each, and
+ *      ultraep_expert_matmul  the experts' products on them, block by block
+ *
  * Conventions for every call:
  *   - Buffer pointers are DEVICE pointers unless marked "host".  The caller
  *     owns and allocates every buffer; the library never allocates, never
@@ -326,6 +335,161 @@ int ultraep_combine(const uint16_t *y, int64_t n_rows, const float *gate,
 int ultraep_grad_reduce(float *main_grad, float *rgrad, int64_t W, int32_t rank,
                         const ultraep_group *g, const ultraep_plan_buf *plan, int64_t cap,
                         int32_t *status, hipStream_t stream);
+
+/* Element types of the operators below that take more than one. */
+enum {
+  ULTRAEP_F32 = 0,
+  ULTRAEP_BF16 = 1
+};
+
+enum {
+  ULTRAEP_SOFTMAX = 0,
+  ULTRAEP_SIGMOID = 1
+};
+
+/* A router (host struct): E experts, k of them a token, 1 <= k <= min(E, 64),
+ * E <= 1024.
+ *   score      of a token's logits z: ULTRAEP_SOFTMAX  s = softmax(z), or
+ *              ULTRAEP_SIGMOID  s = 1 / (1 + exp(-z))
+ *   renorm     1: a token's gates are scale * s_i / (sum of its chosen s);
+ *              0: scale * s_i
+ *   n_group,   0, 0: every expert is eligible.  Else the experts form n_group
+ *   top_group  contiguous groups of at least two (n_group <= 64 divides E);
+ *              a group scores the sum of its two largest keys and the
+ *              token's ids come from its top_group best (ties: the lower
+ *              group; k <= top_group * E / n_group)
+ *   scale      finite
+ *   seq_len    tokens of a sequence for the statistics: token t belongs to
+ *              sequence t / seq_len.  0: all T tokens are one */
+typedef struct {
+  int32_t E;
+  int32_t k;
+  int32_t score;
+  int32_t renorm;
+  int32_t n_group;
+  int32_t top_group;
+  float scale;
+  int64_t seq_len;
+} ultraep_router;
+
+/* Router.  A token's ids are the k experts of largest key, in falling order,
+ * equal keys by rising id, where the key is
+ *   softmax  z + bias
+ *   sigmoid  s + bias; z itself where there is neither bias nor groups
+ * in fp32 (bias enters the selection only).  An expert whose logit is -inf is
+ * never chosen: the ids left over are -1, their gates 0.  A token that is
+ * masked, or has no logit above -inf, gets ids -1 and gates 0 and counts in no
+ * statistic; so does one with a NaN or +inf logit, which raises ULTRAEP_EDATA.
+ * The ids are what ultraep_count and ultraep_dispatch take, the gates what
+ * ultraep_combine takes, and counts (with seq_len 0) this rank's row of the
+ * load matrix.
+ *   logits    [T] rows of E elements of `type`, ld elements apart (E <= ld <= 2^20)
+ *   bias      [E] fp32, or null
+ *   mask      [T] bytes, 0 = masked; or null
+ *   topk      [T][k] int32
+ *   gate      [T][k] fp32
+ * Statistics of each of the n_seg = ceil(T / seq_len) sequences (1 with
+ * seq_len 0, also for T = 0); all three, or null for each:
+ *   counts    [n_seg][E] int32: ids by expert
+ *   prob_sum  [n_seg][E] fp32: sum over tokens of p = s / (sum of all E s)
+ *             (softmax: p = s)
+ *   tokens    [n_seg] int32: tokens that have an id
+ *   ws        workspace of ws_bytes >= ultraep_route_ws_bytes, 4-byte aligned
+ *             (may be null without statistics)
+ * Sums run in one fixed order for given T and router: equal calls give equal
+ * bits.  T <= 2^23. */
+int ultraep_route(const void *logits, int32_t type, int64_t T, int64_t ld,
+                  const ultraep_router *r, const float *bias, const uint8_t *mask,
+                  int32_t *topk, float *gate, int32_t *counts, float *prob_sum,
+                  int32_t *tokens, void *ws, size_t ws_bytes, int32_t *status,
+                  hipStream_t stream);
+
+/* Bytes of device workspace that ultraep_route needs for its statistics (host
+ * only; 0 for unsupported arguments, at least 4 otherwise). */
+size_t ultraep_route_ws_bytes(int64_t T, const ultraep_router *r);
+
+/* Balance loss over n_seg sequences: with c, F = counts, load_tokens (this
+ * rank's own, or summed over all ranks), P, n = prob_sum, tokens
+ *   coef[s][e] = alpha * E * c[s][e] / (n_seg * k * F[s] * n[s])
+ *   loss       = sum over s, e of coef[s][e] * P[s][e]
+ * coef is 0 for a sequence whose F or n is not positive; it is the loss's
+ * gradient with respect to each of the sequence's score rows p, which
+ * ultraep_route_grad takes.  Neither aliases an input.  n_seg >= 0 (0: loss 0). */
+int ultraep_balance_loss(const int32_t *counts, const int32_t *load_tokens,
+                         const float *prob_sum, const int32_t *tokens, int64_t n_seg,
+                         const ultraep_router *r, float alpha, float *loss, float *coef,
+                         hipStream_t stream);
+
+/* Gradient of the router: of  sum dgate * gate + dloss * sum coef * p  with
+ * respect to the logits (topk and coef are constants).
+ *   topk     [T][k] from ultraep_route
+ *   dgate    [T][k] fp32, or null (0)
+ *   coef     [n_seg][E] from ultraep_balance_loss, or null (0)
+ *   dloss    one fp32 on the device, or null (1)
+ *   dlogits  rows like logits': type, ld; all T * E elements are written, the
+ *            ld - E between them are not; may be logits itself
+ * Masked tokens, tokens whose first id is -1, and logits of -inf, get 0.  An id outside
+ * [-1, E), a NaN or a +inf logit raises ULTRAEP_EDATA.  bias and groups only
+ * choose ids and do not enter.  T <= 2^23. */
+int ultraep_route_grad(const void *logits, int32_t type, int64_t T, int64_t ld,
+                       const ultraep_router *r, const uint8_t *mask, const int32_t *topk,
+                       const float *dgate, const float *coef, const float *dloss,
+                       void *dlogits, int32_t *status, hipStream_t stream);
+
+/* Backward pass of ultraep_combine: from dout [T][H] bf16, the gradient of its
+ * output rows,
+ *   dy[row_of_slot[t*k+i]] = bf16(gate[t*k+i] * dout[t])
+ *   dgate[t*k+i]           = sum_h dout[t][h] * y[row_of_slot[t*k+i]][h]  (fp32)
+ * rounded to nearest-even, NaN to 0x7FC0; a masked slot (row -1) has dgate 0.
+ * The backward pass of the dispatch is ultraep_combine with gates 1.
+ *   y, dy     [n_rows][H] bf16 in the dispatch layout; dy may not be y
+ *   n_routed  device, block_off + R * S of the dispatch: dy's rows from there
+ *             to n_rows - 1 are zero-filled
+ * A row outside [-1, n_routed) (that slot is skipped, its dgate 0), or n_routed
+ * outside [0, n_rows] (dy is left alone and dgate 0), raises ULTRAEP_EDATA.
+ * Sizes and alignment as for ultraep_combine; n_rows < 2^31. */
+int ultraep_combine_grad(const uint16_t *dout, const uint16_t *y, int64_t n_rows,
+                         const float *gate, const int32_t *row_of_slot, int64_t T, int32_t k,
+                         int32_t H, const int64_t *n_routed, uint16_t *dy, float *dgate,
+                         int32_t *status, hipStream_t stream);
+
+/* Rows to 8-bit integers with a scale each.  With a = max |x| over a row,
+ *   scale = a / 127,  q = round-to-nearest-even(x * (127 / a))
+ * each operation in fp32; a row with a <= 2^-100 has q 0 and scale 0, a row
+ * with an infinity or a NaN q 0 and scale NaN.  A weight [n][N][K] takes n * N
+ * rows.
+ *   x      rows of K elements of `type`, ld elements apart
+ *   q      rows of ldq bytes, ldq >= K: K integers, then zeros
+ *   scale  [rows] fp32
+ * K, ld % 8 == 0, ldq % 16 == 0, ld, ldq <= 2^20, rows < 2^31, 16-byte aligned x
+ * and q. */
+int ultraep_quant_rows(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
+                       int8_t *q, int64_t ldq, float *scale, hipStream_t stream);
+
+/* The experts' products on 8-bit integers.  Row m of block g (rows block_off[g]
+ * to block_off[g + 1] - 1, as the dispatch writes them) meets weight
+ * w = block_w[g]:
+ *   v[n] = (sum_k xq[m][k] * wq[w][n][k]) * x_scale[m] * w_scale[w][n]
+ * the sum in 32-bit integers (exact), the rest in fp32.  y[m] = v, or with
+ * act 1 (SwiGLU, gate rows of the weight first)
+ *   y[m][n] = v[n] / (1 + exp(-v[n])) * v[N/2 + n],  n < N/2
+ * rounded to nearest-even to `type`, a NaN to 0x7FC0 in bf16.
+ *   xq         [M][K] int8, x_scale [M] fp32
+ *   wq         [n_w][N][K] int8, w_scale [n_w][N] fp32
+ *   block_off  [n_block + 1] int64 (a part of the dispatch's is fine: rows
+ *              outside the blocks are neither read nor written)
+ *   block_w    [n_block] int32, or null (block g takes weight g)
+ *   y          [M][N], or [M][N / 2] with act
+ * Blocks that are not in rising order within [0, M], and a nonempty block
+ * whose weight is outside [0, n_w), raise ULTRAEP_EDATA and are skipped.
+ * 1 <= n_block <= 2048, n_w >= 1, M < 2^31; K % 16 == 0, K <= 2^16 (the sum
+ * stays within 32 bits), N % 8 == 0 (N % 16 == 0 with act), N <= 2^20; 16-byte
+ * aligned xq, wq and y.  M = 1 is the decode form: any M takes any blocks. */
+int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
+                          const int8_t *wq, const float *w_scale, int32_t n_w, int32_t N,
+                          int32_t K, const int64_t *block_off, const int32_t *block_w,
+                          int32_t n_block, int32_t act, void *y, int32_t type,
+                          int32_t *status, hipStream_t stream);
 
 /* Host only.  Static description of a status code. */
 const char *ultraep_strerror(int code);

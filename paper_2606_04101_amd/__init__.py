@@ -67,6 +67,29 @@ class PlanBuf(ctypes.Structure):
                  "reroute", "stats")]
 
 
+ULTRAEP_F32, ULTRAEP_BF16 = 0, 1
+ULTRAEP_SOFTMAX, ULTRAEP_SIGMOID = 0, 1
+
+
+class Router(ctypes.Structure):
+    """ultraep_router: E experts, k of them a token, the score function
+    (ULTRAEP_SOFTMAX or ULTRAEP_SIGMOID), gates renormalised over a token's
+    experts and scaled, the best top_group of n_group groups (0: all eligible),
+    seq_len tokens a sequence in the statistics (0: all are one)."""
+    _fields_ = [("E", ctypes.c_int32), ("k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renorm", ctypes.c_int32), ("n_group", ctypes.c_int32),
+                ("top_group", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("seq_len", ctypes.c_int64)]
+
+    def __init__(self, E, k, score=ULTRAEP_SOFTMAX, renorm=True, n_group=0, top_group=0, scale=1.0,
+                 seq_len=0):
+        super().__init__(E, k, score, int(renorm), n_group, top_group, scale, seq_len)
+
+    def n_seg(self, T):
+        """Sequences of T tokens."""
+        return -(-T // self.seq_len) if self.seq_len > 0 and T > 0 else 1
+
+
 PLAN_FIELDS = ("slot_expert", "quota", "host_ptr", "host_rank", "host_pslot",
                "reroute", "stats")
 
@@ -108,6 +131,17 @@ def lib():
                                          _P, _P]
         L.ultraep_combine.argtypes = [_P, i64, _P, _P, i64, i32, i32, _P, _P, _P]
         L.ultraep_grad_reduce.argtypes = [_P, _P, i64, i32, gp, pp, i64, _P, _P]
+        f32, rp = ctypes.c_float, ctypes.POINTER(Router)
+        L.ultraep_route_ws_bytes.argtypes = [i64, rp]
+        L.ultraep_route_ws_bytes.restype = sz
+        L.ultraep_route.argtypes = [_P, i32, i64, i64, rp, _P, _P, _P, _P, _P, _P, _P, _P, sz,
+                                    _P, _P]
+        L.ultraep_balance_loss.argtypes = [_P, _P, _P, _P, i64, rp, f32, _P, _P, _P]
+        L.ultraep_route_grad.argtypes = [_P, i32, i64, i64, rp, _P, _P, _P, _P, _P, _P, _P, _P]
+        L.ultraep_combine_grad.argtypes = [_P, _P, i64, _P, _P, i64, i32, i32, _P, _P, _P, _P, _P]
+        L.ultraep_quant_rows.argtypes = [_P, i32, i64, i64, i64, _P, i64, _P, _P]
+        L.ultraep_expert_matmul.argtypes = [_P, _P, i64, _P, _P, i32, i32, i32, _P, _P, i32, i32,
+                                            _P, i32, _P, _P]
         L.ultraep_strerror.argtypes = [ctypes.c_int]
         L.ultraep_strerror.restype = ctypes.c_char_p
         for f in ("ultraep_plan_sizes", "ultraep_count", "ultraep_plan",
@@ -115,7 +149,9 @@ def lib():
                   "ultraep_dispatch", "ultraep_dispatch_layout",
                   "ultraep_dispatch_scatter", "ultraep_pack_replicas",
                   "ultraep_reroute_and_pack", "ultraep_relay_plan",
-                  "ultraep_pack_relay", "ultraep_combine", "ultraep_grad_reduce"):
+                  "ultraep_pack_relay", "ultraep_combine", "ultraep_grad_reduce",
+                  "ultraep_route", "ultraep_balance_loss", "ultraep_route_grad",
+                  "ultraep_combine_grad", "ultraep_quant_rows", "ultraep_expert_matmul"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -152,7 +188,9 @@ def _load_native():
                 for n in ("count", "plan", "plan_noalloc", "plan_replicate", "plan_reroute",
                           "dispatch", "dispatch_layout", "dispatch_scatter", "pack_replicas",
                           "reroute_and_pack", "relay_plan", "pack_relay", "combine",
-                          "grad_reduce")}, Group, Plan, PlanBuf)
+                          "grad_reduce", "route", "balance_loss", "route_grad",
+                          "combine_grad", "quant_rows", "expert_matmul")},
+               Group, Plan, PlanBuf, Router)
     _native = m
     return m
 
@@ -431,6 +469,146 @@ def ultraep_grad_reduce(main_grad, rgrad, W, rank, g: Group, plan: Plan, cap, st
     return _check(lib().ultraep_grad_reduce(
         _ptr(main_grad), _ptr(rgrad), W, rank, ctypes.byref(g), ctypes.byref(plan.c), cap,
         _ptr(status), _stream(stream)), "ultraep_grad_reduce")
+
+
+def _row_type(t, name):
+    """ULTRAEP_F32 or ULTRAEP_BF16 by t's element type; bf16 may come as raw
+    16-bit integers."""
+    dt = str(t.dtype) if t is not None else None
+    if dt == "torch.float32":
+        return ULTRAEP_F32
+    if dt in ("torch.bfloat16", "torch.int16", "torch.uint16"):
+        return ULTRAEP_BF16
+    raise ValueError(f"{name}: expected float32 or bfloat16 elements, got {dt}")
+
+
+def _need_rows(t, rows, n, ld, type_, name):
+    """Raises unless t holds rows of n elements, ld apart, of the row type."""
+    if rows > 0:
+        if _row_type(t, name) != type_:
+            raise ValueError(f"{name}: expected elements of the other rows' type, got {t.dtype}")
+        _need(t, (rows - 1) * ld + n, 4 if type_ == ULTRAEP_F32 else 2, name)
+
+
+def ultraep_route_ws_bytes(T, r: Router) -> int:
+    return int(lib().ultraep_route_ws_bytes(T, ctypes.byref(r)))
+
+
+def ultraep_route(logits, T, ld, r: Router, bias, mask, topk, gate, counts, prob_sum, tokens, ws,
+                  status, stream=None):
+    """bias, mask, and counts, prob_sum, tokens, ws together, may be None."""
+    rc = (_native or _load_native()).route(logits, T, ld, r, bias, mask, topk, gate, counts,
+                                          prob_sum, tokens, ws, status, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_route")
+    type_ = _row_type(logits, "logits") if T > 0 else ULTRAEP_F32
+    n_seg = r.n_seg(T)
+    _need_rows(logits, T, r.E, ld, type_, "logits")
+    _need(bias, r.E if bias is not None else 0, 4, "bias")
+    _need(mask, T if mask is not None else 0, 1, "mask")
+    _need(topk, T * r.k, 4, "topk")
+    _need(gate, T * r.k, 4, "gate")
+    _need(counts, n_seg * r.E if counts is not None else 0, 4, "counts")
+    _need(prob_sum, n_seg * r.E if prob_sum is not None else 0, 4, "prob_sum")
+    _need(tokens, n_seg if tokens is not None else 0, 4, "tokens")
+    _need(status, 1, 4, "status")
+    return _check(lib().ultraep_route(
+        _ptr(logits), type_, T, ld, ctypes.byref(r), _ptr(bias), _ptr(mask), _ptr(topk), _ptr(gate),
+        _ptr(counts), _ptr(prob_sum), _ptr(tokens), _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0, _ptr(status), _stream(stream)),
+        "ultraep_route")
+
+
+def ultraep_balance_loss(counts, load_tokens, prob_sum, tokens, n_seg, r: Router, alpha, loss, coef,
+                         stream=None):
+    rc = (_native or _load_native()).balance_loss(counts, load_tokens, prob_sum, tokens, n_seg, r,
+                                                 alpha, loss, coef, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_balance_loss")
+    _need(counts, n_seg * r.E, 4, "counts")
+    _need(load_tokens, n_seg, 4, "load_tokens")
+    _need(prob_sum, n_seg * r.E, 4, "prob_sum")
+    _need(tokens, n_seg, 4, "tokens")
+    _need(loss, 1, 4, "loss")
+    _need(coef, n_seg * r.E, 4, "coef")
+    return _check(lib().ultraep_balance_loss(
+        _ptr(counts), _ptr(load_tokens), _ptr(prob_sum), _ptr(tokens), n_seg, ctypes.byref(r), alpha,
+        _ptr(loss), _ptr(coef), _stream(stream)), "ultraep_balance_loss")
+
+
+def ultraep_route_grad(logits, T, ld, r: Router, mask, topk, dgate, coef, dloss, dlogits, status,
+                       stream=None):
+    """mask, dgate, coef and dloss may be None."""
+    rc = (_native or _load_native()).route_grad(logits, T, ld, r, mask, topk, dgate, coef, dloss,
+                                               dlogits, status, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_route_grad")
+    type_ = _row_type(logits, "logits") if T > 0 else ULTRAEP_F32
+    _need_rows(logits, T, r.E, ld, type_, "logits")
+    _need_rows(dlogits, T, r.E, ld, type_, "dlogits")
+    _need(mask, T if mask is not None else 0, 1, "mask")
+    _need(topk, T * r.k, 4, "topk")
+    _need(dgate, T * r.k if dgate is not None else 0, 4, "dgate")
+    _need(coef, r.n_seg(T) * r.E if coef is not None else 0, 4, "coef")
+    _need(dloss, 1 if dloss is not None else 0, 4, "dloss")
+    _need(status, 1, 4, "status")
+    return _check(lib().ultraep_route_grad(
+        _ptr(logits), type_, T, ld, ctypes.byref(r), _ptr(mask), _ptr(topk), _ptr(dgate), _ptr(coef),
+        _ptr(dloss), _ptr(dlogits), _ptr(status), _stream(stream)), "ultraep_route_grad")
+
+
+def ultraep_combine_grad(dout, y, n_rows, gate, row_of_slot, T, k, H, n_routed, dy, dgate, status,
+                         stream=None):
+    """n_routed: a one-element int64 device tensor (e.g. block_off[-1:])."""
+    rc = (_native or _load_native()).combine_grad(dout, y, n_rows, gate, row_of_slot, T, k, H,
+                                                 n_routed, dy, dgate, status, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_combine_grad")
+    _need(dout, T * H, 2, "dout")
+    _need(y, n_rows * H, 2, "y")
+    _need(gate, T * k, 4, "gate")
+    _need(row_of_slot, T * k, 4, "row_of_slot")
+    _need(n_routed, 1, 8, "n_routed")
+    _need(dy, n_rows * H, 2, "dy")
+    _need(dgate, T * k, 4, "dgate")
+    _need(status, 1, 4, "status")
+    return _check(lib().ultraep_combine_grad(
+        _ptr(dout), _ptr(y), n_rows, _ptr(gate), _ptr(row_of_slot), T, k, H, _ptr(n_routed),
+        _ptr(dy), _ptr(dgate), _ptr(status), _stream(stream)), "ultraep_combine_grad")
+
+
+def ultraep_quant_rows(x, rows, K, ld, q, ldq, scale, stream=None):
+    rc = (_native or _load_native()).quant_rows(x, rows, K, ld, q, ldq, scale, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_quant_rows")
+    type_ = _row_type(x, "x") if rows > 0 else ULTRAEP_BF16
+    _need_rows(x, rows, K, ld, type_, "x")
+    _need(q, rows * ldq, 1, "q")
+    _need(scale, rows, 4, "scale")
+    return _check(lib().ultraep_quant_rows(_ptr(x), type_, rows, K, ld, _ptr(q), ldq, _ptr(scale),
+                                           _stream(stream)), "ultraep_quant_rows")
+
+
+def ultraep_expert_matmul(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w, n_block, act,
+                          y, status, stream=None):
+    """block_w may be None (block g takes weight g); y is float32 or bfloat16."""
+    rc = (_native or _load_native()).expert_matmul(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off,
+                                                  block_w, n_block, act, y, status, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_matmul")
+    type_ = _row_type(y, "y") if M > 0 else ULTRAEP_BF16
+    _need(xq, M * K, 1, "xq")
+    _need(x_scale, M, 4, "x_scale")
+    _need(wq, n_w * N * K, 1, "wq")
+    _need(w_scale, n_w * N, 4, "w_scale")
+    _need(block_off, n_block + 1, 8, "block_off")
+    _need(block_w, n_block if block_w is not None else 0, 4, "block_w")
+    _need(y, M * (N // 2 if act else N), 4 if type_ == ULTRAEP_F32 else 2, "y")
+    _need(status, 1, 4, "status")
+    return _check(lib().ultraep_expert_matmul(
+        _ptr(xq), _ptr(x_scale), M, _ptr(wq), _ptr(w_scale), n_w, N, K, _ptr(block_off),
+        _ptr(block_w), n_block, int(act), _ptr(y), type_, _ptr(status), _stream(stream)),
+        "ultraep_expert_matmul")
 
 
 def build():

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libultraep.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["abi.hip", "count.hip", "plan.hip", "dispatch.hip", "pack.hip",
-           "relay.hip", "combine.hip", "reduce.hip"]
+           "relay.hip", "combine.hip", "reduce.hip",
+           "operators.hip", "route.hip", "combine_grad.hip", "expert.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions are disabled for all device code

@@ -21,14 +21,15 @@ typedef __int128 wide;  // products of caller-given sizes
 #define ENTRIES(X)                                                                           \
   X(count) X(plan) X(plan_noalloc) X(plan_replicate) X(plan_reroute) X(dispatch)             \
   X(dispatch_layout) X(dispatch_scatter) X(pack_replicas) X(reroute_and_pack) X(relay_plan)  \
-  X(pack_relay) X(combine) X(grad_reduce)
+  X(pack_relay) X(combine) X(grad_reduce) X(route) X(balance_loss) X(route_grad)             \
+  X(combine_grad) X(quant_rows) X(expert_matmul)
 
 struct Library {
 #define FIELD(n) decltype(&ultraep_##n) n = nullptr;
   ENTRIES(FIELD)
 #undef FIELD
 } lib;
-PyObject *t_group, *t_plan, *t_buf;       // Group, Plan, PlanBuf
+PyObject *t_group, *t_plan, *t_buf, *t_router;  // Group, Plan, PlanBuf, Router
 PyObject *s_c, *s_ws, *s_cuda_stream;     // attribute names
 
 // The arguments of one call, in order; ok turns false at the first one that
@@ -84,6 +85,36 @@ struct Args {
     return tensor<T>(ok ? a[i] : Py_None, n, sizeof(T));
   }
 
+  // the same where None stands for a buffer left out
+  template <class T = void>
+  T *maybe(int i, wide n) {
+    return ok && a[i] != Py_None ? tensor<T>(i, n) : nullptr;
+  }
+  // rows of fp32 or bf16 elements, and which; bf16 may come as raw 16-bit integers
+  void *rows(int i, wide n, int32_t &type) {
+    type = ULTRAEP_F32;
+    if (!ok || n <= 0) return ok ? tensor(a[i], 0, 0) : nullptr;
+    if (!THPVariable_CheckExact(a[i])) return fail();
+    const at::Tensor &t = THPVariable_Unpack(a[i]);
+    if (!t.defined()) return fail();
+    const at::ScalarType d = t.scalar_type();
+    if (d != at::kFloat && d != at::kBFloat16 && d != at::kShort && d != at::kUInt16) return fail();
+    type = d == at::kFloat ? ULTRAEP_F32 : ULTRAEP_BF16;
+    return tensor(a[i], n, d == at::kFloat ? 4 : 2);
+  }
+  // a float, or an int
+  float number(int i) {
+    if (!ok || !(PyFloat_CheckExact(a[i]) || PyLong_CheckExact(a[i]))) return fail(), 0.f;
+    const double v = PyFloat_AsDouble(a[i]);
+    if (PyErr_Occurred()) return PyErr_Clear(), fail(), 0.f;
+    return static_cast<float>(v);
+  }
+  // a bool, or an int
+  int32_t flag(int i) {
+    if (ok && PyBool_Check(a[i])) return a[i] == Py_True;
+    return i32(i);
+  }
+
   // the memory of a ctypes structure of exactly type `type`
   void *structure(PyObject *o, PyObject *type, Py_ssize_t size) {
     if (!ok || reinterpret_cast<PyObject *>(Py_TYPE(o)) != type) return fail();
@@ -97,6 +128,11 @@ struct Args {
     auto *g = static_cast<const ultraep_group *>(structure(a[i], t_group, sizeof(ultraep_group)));
     if (g && (g->R < 1 || g->E < 1 || g->n_slot < 0)) return fail(), nullptr;
     return g;
+  }
+  const ultraep_router *router(int i) {
+    auto *r = static_cast<const ultraep_router *>(structure(a[i], t_router, sizeof(ultraep_router)));
+    if (r && (r->E < 1 || r->k < 1 || r->seq_len < 0)) return fail(), nullptr;
+    return r;
   }
   PyObject *attr(PyObject *o, PyObject *name) {
     PyObject *v = ok ? PyObject_GetAttr(o, name) : nullptr;
@@ -149,6 +185,11 @@ int64_t blocks(const ultraep_group *g) {
 }
 wide loads(const ultraep_group *g) { return wide(g->R) * g->E; }
 wide mains(const ultraep_group *g) { return g->E / g->R; }
+// elements that T rows of n, ld apart, take
+wide strided(int64_t T, int64_t n, int64_t ld) { return T > 0 ? (wide(T) - 1) * ld + n : 0; }
+wide sequences(const ultraep_router *r, int64_t T) {
+  return r->seq_len > 0 && T > 0 ? (wide(T) + r->seq_len - 1) / r->seq_len : 1;
+}
 
 // None if an argument was not taken, else the entry point's return value
 template <class F>
@@ -357,10 +398,121 @@ ENTRY(grad_reduce, 9, {
   return finish(v, [&] { return lib.grad_reduce(mg, rg, W, rank, g, p, cap, status, s); });
 })
 
-// bind({entry point: address}, Group, Plan, PlanBuf)
+// logits, T, ld, router, bias, mask, topk, gate, counts, prob_sum, tokens, ws, status, stream
+ENTRY(route, 14, {
+  const int64_t T = v.i64(1), ld = v.i64(2);
+  auto *r = v.router(3);
+  const wide E = r ? r->E : 0, k = r ? r->k : 0, n = r ? sequences(r, T) : 0;
+  int32_t type;
+  void *logits = v.rows(0, r ? strided(T, r->E, ld) : 0, type);
+  auto *bias = v.maybe<float>(4, E);
+  auto *mask = v.maybe<uint8_t>(5, T);
+  auto *topk = v.tensor<int32_t>(6, T * k);
+  auto *gate = v.tensor<float>(7, T * k);
+  auto *counts = v.maybe<int32_t>(8, n * E);
+  auto *prob = v.maybe<float>(9, n * E);
+  auto *tokens = v.maybe<int32_t>(10, n);
+  size_t bytes = 0;
+  void *ws = v.ok && argv[11] != Py_None ? v.workspace(11, -1, bytes) : nullptr;
+  auto *status = v.tensor<int32_t>(12, 1);
+  hipStream_t s = v.stream(13);
+  return finish(v, [&] {
+    return lib.route(logits, type, T, ld, r, bias, mask, topk, gate, counts, prob, tokens, ws, bytes,
+                     status, s);
+  });
+})
+
+// counts, load_tokens, prob_sum, tokens, n_seg, router, alpha, loss, coef, stream
+ENTRY(balance_loss, 10, {
+  const int64_t n = v.i64(4);
+  auto *r = v.router(5);
+  const wide all = r ? wide(n) * r->E : 0;
+  auto *counts = v.tensor<int32_t>(0, all);
+  auto *load = v.tensor<int32_t>(1, n);
+  auto *prob = v.tensor<float>(2, all);
+  auto *tokens = v.tensor<int32_t>(3, n);
+  const float alpha = v.number(6);
+  auto *loss = v.tensor<float>(7, 1);
+  auto *coef = v.tensor<float>(8, all);
+  hipStream_t s = v.stream(9);
+  return finish(v, [&] {
+    return lib.balance_loss(counts, load, prob, tokens, n, r, alpha, loss, coef, s);
+  });
+})
+
+// logits, T, ld, router, mask, topk, dgate, coef, dloss, dlogits, status, stream
+ENTRY(route_grad, 12, {
+  const int64_t T = v.i64(1), ld = v.i64(2);
+  auto *r = v.router(3);
+  const wide E = r ? r->E : 0, k = r ? r->k : 0, n = r ? sequences(r, T) : 0;
+  int32_t type, out_type;
+  void *logits = v.rows(0, r ? strided(T, r->E, ld) : 0, type);
+  auto *mask = v.maybe<uint8_t>(4, T);
+  auto *topk = v.tensor<int32_t>(5, T * k);
+  auto *dgate = v.maybe<float>(6, T * k);
+  auto *coef = v.maybe<float>(7, n * E);
+  auto *dloss = v.maybe<float>(8, 1);
+  void *dlogits = v.rows(9, r ? strided(T, r->E, ld) : 0, out_type);
+  if (type != out_type) Py_RETURN_NONE;
+  auto *status = v.tensor<int32_t>(10, 1);
+  hipStream_t s = v.stream(11);
+  return finish(v, [&] {
+    return lib.route_grad(logits, type, T, ld, r, mask, topk, dgate, coef, dloss, dlogits, status, s);
+  });
+})
+
+// dout, y, n_rows, gate, row_of_slot, T, k, H, n_routed, dy, dgate, status, stream
+ENTRY(combine_grad, 13, {
+  const int64_t n_rows = v.i64(2), T = v.i64(5);
+  const int32_t k = v.i32(6), H = v.i32(7);
+  auto *dout = v.tensor<uint16_t>(0, wide(T) * H);
+  auto *y = v.tensor<uint16_t>(1, wide(n_rows) * H);
+  auto *gate = v.tensor<float>(3, wide(T) * k);
+  auto *ros = v.tensor<int32_t>(4, wide(T) * k);
+  auto *nr = v.tensor<int64_t>(8, 1);
+  auto *dy = v.tensor<uint16_t>(9, wide(n_rows) * H);
+  auto *dgate = v.tensor<float>(10, wide(T) * k);
+  auto *status = v.tensor<int32_t>(11, 1);
+  hipStream_t s = v.stream(12);
+  return finish(v, [&] {
+    return lib.combine_grad(dout, y, n_rows, gate, ros, T, k, H, nr, dy, dgate, status, s);
+  });
+})
+
+// x, rows, K, ld, q, ldq, scale, stream
+ENTRY(quant_rows, 8, {
+  const int64_t rows = v.i64(1), K = v.i64(2), ld = v.i64(3), ldq = v.i64(5);
+  int32_t type;
+  void *x = v.rows(0, strided(rows, K, ld), type);
+  auto *q = v.tensor<int8_t>(4, wide(rows) * ldq);
+  auto *scale = v.tensor<float>(6, rows);
+  hipStream_t s = v.stream(7);
+  return finish(v, [&] { return lib.quant_rows(x, type, rows, K, ld, q, ldq, scale, s); });
+})
+
+// xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w, n_block, act, y, status, stream
+ENTRY(expert_matmul, 15, {
+  const int64_t M = v.i64(2);
+  const int32_t n_w = v.i32(5), N = v.i32(6), K = v.i32(7), n = v.i32(10), act = v.flag(11);
+  auto *xq = v.tensor<int8_t>(0, wide(M) * K);
+  auto *xs = v.tensor<float>(1, M);
+  auto *wq = v.tensor<int8_t>(3, wide(n_w) * N * K);
+  auto *ws = v.tensor<float>(4, wide(n_w) * N);
+  auto *off = v.tensor<int64_t>(8, wide(n) + 1);
+  auto *bw = v.maybe<int32_t>(9, n);
+  int32_t type;
+  void *y = v.rows(12, wide(M) * (act ? N / 2 : N), type);
+  auto *status = v.tensor<int32_t>(13, 1);
+  hipStream_t s = v.stream(14);
+  return finish(v, [&] {
+    return lib.expert_matmul(xq, xs, M, wq, ws, n_w, N, K, off, bw, n, act, y, type, status, s);
+  });
+})
+
+// bind({entry point: address}, Group, Plan, PlanBuf, Router)
 PyObject *py_bind(PyObject *, PyObject *args) {
-  PyObject *d, *g, *p, *b;
-  if (!PyArg_ParseTuple(args, "O!OOO", &PyDict_Type, &d, &g, &p, &b)) return nullptr;
+  PyObject *d, *g, *p, *b, *r;
+  if (!PyArg_ParseTuple(args, "O!OOOO", &PyDict_Type, &d, &g, &p, &b, &r)) return nullptr;
 #define SET(n)                                                                        \
   {                                                                                   \
     PyObject *v = PyDict_GetItemString(d, "ultraep_" #n);                             \
@@ -372,12 +524,15 @@ PyObject *py_bind(PyObject *, PyObject *args) {
   Py_INCREF(g);
   Py_INCREF(p);
   Py_INCREF(b);
+  Py_INCREF(r);
   Py_XDECREF(t_group);
   Py_XDECREF(t_plan);
   Py_XDECREF(t_buf);
+  Py_XDECREF(t_router);
   t_group = g;
   t_plan = p;
   t_buf = b;
+  t_router = r;
   Py_RETURN_NONE;
 }
 
@@ -390,6 +545,8 @@ PyMethodDef methods[] = {FAST(count), FAST(plan), FAST(plan_noalloc), FAST(plan_
                          FAST(plan_reroute), FAST(dispatch), FAST(dispatch_layout),
                          FAST(dispatch_scatter), FAST(pack_replicas), FAST(reroute_and_pack),
                          FAST(relay_plan), FAST(pack_relay), FAST(combine), FAST(grad_reduce),
+                         FAST(route), FAST(balance_loss), FAST(route_grad), FAST(combine_grad),
+                         FAST(quant_rows), FAST(expert_matmul),
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,

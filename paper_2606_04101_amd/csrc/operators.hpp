@@ -1,0 +1,94 @@
+// Launchers of the operators around the balancing path (router, combine's
+// backward pass, 8-bit expert products) and the numeric helpers they share.
+// Internal header; the C ABI in operators.hip validates arguments and calls
+// these.
+#pragma once
+
+#include "common.hpp"
+
+namespace uep {
+
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// route workspace: one partial of every statistic per chunk of a sequence
+struct RouteShape {
+  int64_t n_seg;    // sequences
+  int64_t seq;      // tokens of a sequence (the last may have fewer)
+  int64_t chunk;    // tokens of a workgroup
+  int64_t n_chunk;  // workgroups of a sequence
+};
+RouteShape route_shape(int64_t T, const ultraep_router &r);
+size_t route_ws_bytes(int64_t T, const ultraep_router &r);
+
+hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
+                        const ultraep_router &r, const float *bias, const uint8_t *mask,
+                        int32_t *topk, float *gate, int32_t *counts, float *prob_sum,
+                        int32_t *tokens, void *ws, int32_t *status, hipStream_t stream);
+hipError_t launch_balance_loss(const int32_t *counts, const int32_t *load_tokens,
+                               const float *prob_sum, const int32_t *tokens, int64_t n_seg,
+                               const ultraep_router &r, float alpha, float *loss, float *coef,
+                               hipStream_t stream);
+hipError_t launch_route_grad(const void *logits, int32_t type, int64_t T, int64_t ld,
+                             const ultraep_router &r, const uint8_t *mask, const int32_t *topk,
+                             const float *dgate, const float *coef, const float *dloss,
+                             void *dlogits, int32_t *status, hipStream_t stream);
+hipError_t launch_combine_grad(const uint16_t *dout, const uint16_t *y, int64_t n_rows,
+                               const float *gate, const int32_t *row_of_slot, int64_t T, int32_t k,
+                               int32_t H, const int64_t *n_routed, uint16_t *dy, float *dgate,
+                               int32_t *status, hipStream_t stream);
+hipError_t launch_quant_rows(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
+                             int8_t *q, int64_t ldq, float *scale, hipStream_t stream);
+hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, const int8_t *wq,
+                                const float *ws, int32_t n_w, int32_t N, int32_t K,
+                                const int64_t *block_off, const int32_t *block_w, int32_t n_block,
+                                int32_t act, void *y, int32_t type, int32_t *status,
+                                hipStream_t stream);
+
+__device__ __forceinline__ float bf16_at_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_at_high(uint32_t w) {
+  return __uint_as_float(w & 0xFFFF0000u);
+}
+
+// fp32 -> bf16, to nearest-even; NaN -> 0x7FC0
+__device__ __forceinline__ uint32_t round_bf16(float f) {
+  const uint32_t u = __float_as_uint(f);
+  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0u;
+  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+
+__device__ __forceinline__ float readlane_f(float v, int l) {
+  return __int_as_float(readlane(__float_as_int(v), l));
+}
+
+// Float reductions over the 64 lanes, each in one fixed order (DPP mirrors
+// inside rows of 16 lanes, then the four rows in order).  Every lane must be
+// active.
+template <int kCtrl>
+__device__ __forceinline__ float dpp_f(float v) {
+  const int i = __float_as_int(v);
+  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, kCtrl, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float wave_sum_f(float v) {
+  v += dpp_f<0xB1>(v);   // quad_perm 1,0,3,2
+  v += dpp_f<0x4E>(v);   // quad_perm 2,3,0,1
+  v += dpp_f<0x141>(v);  // row_half_mirror
+  v += dpp_f<0x140>(v);  // row_mirror
+  return (readlane_f(v, 0) + readlane_f(v, 16)) + (readlane_f(v, 32) + readlane_f(v, 48));
+}
+__device__ __forceinline__ float wave_max_f(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  v = fmaxf(v, dpp_f<0x140>(v));
+  return fmaxf(fmaxf(readlane_f(v, 0), readlane_f(v, 16)),
+               fmaxf(readlane_f(v, 32), readlane_f(v, 48)));
+}
+
+// 1 / (1 + exp(-z)), without overflow for any z
+__device__ __forceinline__ float sigmoid(float z) {
+  const float e = expf(-fabsf(z));
+  return (z >= 0.f ? 1.f : e) / (1.f + e);
+}
+
+}  // namespace uep
