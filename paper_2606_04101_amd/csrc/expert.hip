@@ -1,5 +1,7 @@
 // The experts' products on 8-bit integers: the quantisation of rows, and the
 // product of each dispatched block of rows with its expert's weight.
+#include <type_traits>
+
 #include "operators.hpp"
 
 namespace uep {
@@ -107,18 +109,11 @@ struct MatmulArgs {
   int32_t n_w, N, K, n_block, n_out, bf16;
 };
 
-constexpr int kMmThreads = 256;
 constexpr int kMmMaxBlocks = 2048;
-constexpr int kMmPer = kMmMaxBlocks / kMmThreads;  // blocks a thread looks at
 
-// Row tiles are numbered block by block.  The workgroup finds the block and the
-// first row of tile `tile` by a scan over the blocks' tile counts; .rows is 0
-// past the last tile.  A block that is out of order or out of [0, M], or has
-// rows and no weight, has no tile.
-struct RowTile {
-  int64_t row;
-  int32_t rows, w;
-};
+// Row tiles are numbered block by block.  cum[g] becomes the number of tiles
+// before block g, cum[n_block] that of all; a block that is out of order or out
+// of [0, M], or has rows and no weight, is reported and has none.
 __device__ __forceinline__ int64_t block_rows(const MatmulArgs &a, int g, bool &bad) {
   const int64_t lo = a.block_off[g], hi = a.block_off[g + 1];
   if (lo < 0 || hi < lo || hi > a.M) {
@@ -134,138 +129,272 @@ __device__ __forceinline__ int64_t block_rows(const MatmulArgs &a, int g, bool &
   }
   return hi - lo;
 }
-__device__ RowTile find_tile(const MatmulArgs &a, int64_t tile, int tile_rows) {
-  __shared__ int s_wave[kMmThreads / kWave];
-  __shared__ RowTile s_tile;
+template <int kThreads>
+__device__ void count_tiles(const MatmulArgs &a, int tile_rows, int *cum, int *wave_sums) {
   const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  if (tid == 0) s_tile = {0, 0, 0};
+  const int per = (a.n_block + kThreads - 1) / kThreads;  // blocks of a thread
   int mine = 0;
   bool bad = false;
-  for (int j = 0; j < kMmPer; ++j) {
-    const int g = tid * kMmPer + j;
+  for (int j = 0; j < per; ++j) {
+    const int g = tid * per + j;
     if (g < a.n_block)
       mine += static_cast<int>((block_rows(a, g, bad) + tile_rows - 1) / tile_rows);
   }
-  if (bad) report(a.status, ULTRAEP_EDATA);
+  if (bad && blockIdx.x == 0) report(a.status, ULTRAEP_EDATA);
   const int incl = wave_scan_incl(mine);
-  if (lane == kWave - 1) s_wave[wave] = incl;
+  if (lane == kWave - 1) wave_sums[wave] = incl;
   __syncthreads();
-  int64_t at = incl - mine;
-  for (int w = 0; w < wave; ++w) at += s_wave[w];
-  if (tile >= at && tile < at + mine) {
-    for (int j = 0; j < kMmPer; ++j) {
-      const int g = tid * kMmPer + j;
-      if (g >= a.n_block) break;
-      const int64_t n = block_rows(a, g, bad);
-      const int64_t tiles = (n + tile_rows - 1) / tile_rows;
-      if (tile < at + tiles) {
-        const int64_t r = (tile - at) * tile_rows;
-        s_tile = {a.block_off[g] + r, static_cast<int32_t>(n - r < tile_rows ? n - r : tile_rows),
-                  a.block_w ? a.block_w[g] : g};
-        break;
-      }
-      at += tiles;
+  int at = incl - mine;
+  for (int w = 0; w < wave; ++w) at += wave_sums[w];
+  for (int j = 0; j < per; ++j) {
+    const int g = tid * per + j;
+    if (g < a.n_block) {
+      cum[g] = at;
+      at += static_cast<int>((block_rows(a, g, bad) + tile_rows - 1) / tile_rows);
+      if (g == a.n_block - 1) cum[a.n_block] = at;
     }
   }
   __syncthreads();
-  return s_tile;
+}
+
+// Tile `tile` < cum[n_block]: its first row, rows and weight.  Every lane must
+// be active; all results are uniform.
+struct RowTile {
+  int64_t row;
+  int32_t rows, w;
+};
+__device__ __forceinline__ RowTile find_tile(const MatmulArgs &a, const int *cum, int tile,
+                                             int tile_rows) {
+  // the last block that begins at or before the tile, among equals the last,
+  // which is the one with tiles: first its run of 64 blocks, then the block
+  const int lane = lane_id();
+  int g = 0;
+  if (a.n_block > kWave) {
+    const int j = lane * kWave;
+    g = (__builtin_popcountll(ballot(j < a.n_block && cum[min(j, a.n_block)] <= tile)) - 1) * kWave;
+  }
+  const int j = g + lane;
+  g += __builtin_popcountll(ballot(j < a.n_block && cum[min(j, a.n_block)] <= tile)) - 1;
+  g = __builtin_amdgcn_readfirstlane(g);
+  const int64_t r = static_cast<int64_t>(tile - cum[g]) * tile_rows;
+  const int64_t lo = a.block_off[g], n = a.block_off[g + 1] - lo;
+  return {lo + r, __builtin_amdgcn_readfirstlane(static_cast<int>(min<int64_t>(n - r, tile_rows))),
+          __builtin_amdgcn_readfirstlane(a.block_w ? a.block_w[g] : g)};
 }
 
 __device__ __forceinline__ float silu(float v) { return v / (1.f + expf(-v)); }
 
-// Tile of 128 channels x 128 rows, K in steps of 64 bytes through LDS; four
-// waves of 64 x 64 each.  The weights are the MFMA's first operand, so a lane
-// holds 4 neighbouring channels of one row.  With act, channels 0..31 of each
-// wave's 64 are gates and the other 32 their partners.
-constexpr int kBn = 128, kBm = 128, kBk = 64;
+// 16 bytes a lane from base + off straight into LDS, lane l's at lds + 16 l.
+// The wait for it is the caller's (vmcnt).
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
+               : "memory");
+}
 
-// byte of 16-byte chunk c of tile row r in LDS, chunks exchanged so that eight
-// neighbouring rows lie in all banks
-__device__ __forceinline__ int lds_at(int r, int c) { return r * kBk + ((c ^ ((r >> 1) & 3)) * 16); }
+constexpr int kBk = 128;  // bytes of K of a step
 
-template <bool kAct>
-__global__ void __launch_bounds__(kMmThreads) k_matmul(MatmulArgs a, int64_t n_item, int32_t n_col) {
-  __shared__ __align__(16) int8_t s_w[kBn * kBk];
-  __shared__ __align__(16) int8_t s_x[kBm * kBk];
-  for (int64_t item = blockIdx.x; item < n_item; item += gridDim.x) {
-    const RowTile tile = find_tile(a, item / n_col, kBm);
-    if (tile.rows == 0) return;  // past the last tile, as are all later items
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-    const int wn = wave & 1, wm = wave >> 1;
-    const int half = kAct ? a.N / 2 : 0;
-    const int n0 = static_cast<int>(item % n_col) * (kAct ? kBn / 2 : kBn);  // first output channel
-    // weight row of tile row j, in range for any j
-    auto weight_row = [&](int j) {
-      if (!kAct) return min(n0 + j, a.N - 1);
-      const int o = n0 + (j / 64) * 32 + j % 32;
-      return min(o, half - 1) + (j % 64 >= 32 ? half : 0);
-    };
-    const int8_t *w = a.wq + static_cast<int64_t>(tile.w) * a.N * a.K;
-    const int8_t *x = a.xq + tile.row * a.K;
+// Output tile of kN weight rows x kM rows, K in steps of 128 bytes through two
+// LDS buffers; kWn x kWm waves.  The weights are the MFMA's first operand, so a
+// lane holds 4 neighbouring channels of one row.  With act, a wave's parts of 32
+// weight rows alternate between gates and their partners.
+template <int kN, int kM, int kWn, int kWm, bool kAct>
+__global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t n_col) {
+  constexpr int kThreads = 64 * kWn * kWm, kWaves = kWn * kWm;
+  constexpr int kFn = kN / kWn / 32, kFm = kM / kWm / 32;  // 32 x 32 parts of a wave
+  constexpr int kBuf = (kN + kM) * kBk;
+  constexpr int kLoads = kBuf / 1024 / kWaves;             // of a wave in a step
+  constexpr int kLoadsN = kLoads * kN / (kN + kM);
+  constexpr int kOut = kAct ? kN / 2 : kN;                 // channels of a tile
+  constexpr int kOutW = kOut / kWn;                        // of a wave
+  __shared__ __align__(1024) int8_t s_buf[2][kBuf];
+  __shared__ __align__(16) int8_t s_out[kWaves][4096];
+  __shared__ int s_cum[kMmMaxBlocks + 1];
+  __shared__ int s_sums[kWaves];
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int wn = wave % kWn, wm = wave / kWn;
+  const int lr = lane & 31, hi = lane >> 5;
+  const int half = a.N / 2;
+  count_tiles<kThreads>(a, kM, s_cum, s_sums);
+  const int n_tile = s_cum[a.n_block];
+  const int64_t n_item = static_cast<int64_t>(n_tile) * n_col;
 
-    v16i acc[2][2] = {};
-    const int nk = a.K / 16;  // 16-byte chunks of a row
-    for (int k0 = 0; k0 < nk; k0 += kBk / 16) {
-      __syncthreads();
-  #pragma unroll
-      for (int j = 0; j < kBn * kBk / 16 / kMmThreads; ++j) {
-        const int i = tid + j * kMmThreads, r = i / 4, c = i % 4;
-        v4i vw = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
-        if (k0 + c < nk) {
-          vw = *reinterpret_cast<const v4i *>(w + static_cast<int64_t>(weight_row(r)) * a.K + (k0 + c) * 16);
-          vx = *reinterpret_cast<const v4i *>(x + static_cast<int64_t>(min(r, tile.rows - 1)) * a.K + (k0 + c) * 16);
+  // the workgroups of one XCD (those of equal number modulo 8) take neighbouring
+  // items, 8 row tiles by 4 column tiles at a time
+  constexpr int kXcd = 8, kGroup = 8;
+  const int per_xcd = gridDim.x / kXcd;  // the grid is a multiple
+  const int64_t slot = static_cast<int64_t>(blockIdx.x % kXcd) * per_xcd + blockIdx.x / kXcd;
+  const uint32_t lds0 = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int8_t *)&s_buf[0][0]));
+  const int steps = (a.K + kBk - 1) / kBk;
+  const int tail = (a.K - (steps - 1) * kBk) / 16;  // chunks of the last step
+
+  for (int64_t item = slot; item < n_item; item += gridDim.x) {
+    const int group = static_cast<int>(item / (kGroup * n_col));
+    const int rest = static_cast<int>(item - static_cast<int64_t>(group) * kGroup * n_col);
+    const int high = min(kGroup, n_tile - group * kGroup);
+    const RowTile tile = find_tile(a, s_cum, group * kGroup + rest % high, kM);
+    const int n0 = rest / high * kOut;  // first channel
+
+    // byte offsets of this lane's loads: 8 rows of 8 chunks an instruction, the
+    // chunks of row r exchanged by r % 8 so that a column of chunks lies in all banks
+    const int8_t *wbase = a.wq + static_cast<int64_t>(tile.w) * a.N * a.K;
+    const int8_t *xbase = a.xq + tile.row * a.K;
+    uint32_t off[kLoads];
+    const int chunk = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int r;
+      if (i < kLoadsN) {
+        const int j = (i * kWaves + wave) * 8 + (lane >> 3);  // tile row
+        if (kAct) {
+          const int o = n0 + j / 64 * 32 + j % 32;
+          r = min(o, half - 1) + (j % 64 >= 32 ? half : 0);
+        } else {
+          r = min(n0 + j, a.N - 1);
         }
-        *reinterpret_cast<v4i *>(s_w + lds_at(r, c)) = vw;
-        *reinterpret_cast<v4i *>(s_x + lds_at(r, c)) = vx;
+      } else {
+        r = min(((i - kLoadsN) * kWaves + wave) * 8 + (lane >> 3), tile.rows - 1);
       }
-      __syncthreads();
-  #pragma unroll
-      for (int kk = 0; kk < kBk / 32; ++kk) {
-        const int c = kk * 2 + lane / 32;
-        v4i fw[2], fx[2];
-  #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          fw[i] = *reinterpret_cast<const v4i *>(s_w + lds_at(wn * 64 + i * 32 + lane % 32, c));
-          fx[i] = *reinterpret_cast<const v4i *>(s_x + lds_at(wm * 64 + i * 32 + lane % 32, c));
-        }
-  #pragma unroll
-        for (int i = 0; i < 2; ++i)
-  #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
-      }
+      off[i] = static_cast<uint32_t>(r) * a.K + chunk * 16;
     }
+    // load i of a step; chunks past K (in the last step) are loaded from the step's
+    // first one and not used
+    auto issue = [&](int s, int i) {
+      const uint32_t back = s == steps - 1 && chunk >= tail ? chunk * 16 : 0;
+      load_to_lds((i < kLoadsN ? wbase : xbase) + static_cast<int64_t>(s) * kBk, off[i] - back,
+                  __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * kBuf + (i * kWaves + wave) * 1024));
+    };
 
-    // lane: row lane % 32 of a 32 x 32 part, channels 8 (i / 4) + 4 (lane / 32) + i % 4
-    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N;
-  #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = wm * 64 + j * 32 + lane % 32;
-      if (r >= tile.rows) continue;
-      const float xs = a.xs[tile.row + r];
-      char *out = static_cast<char *>(a.y) + (tile.row + r) * a.n_out * (a.bf16 ? 2 : 4);
-  #pragma unroll
-      for (int i = 0; i < (kAct ? 1 : 2); ++i) {
-  #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = n0 + wn * (kAct ? 32 : 64) + i * 32 + q * 8 + lane / 32 * 4;
-          if (n >= a.n_out) continue;
-          float v[4];
-  #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = static_cast<float>(acc[i][j][q * 4 + e]) * xs * ws[n + e];
-            if (kAct)
-              v[e] = silu(v[e]) * (static_cast<float>(acc[1][j][q * 4 + e]) * xs * ws[half + n + e]);
+    v16i acc[kFn][kFm] = {};
+    v4i fw[2][kFn], fx[2][kFm];
+    // part f of the operands for 32 bytes kk of a step
+    auto fetch = [&](int s, int kk, int f) {
+      const int8_t *b = s_buf[s & 1] + ((kk * 2 + hi) ^ (lane & 7)) * 16;
+      if (f < kFn)
+        fw[kk & 1][f] = *reinterpret_cast<const v4i *>(b + (wn * kFn * 32 + f * 32 + lr) * kBk);
+      else
+        fx[kk & 1][f - kFn] = *reinterpret_cast<const v4i *>(
+            b + (kN + wm * kFm * 32 + (f - kFn) * 32 + lr) * kBk);
+    };
+    // One step, its first parts already in registers.  The products run in the
+    // order that keeps the matrix unit fed: reads of the next parts, and at the
+    // step's end the loads of the step after the next, between them.  kAhead: how
+    // many steps follow, up to 2.
+    auto step = [&](int s, auto ahead) {
+      constexpr int kAhead = decltype(ahead)::value;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        if (kk == 3)  // the next step's bytes are there, and nobody reads this step's any more
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        if (kAhead == 0 && kk * 2 + 1 >= tail) {
+#pragma unroll
+          for (int j = 0; j < kFm; ++j)
+            if (kk * 2 + hi >= tail) fx[kk & 1][j] = v4i{0, 0, 0, 0};
+        }
+        constexpr int kAll = kFn * kFm, kParts = kFn + kFm;
+#pragma unroll
+        for (int m = 0; m < kAll; ++m) {
+          const int i = m / kFm, j = m % kFm;
+          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][i], fx[kk & 1][j], acc[i][j],
+                                                            0, 0, 0);
+          // spread evenly over the products
+          for (int f = m * kParts / kAll; f < (m + 1) * kParts / kAll; ++f) {
+            if (kk < 3) fetch(s, kk + 1, f);
+            else if (kAhead > 0) fetch(s + 1, 0, f);
           }
-          if (a.bf16)
-            *reinterpret_cast<v2u *>(out + n * 2) =
+          if (kk == 3 && kAhead == 2)
+            for (int f = m * kLoads / kAll; f < (m + 1) * kLoads / kAll; ++f) issue(s + 2, f);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) issue(0, i);
+    if (steps > 1) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) issue(1, i);
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kLoads) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
+    }
+#pragma unroll
+    for (int f = 0; f < kFn + kFm; ++f) fetch(0, 0, f);
+    int s = 0;
+    for (; s < steps - 2; ++s) step(s, std::integral_constant<int, 2>());
+    if (s < steps - 1) step(s++, std::integral_constant<int, 1>());
+    step(s, std::integral_constant<int, 0>());
+
+    // 32 rows x 64 channels (32 in fp32) at a time through LDS, so that a row's
+    // channels leave in whole lines
+    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N;
+    const int nw = n0 + wn * kOutW;  // the wave's first channel
+    int8_t *stage = s_out[wave];
+    const int width = a.bf16 ? 64 : 32, esize = a.bf16 ? 2 : 4;
+#pragma unroll
+    for (int j = 0; j < kFm; ++j) {
+      const int r0 = wm * kFm * 32 + j * 32;
+      const float xs = r0 + lr < tile.rows ? a.xs[tile.row + r0 + lr] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kOutW / 32; ++i) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = nw + i * 32 + q * 8 + hi * 4;
+          float v[4] = {};
+          if (n < a.n_out) {
+            const v4f w0 = *reinterpret_cast<const v4f *>(ws + n);
+            if (kAct) {
+              const v4f w1 = *reinterpret_cast<const v4f *>(ws + half + n);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                v[e] = silu(static_cast<float>(acc[2 * i][j][q * 4 + e]) * xs * w0[e]) *
+                       (static_cast<float>(acc[kAct ? 2 * i + 1 : 0][j][q * 4 + e]) * xs * w1[e]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                v[e] = static_cast<float>(acc[i][j][q * 4 + e]) * xs * w0[e];
+            }
+          }
+          // 16-byte slots of the stage's 128-byte row, exchanged by the row
+          if (a.bf16) {
+            const int at = ((i & 1) * 4 + q) ^ (lr & 7);
+            *reinterpret_cast<v2u *>(stage + lr * 128 + at * 16 + hi * 8) =
                 v2u{round_bf16(v[0]) | (round_bf16(v[1]) << 16), round_bf16(v[2]) | (round_bf16(v[3]) << 16)};
-          else
-            *reinterpret_cast<v4f *>(out + n * 4) = v4f{v[0], v[1], v[2], v[3]};
+          } else {
+            const int at = (q * 2 + hi) ^ (lr & 7);
+            *reinterpret_cast<v4f *>(stage + lr * 128 + at * 16) = v4f{v[0], v[1], v[2], v[3]};
+          }
+        }
+        if (a.bf16 && (i & 1) == 0 && i + 1 < kOutW / 32) continue;
+        const int c0 = nw + (a.bf16 ? i / 2 * 64 : i * 32);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int r = p * 8 + lane / 8, slot16 = lane & 7;
+          const int n = c0 + slot16 * (16 / esize);
+          const v4u o = *reinterpret_cast<const v4u *>(stage + r * 128 + ((slot16 ^ (r & 7)) * 16));
+          if (r0 + r < tile.rows && n < a.n_out && n < c0 + width && n < nw + kOutW)
+            *reinterpret_cast<v4u *>(static_cast<char *>(a.y) +
+                                     ((tile.row + r0 + r) * a.n_out + n) * esize) = o;
         }
       }
     }
   }
+}
+
+template <int kN, int kM, int kWn, int kWm>
+static void start_matmul(const MatmulArgs &a, bool act, int n_cu, hipStream_t stream) {
+  const int out = act ? kN / 2 : kN;
+  const int32_t n_col = (a.n_out + out - 1) / out;
+  // every block may end in a part of a tile
+  const int64_t items = ((a.M + kM - 1) / kM + a.n_block) * n_col;
+  const dim3 grid(static_cast<unsigned>(items < n_cu ? (items + 7) / 8 * 8 : n_cu)), block(64 * kWn * kWm);
+  if (act)
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true>), grid, block, 0, stream, a, n_col);
+  else
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false>), grid, block, 0, stream, a, n_col);
 }
 
 hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, const int8_t *wq,
@@ -273,19 +402,9 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
                                 const int64_t *block_off, const int32_t *block_w, int32_t n_block,
                                 int32_t act, void *y, int32_t type, int32_t *status,
                                 hipStream_t stream) {
-  const int n_out = act ? N / 2 : N;
-  const MatmulArgs a{xq, xs, wq, ws, block_off, block_w, y, status, M, n_w, N, K, n_block, n_out,
-                     type == ULTRAEP_BF16};
-  const int bn = act ? kBn / 2 : kBn;
-  // every block may end in a part of a tile
-  const int64_t tiles = (M + kBm - 1) / kBm + n_block;
-  const int32_t n_col = (n_out + bn - 1) / bn;
-  const int64_t n_item = tiles * n_col;
-  const dim3 grid(static_cast<unsigned>(n_item < 1 << 23 ? n_item : 1 << 23));
-  if (act)
-    hipLaunchKernelGGL((k_matmul<true>), grid, dim3(kMmThreads), 0, stream, a, n_item, n_col);
-  else
-    hipLaunchKernelGGL((k_matmul<false>), grid, dim3(kMmThreads), 0, stream, a, n_item, n_col);
+  const MatmulArgs a{xq, xs, wq, ws, block_off, block_w, y, status, M, n_w, N, K, n_block,
+                     act ? N / 2 : N, type == ULTRAEP_BF16};
+  start_matmul<256, 256, 2, 2>(a, act, 256, stream);
   return hipGetLastError();
 }
 
