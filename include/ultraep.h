@@ -473,7 +473,7 @@ int ultraep_quant_rows(const void *x, int32_t type, int64_t rows, int64_t K, int
  * the sum in 32-bit integers (exact), the rest in fp32.  y[m] = v, or with
  * act 1 (SwiGLU, gate rows of the weight first)
  *   y[m][n] = v[n] / (1 + exp(-v[n])) * v[N/2 + n],  n < N/2
- * rounded to nearest-even to `type`, a NaN to 0x7FC0 in bf16.
+ * rounded to nearest-even to `type`.
  *   xq         [M][K] int8, x_scale [M] fp32
  *   wq         [n_w][N][K] int8, w_scale [n_w][N] fp32
  *   block_off  [n_block + 1] int64 (a part of the dispatch's is fine: rows
@@ -483,8 +483,8 @@ int ultraep_quant_rows(const void *x, int32_t type, int64_t rows, int64_t K, int
  * Blocks that are not in rising order within [0, M], and a nonempty block
  * whose weight is outside [0, n_w), raise ULTRAEP_EDATA and are skipped.
  * 1 <= n_block <= 2048, n_w >= 1, M < 2^31; K % 16 == 0, K <= 2^16 (the sum
- * stays within 32 bits), N % 8 == 0 (N % 16 == 0 with act), N <= 2^20; 16-byte
- * aligned xq, wq and y.  M = 1 is the decode form: any M takes any blocks. */
+ * stays within 32 bits), N % 8 == 0 (N % 16 == 0 with act), N <= 2^20,
+ * M * N < 2^40; 16-byte aligned xq, wq and y.  M = 1 is the decode form: any M takes any blocks. */
 int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
                           const int8_t *wq, const float *w_scale, int32_t n_w, int32_t N,
                           int32_t K, const int64_t *block_off, const int32_t *block_w,

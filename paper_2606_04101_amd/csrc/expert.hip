@@ -106,7 +106,7 @@ struct MatmulArgs {
   void *y;
   int32_t *status;
   int64_t M;
-  int32_t n_w, N, K, n_block, n_out, bf16;
+  int32_t n_w, N, K, n_block, n_out;
 };
 
 constexpr int kMmMaxBlocks = 2048;
@@ -157,6 +157,19 @@ __device__ void count_tiles(const MatmulArgs &a, int tile_rows, int *cum, int *w
   __syncthreads();
 }
 
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// v, with what follows from it computed where it is used: a persistent loop would
+// otherwise hold every lane's address of its rare parts in registers throughout
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // Tile `tile` < cum[n_block]: its first row, rows and weight.  Every lane must
 // be active; all results are uniform.
 struct RowTile {
@@ -176,8 +189,8 @@ __device__ __forceinline__ RowTile find_tile(const MatmulArgs &a, const int *cum
   const int j = g + lane;
   g += __builtin_popcountll(ballot(j < a.n_block && cum[min(j, a.n_block)] <= tile)) - 1;
   g = __builtin_amdgcn_readfirstlane(g);
-  const int64_t r = static_cast<int64_t>(tile - cum[g]) * tile_rows;
-  const int64_t lo = a.block_off[g], n = a.block_off[g + 1] - lo;
+  const int64_t r = static_cast<int64_t>(tile - __builtin_amdgcn_readfirstlane(cum[g])) * tile_rows;
+  const int64_t lo = uniform(a.block_off[g]), n = uniform(a.block_off[g + 1]) - lo;
   return {lo + r, __builtin_amdgcn_readfirstlane(static_cast<int>(min<int64_t>(n - r, tile_rows))),
           __builtin_amdgcn_readfirstlane(a.block_w ? a.block_w[g] : g)};
 }
@@ -193,13 +206,25 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint
                : "memory");
 }
 
+// the same for 4 bytes a lane
+__device__ __forceinline__ void load_word_to_lds(const void *base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
+               : "memory");
+}
+template <class T>
+__device__ __forceinline__ uint32_t lds_address(T *p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) T *)p));
+}
+
 constexpr int kBk = 128;  // bytes of K of a step
 
 // Output tile of kN weight rows x kM rows, K in steps of 128 bytes through two
 // LDS buffers; kWn x kWm waves.  The weights are the MFMA's first operand, so a
 // lane holds 4 neighbouring channels of one row.  With act, a wave's parts of 32
 // weight rows alternate between gates and their partners.
-template <int kN, int kM, int kWn, int kWm, bool kAct>
+template <int kN, int kM, int kWn, int kWm, bool kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t n_col) {
   constexpr int kThreads = 64 * kWn * kWm, kWaves = kWn * kWm;
   constexpr int kFn = kN / kWn / 32, kFm = kM / kWm / 32;  // 32 x 32 parts of a wave
@@ -210,6 +235,7 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   constexpr int kOutW = kOut / kWn;                        // of a wave
   __shared__ __align__(1024) int8_t s_buf[2][kBuf];
   __shared__ __align__(16) int8_t s_out[kWaves][4096];
+  __shared__ __align__(16) float s_scale[2][kN + kM];  // of this item and of the next
   __shared__ int s_cum[kMmMaxBlocks + 1];
   __shared__ int s_sums[kWaves];
   const int tid = threadIdx.x, lane = lane_id();
@@ -218,61 +244,88 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   const int lr = lane & 31, hi = lane >> 5;
   const int half = a.N / 2;
   count_tiles<kThreads>(a, kM, s_cum, s_sums);
-  const int n_tile = s_cum[a.n_block];
-  const int64_t n_item = static_cast<int64_t>(n_tile) * n_col;
+  const int n_tile = __builtin_amdgcn_readfirstlane(s_cum[a.n_block]);
+  const int n_item = n_tile * n_col;  // (a y that fits the memory has fewer than 2^31)
 
   // the workgroups of one XCD (those of equal number modulo 8) take neighbouring
   // items, 8 row tiles by 4 column tiles at a time
   constexpr int kXcd = 8, kGroup = 8;
   const int per_xcd = gridDim.x / kXcd;  // the grid is a multiple
-  const int64_t slot = static_cast<int64_t>(blockIdx.x % kXcd) * per_xcd + blockIdx.x / kXcd;
-  const uint32_t lds0 = static_cast<uint32_t>(
-      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int8_t *)&s_buf[0][0]));
+  const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
+  const uint32_t lds0 = lds_address(&s_buf[0][0]), lds_scale = lds_address(&s_scale[0][0]);
   const int steps = (a.K + kBk - 1) / kBk;
   const int tail = (a.K - (steps - 1) * kBk) / 16;  // chunks of the last step
 
-  for (int64_t item = slot; item < n_item; item += gridDim.x) {
-    const int group = static_cast<int>(item / (kGroup * n_col));
-    const int rest = static_cast<int>(item - static_cast<int64_t>(group) * kGroup * n_col);
+  // an item: its rows and weight, its first channel
+  RowTile tile;
+  int n0;
+  // byte offsets of this lane's loads: 8 rows of 8 chunks an instruction; chunk c of
+  // tile row r lies at c ^ (r / 2 % 8), so that 16 neighbouring rows' lie in all banks
+  const int8_t *wbase, *xbase;
+  uint32_t off[kLoads];
+  int turn = 1;  // which half of s_scale the item's scales are in
+  const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+  auto aim = [&](int item) {
+    const int lane = opaque(lane_id());
+    const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    const int group = item / (kGroup * n_col), rest = item - group * kGroup * n_col;
     const int high = min(kGroup, n_tile - group * kGroup);
-    const RowTile tile = find_tile(a, s_cum, group * kGroup + rest % high, kM);
-    const int n0 = rest / high * kOut;  // first channel
-
-    // byte offsets of this lane's loads: 8 rows of 8 chunks an instruction, the
-    // chunks of row r exchanged by r % 8 so that a column of chunks lies in all banks
-    const int8_t *wbase = a.wq + static_cast<int64_t>(tile.w) * a.N * a.K;
-    const int8_t *xbase = a.xq + tile.row * a.K;
-    uint32_t off[kLoads];
-    const int chunk = (lane & 7) ^ (lane >> 3);
+    tile = find_tile(a, s_cum, group * kGroup + rest % high, kM);
+    n0 = rest / high * kOut;
+    wbase = a.wq + static_cast<int64_t>(tile.w) * a.N * a.K;
+    xbase = a.xq + tile.row * a.K;
+    // weight row of tile row j, in range for any j
+    auto weight_row = [&](int j) {
+      if (!kAct) return min(n0 + j, a.N - 1);
+      return min(n0 + j / 64 * 32 + j % 32, half - 1) + (j % 64 >= 32 ? half : 0);
+    };
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      int r;
-      if (i < kLoadsN) {
-        const int j = (i * kWaves + wave) * 8 + (lane >> 3);  // tile row
-        if (kAct) {
-          const int o = n0 + j / 64 * 32 + j % 32;
-          r = min(o, half - 1) + (j % 64 >= 32 ? half : 0);
-        } else {
-          r = min(n0 + j, a.N - 1);
-        }
-      } else {
-        r = min(((i - kLoadsN) * kWaves + wave) * 8 + (lane >> 3), tile.rows - 1);
-      }
+      const int j = ((i < kLoadsN ? i : i - kLoadsN) * kWaves + wave) * 8 + (lane >> 3);
+      const int r = i < kLoadsN ? weight_row(j) : min(j, tile.rows - 1);
       off[i] = static_cast<uint32_t>(r) * a.K + chunk * 16;
     }
-    // load i of a step; chunks past K (in the last step) are loaded from the step's
-    // first one and not used
-    auto issue = [&](int s, int i) {
-      const uint32_t back = s == steps - 1 && chunk >= tail ? chunk * 16 : 0;
-      load_to_lds((i < kLoadsN ? wbase : xbase) + static_cast<int64_t>(s) * kBk, off[i] - back,
-                  __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * kBuf + (i * kWaves + wave) * 1024));
-    };
+    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N, *xs = a.xs + tile.row;
+    turn ^= 1;
+#pragma unroll
+    for (int i = 0; i < (kN + kM) / kWave / kWaves; ++i) {
+      const int j = (i * kWaves + wave) * kWave;  // the same operand for all lanes
+      const int r = j < kN ? weight_row(j + lane) : min(j - kN + lane, tile.rows - 1);
+      load_word_to_lds(j < kN ? ws : xs, r * 4,
+                       __builtin_amdgcn_readfirstlane(lds_scale + (turn * (kN + kM) + j) * 4));
+    }
+  };
+  // load i of a step; chunks past K (in the last step) are loaded from the step's
+  // first one and not used
+  auto issue = [&](int s, int i) {
+    const uint32_t back = s == steps - 1 && chunk >= tail ? chunk * 16 : 0;
+    load_to_lds((i < kLoadsN ? wbase : xbase) + static_cast<int64_t>(s) * kBk, off[i] - back,
+                __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * kBuf + (i * kWaves + wave) * 1024));
+  };
+  auto begin = [&](int item) {
+    aim(item);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) issue(0, i);
+    if (steps > 1) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) issue(1, i);
+    }
+  };
 
+  int item = slot;
+  if (item >= n_item) return;
+  begin(item);
+  if (steps > 1)
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  while (true) {
+    asm volatile("s_barrier" : : : "memory");
     v16i acc[kFn][kFm] = {};
     v4i fw[2][kFn], fx[2][kFm];
     // part f of the operands for 32 bytes kk of a step
     auto fetch = [&](int s, int kk, int f) {
-      const int8_t *b = s_buf[s & 1] + ((kk * 2 + hi) ^ (lane & 7)) * 16;
+      const int8_t *b = s_buf[s & 1] + ((kk * 2 + hi) ^ (lr >> 1 & 7)) * 16;
       if (f < kFn)
         fw[kk & 1][f] = *reinterpret_cast<const v4i *>(b + (wn * kFn * 32 + f * 32 + lr) * kBk);
       else
@@ -313,88 +366,97 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
     };
 
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) issue(0, i);
-    if (steps > 1) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) issue(1, i);
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kLoads) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
-    }
-#pragma unroll
     for (int f = 0; f < kFn + kFm; ++f) fetch(0, 0, f);
     int s = 0;
     for (; s < steps - 2; ++s) step(s, std::integral_constant<int, 2>());
     if (s < steps - 1) step(s++, std::integral_constant<int, 1>());
     step(s, std::integral_constant<int, 0>());
 
+    // the next item's first loads fly while this one's results leave
+    const RowTile out = tile;
+    const int nw = n0 + wn * kOutW;  // the wave's first channel
+    const int was = turn;
+    item += gridDim.x;
+    const bool more = item < n_item;
+    if (more) begin(item);
+
     // 32 rows x 64 channels (32 in fp32) at a time through LDS, so that a row's
     // channels leave in whole lines
-    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N;
-    const int nw = n0 + wn * kOutW;  // the wave's first channel
+    constexpr int kParts = kOutW / 32;
+    const int el = opaque(lane), er = el & 31, eh = el >> 5;
+    const float *scale = s_scale[was];
     int8_t *stage = s_out[wave];
-    const int width = a.bf16 ? 64 : 32, esize = a.bf16 ? 2 : 4;
 #pragma unroll
     for (int j = 0; j < kFm; ++j) {
-      const int r0 = wm * kFm * 32 + j * 32;
-      const float xs = r0 + lr < tile.rows ? a.xs[tile.row + r0 + lr] : 0.f;
+      const int r0 = (wm * kFm + j) * 32;
+      const float xs = scale[kN + r0 + er];
+      // the sums stay in the accumulation registers until here
 #pragma unroll
-      for (int i = 0; i < kOutW / 32; ++i) {
+      for (int i = 0; i < kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
+      // before the last stores: all loads, and the earlier stores, are done (and
+      // nothing read from LDS is held in registers from one part to the next)
+      if (j == kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      else asm volatile("" : : : "memory");
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int n = nw + i * 32 + q * 8 + hi * 4;
-          float v[4] = {};
-          if (n < a.n_out) {
-            const v4f w0 = *reinterpret_cast<const v4f *>(ws + n);
-            if (kAct) {
-              const v4f w1 = *reinterpret_cast<const v4f *>(ws + half + n);
+          const int f = kAct ? 2 * i : i;
+          const float *of = scale + wn * kFn * 32 + f * 32 + q * 8 + eh * 4;
+          const v4f w0 = *reinterpret_cast<const v4f *>(of);
+          float v[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                v[e] = silu(static_cast<float>(acc[2 * i][j][q * 4 + e]) * xs * w0[e]) *
-                       (static_cast<float>(acc[kAct ? 2 * i + 1 : 0][j][q * 4 + e]) * xs * w1[e]);
-            } else {
+          for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[f][j][q * 4 + e]) * xs * w0[e];
+          if (kAct) {
+            const v4f w1 = *reinterpret_cast<const v4f *>(of + 32);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                v[e] = static_cast<float>(acc[i][j][q * 4 + e]) * xs * w0[e];
-            }
+            for (int e = 0; e < 4; ++e)
+              v[e] = silu(v[e]) *
+                     (static_cast<float>(acc[kAct ? f + 1 : 0][j][q * 4 + e]) * xs * w1[e]);
           }
           // 16-byte slots of the stage's 128-byte row, exchanged by the row
-          if (a.bf16) {
-            const int at = ((i & 1) * 4 + q) ^ (lr & 7);
-            *reinterpret_cast<v2u *>(stage + lr * 128 + at * 16 + hi * 8) =
-                v2u{round_bf16(v[0]) | (round_bf16(v[1]) << 16), round_bf16(v[2]) | (round_bf16(v[3]) << 16)};
+          if (kBf16) {
+            const int at = ((i & 1) * 4 + q) ^ (er & 7);
+            *reinterpret_cast<v2u *>(stage + er * 128 + at * 16 + eh * 8) =
+                v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
           } else {
-            const int at = (q * 2 + hi) ^ (lr & 7);
-            *reinterpret_cast<v4f *>(stage + lr * 128 + at * 16) = v4f{v[0], v[1], v[2], v[3]};
+            const int at = (q * 2 + eh) ^ (er & 7);
+            *reinterpret_cast<v4f *>(stage + er * 128 + at * 16) = v4f{v[0], v[1], v[2], v[3]};
           }
         }
-        if (a.bf16 && (i & 1) == 0 && i + 1 < kOutW / 32) continue;
-        const int c0 = nw + (a.bf16 ? i / 2 * 64 : i * 32);
+        if (kBf16 && (i & 1) == 0 && i + 1 < kParts) continue;
+        const int c0 = nw + (kBf16 ? i / 2 * 64 : i * 32), esize = kBf16 ? 2 : 4;
+        const int c = (el & 7) * (16 / esize);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const int r = p * 8 + lane / 8, slot16 = lane & 7;
-          const int n = c0 + slot16 * (16 / esize);
-          const v4u o = *reinterpret_cast<const v4u *>(stage + r * 128 + ((slot16 ^ (r & 7)) * 16));
-          if (r0 + r < tile.rows && n < a.n_out && n < c0 + width && n < nw + kOutW)
+          const int r = p * 8 + el / 8;
+          const v4u o = *reinterpret_cast<const v4u *>(stage + r * 128 + ((el & 7) ^ (r & 7)) * 16);
+          if (r0 + r < out.rows && c0 + c < min(a.n_out, nw + kOutW))
             *reinterpret_cast<v4u *>(static_cast<char *>(a.y) +
-                                     ((tile.row + r0 + r) * a.n_out + n) * esize) = o;
+                                     ((out.row + r0 + r) * a.n_out + c0 + c) * esize) = o;
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if (!more) return;
   }
 }
 
 template <int kN, int kM, int kWn, int kWm>
-static void start_matmul(const MatmulArgs &a, bool act, int n_cu, hipStream_t stream) {
+static void start_matmul(const MatmulArgs &a, bool act, bool bf16, int n_cu, hipStream_t stream) {
   const int out = act ? kN / 2 : kN;
   const int32_t n_col = (a.n_out + out - 1) / out;
   // every block may end in a part of a tile
   const int64_t items = ((a.M + kM - 1) / kM + a.n_block) * n_col;
   const dim3 grid(static_cast<unsigned>(items < n_cu ? (items + 7) / 8 * 8 : n_cu)), block(64 * kWn * kWm);
-  if (act)
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true>), grid, block, 0, stream, a, n_col);
+  if (act && bf16)
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true, true>), grid, block, 0, stream, a, n_col);
+  else if (act)
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true, false>), grid, block, 0, stream, a, n_col);
+  else if (bf16)
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false, true>), grid, block, 0, stream, a, n_col);
   else
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false>), grid, block, 0, stream, a, n_col);
+    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false, false>), grid, block, 0, stream, a, n_col);
 }
 
 hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, const int8_t *wq,
@@ -403,8 +465,8 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
                                 int32_t act, void *y, int32_t type, int32_t *status,
                                 hipStream_t stream) {
   const MatmulArgs a{xq, xs, wq, ws, block_off, block_w, y, status, M, n_w, N, K, n_block,
-                     act ? N / 2 : N, type == ULTRAEP_BF16};
-  start_matmul<256, 256, 2, 2>(a, act, 256, stream);
+                     act ? N / 2 : N};
+  start_matmul<256, 256, 2, 2>(a, act, type == ULTRAEP_BF16, 256, stream);
   return hipGetLastError();
 }
 

@@ -57,6 +57,13 @@ __device__ __forceinline__ uint32_t round_bf16(float f) {
   return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
 }
 
+// two of them, a in the low half, by the converter (a NaN stays one)
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef float v2f __attribute__((ext_vector_type(2)));
+  typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2b));
+}
+
 __device__ __forceinline__ float readlane_f(float v, int l) {
   return __int_as_float(readlane(__float_as_int(v), l));
 }
