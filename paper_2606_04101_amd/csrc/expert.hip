@@ -111,58 +111,6 @@ struct MatmulArgs {
 
 constexpr int kMmMaxBlocks = 2048;
 
-// Row tiles are numbered block by block.  cum[g] becomes the number of tiles
-// before block g, cum[n_block] that of all; a block that is out of order or out
-// of [0, M], or has rows and no weight, is reported and has none.
-__device__ __forceinline__ int64_t block_rows(const MatmulArgs &a, int g, bool &bad) {
-  const int64_t lo = a.block_off[g], hi = a.block_off[g + 1];
-  if (lo < 0 || hi < lo || hi > a.M) {
-    bad = true;
-    return 0;
-  }
-  if (hi > lo) {
-    const int w = a.block_w ? a.block_w[g] : g;
-    if (w < 0 || w >= a.n_w) {
-      bad = true;
-      return 0;
-    }
-  }
-  return hi - lo;
-}
-template <int kThreads>
-__device__ void count_tiles(const MatmulArgs &a, int tile_rows, int *cum, int *wave_sums) {
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  const int per = (a.n_block + kThreads - 1) / kThreads;  // blocks of a thread
-  int mine = 0;
-  bool bad = false;
-  for (int j = 0; j < per; ++j) {
-    const int g = tid * per + j;
-    if (g < a.n_block)
-      mine += static_cast<int>((block_rows(a, g, bad) + tile_rows - 1) / tile_rows);
-  }
-  if (bad && blockIdx.x == 0) report(a.status, ULTRAEP_EDATA);
-  const int incl = wave_scan_incl(mine);
-  if (lane == kWave - 1) wave_sums[wave] = incl;
-  __syncthreads();
-  int at = incl - mine;
-  for (int w = 0; w < wave; ++w) at += wave_sums[w];
-  for (int j = 0; j < per; ++j) {
-    const int g = tid * per + j;
-    if (g < a.n_block) {
-      cum[g] = at;
-      at += static_cast<int>((block_rows(a, g, bad) + tile_rows - 1) / tile_rows);
-      if (g == a.n_block - 1) cum[a.n_block] = at;
-    }
-  }
-  __syncthreads();
-}
-
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-
 // v, with what follows from it computed where it is used: a persistent loop would
 // otherwise hold every lane's address of its rare parts in registers throughout
 __device__ __forceinline__ int opaque(int v) {
@@ -170,30 +118,90 @@ __device__ __forceinline__ int opaque(int v) {
   return v;
 }
 
-// Tile `tile` < cum[n_block]: its first row, rows and weight.  Every lane must
-// be active; all results are uniform.
+__device__ __forceinline__ int64_t readlane64(int64_t v, int l) {
+  const uint32_t lo = readlane(static_cast<int>(v), l), hi = readlane(static_cast<int>(v >> 32), l);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// an address that is the same in all lanes, in scalar registers
+template <class T>
+__device__ __forceinline__ T *uniform(T *p) {
+  const uintptr_t v = reinterpret_cast<uintptr_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+  return reinterpret_cast<T *>(static_cast<uintptr_t>(hi) << 32 | lo);
+}
+
+// A tile of rows of one block: its first row, rows and weight.
 struct RowTile {
   int64_t row;
   int32_t rows, w;
 };
-__device__ __forceinline__ RowTile find_tile(const MatmulArgs &a, const int *cum, int tile,
-                                             int tile_rows) {
-  // the last block that begins at or before the tile, among equals the last,
-  // which is the one with tiles: first its run of 64 blocks, then the block
-  const int lane = lane_id();
-  int g = 0;
-  if (a.n_block > kWave) {
-    const int j = lane * kWave;
-    g = (__builtin_popcountll(ballot(j < a.n_block && cum[min(j, a.n_block)] <= tile)) - 1) * kWave;
+
+// Row tiles are numbered block by block.  Blocks are looked at in runs of 64, one a
+// lane; a wave holds one run's blocks, and the runs' tile counts, in registers.  A
+// block that is out of order or out of [0, M], or has rows and no weight, is reported
+// and has no tile.  Every lane must be active in each call.
+template <int kTileRows>
+struct RowTiles {
+  int64_t lo;               // this lane's block of run `run`:
+  int rows, w;              //   its first row, rows, weight
+  int before, tiles;        //   its tiles, and the run's before it
+  int run, n_run;
+  int run_before, run_tiles;  // of run `lane`
+  int total;                // tiles in all
+
+  __device__ void load(const MatmulArgs &a, int r) {
+    run = r;
+    const int g = r * kWave + lane_id();
+    lo = 0;
+    rows = w = 0;
+    if (g < a.n_block) {
+      lo = a.block_off[g];
+      const int64_t hi = a.block_off[g + 1];
+      w = a.block_w ? a.block_w[g] : g;
+      if (lo < 0 || hi < lo || hi > a.M || (hi > lo && (w < 0 || w >= a.n_w)))
+        report(a.status, ULTRAEP_EDATA);
+      else
+        rows = static_cast<int>(hi - lo);
+    }
+    tiles = rows > 0 ? (rows - 1) / kTileRows + 1 : 0;
+    before = wave_scan_incl(tiles) - tiles;
   }
-  const int j = g + lane;
-  g += __builtin_popcountll(ballot(j < a.n_block && cum[min(j, a.n_block)] <= tile)) - 1;
-  g = __builtin_amdgcn_readfirstlane(g);
-  const int64_t r = static_cast<int64_t>(tile - __builtin_amdgcn_readfirstlane(cum[g])) * tile_rows;
-  const int64_t lo = uniform(a.block_off[g]), n = uniform(a.block_off[g + 1]) - lo;
-  return {lo + r, __builtin_amdgcn_readfirstlane(static_cast<int>(min<int64_t>(n - r, tile_rows))),
-          __builtin_amdgcn_readfirstlane(a.block_w ? a.block_w[g] : g)};
-}
+  // s_run: 32 words of LDS, free again after the call's last barrier
+  __device__ void count(const MatmulArgs &a, int *s_run, int wave, int n_waves) {
+    n_run = (a.n_block + kWave - 1) / kWave;
+    if (n_run == 1) {
+      load(a, 0);
+      run_before = 0;
+      total = readlane(before + tiles, kWave - 1);
+      run_tiles = lane_id() == 0 ? total : 0;
+      return;
+    }
+    for (int r = wave; r < n_run; r += n_waves) {
+      load(a, r);
+      if (lane_id() == kWave - 1) s_run[r] = before + tiles;
+    }
+    __syncthreads();
+    run_tiles = lane_id() < n_run ? s_run[lane_id()] : 0;
+    __syncthreads();
+    run_before = wave_scan_incl(run_tiles) - run_tiles;
+    total = readlane(run_before, kWave - 1);  // (fewer than 64 runs)
+    run = -1;
+  }
+  // tile < total
+  __device__ RowTile find(const MatmulArgs &a, int tile) {
+    int t = tile;
+    if (n_run > 1) {
+      const int r = __builtin_ctzll(ballot(tile >= run_before && tile < run_before + run_tiles));
+      t -= readlane(run_before, r);
+      if (r != run) load(a, r);
+    }
+    const int l = __builtin_ctzll(ballot(t >= before && t < before + tiles));
+    const int first = (t - readlane(before, l)) * kTileRows;
+    return {readlane64(lo, l) + first, min(readlane(rows, l) - first, kTileRows), readlane(w, l)};
+  }
+};
 
 __device__ __forceinline__ float silu(float v) { return v / (1.f + expf(-v)); }
 
@@ -224,7 +232,7 @@ constexpr int kBk = 128;  // bytes of K of a step
 // LDS buffers; kWn x kWm waves.  The weights are the MFMA's first operand, so a
 // lane holds 4 neighbouring channels of one row.  With act, a wave's parts of 32
 // weight rows alternate between gates and their partners.
-template <int kN, int kM, int kWn, int kWm, bool kAct, bool kBf16>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t n_col) {
   constexpr int kThreads = 64 * kWn * kWm, kWaves = kWn * kWm;
   constexpr int kFn = kN / kWn / 32, kFm = kM / kWm / 32;  // 32 x 32 parts of a wave
@@ -233,18 +241,20 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   constexpr int kLoadsN = kLoads * kN / (kN + kM);
   constexpr int kOut = kAct ? kN / 2 : kN;                 // channels of a tile
   constexpr int kOutW = kOut / kWn;                        // of a wave
-  __shared__ __align__(1024) int8_t s_buf[2][kBuf];
-  __shared__ __align__(16) int8_t s_out[kWaves][4096];
-  __shared__ __align__(16) float s_scale[2][kN + kM];  // of this item and of the next
-  __shared__ int s_cum[kMmMaxBlocks + 1];
-  __shared__ int s_sums[kWaves];
+  constexpr int kTurns = kAhead ? 2 : 1;
+  static_assert(!kAct || kFn % 2 == 0, "a wave has gates with their partners");
+  static_assert(kAhead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
+  __shared__ __align__(1024) int8_t s_lds[2 * kBuf + (kAhead ? kWaves * 4096 : 0)];
+  __shared__ __align__(16) float s_scale[kTurns][kN + kM];  // of this item, and of the next
+  __shared__ int s_run[32];
   const int tid = threadIdx.x, lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wn = wave % kWn, wm = wave / kWn;
   const int lr = lane & 31, hi = lane >> 5;
   const int half = a.N / 2;
-  count_tiles<kThreads>(a, kM, s_cum, s_sums);
-  const int n_tile = __builtin_amdgcn_readfirstlane(s_cum[a.n_block]);
+  RowTiles<kM> tiles;
+  tiles.count(a, s_run, wave, kWaves);
+  const int n_tile = tiles.total;
   const int n_item = n_tile * n_col;  // (a y that fits the memory has fewer than 2^31)
 
   // the workgroups of one XCD (those of equal number modulo 8) take neighbouring
@@ -252,7 +262,7 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   constexpr int kXcd = 8, kGroup = 8;
   const int per_xcd = gridDim.x / kXcd;  // the grid is a multiple
   const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
-  const uint32_t lds0 = lds_address(&s_buf[0][0]), lds_scale = lds_address(&s_scale[0][0]);
+  const uint32_t lds0 = lds_address(s_lds), lds_scale = lds_address(&s_scale[0][0]);
   const int steps = (a.K + kBk - 1) / kBk;
   const int tail = (a.K - (steps - 1) * kBk) / 16;  // chunks of the last step
 
@@ -263,21 +273,21 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   // tile row r lies at c ^ (r / 2 % 8), so that 16 neighbouring rows' lie in all banks
   const int8_t *wbase, *xbase;
   uint32_t off[kLoads];
-  int turn = 1;  // which half of s_scale the item's scales are in
+  int turn = 0;  // which part of s_scale the item's scales are in
   const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
   auto aim = [&](int item) {
     const int lane = opaque(lane_id());
     const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
     const int group = item / (kGroup * n_col), rest = item - group * kGroup * n_col;
     const int high = min(kGroup, n_tile - group * kGroup);
-    tile = find_tile(a, s_cum, group * kGroup + rest % high, kM);
+    tile = tiles.find(a, group * kGroup + rest % high);
     n0 = rest / high * kOut;
-    wbase = a.wq + static_cast<int64_t>(tile.w) * a.N * a.K;
-    xbase = a.xq + tile.row * a.K;
-    // weight row of tile row j, in range for any j
+    wbase = uniform(a.wq + (static_cast<int64_t>(tile.w) * a.N + n0) * a.K);
+    xbase = uniform(a.xq + tile.row * a.K);
+    // weight row of tile row j after the tile's first (with act, among the gates or
+    // among their partners), in range for any j
     auto weight_row = [&](int j) {
-      if (!kAct) return min(n0 + j, a.N - 1);
-      return min(n0 + j / 64 * 32 + j % 32, half - 1) + (j % 64 >= 32 ? half : 0);
+      return kAct ? min(j / 64 * 32 + j % 32, half - 1 - n0) : min(j, a.N - 1 - n0);
     };
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -285,12 +295,15 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
       const int r = i < kLoadsN ? weight_row(j) : min(j, tile.rows - 1);
       off[i] = static_cast<uint32_t>(r) * a.K + chunk * 16;
     }
-    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N, *xs = a.xs + tile.row;
-    turn ^= 1;
+    const float *ws = uniform(a.ws + static_cast<int64_t>(tile.w) * a.N + n0);
+    const float *xs = uniform(a.xs + tile.row);
+    if (kAhead) turn ^= 1;
 #pragma unroll
-    for (int i = 0; i < (kN + kM) / kWave / kWaves; ++i) {
-      const int j = (i * kWaves + wave) * kWave;  // the same operand for all lanes
-      const int r = j < kN ? weight_row(j + lane) : min(j - kN + lane, tile.rows - 1);
+    for (int i = 0; i < kN + kM; i += kWaves * kWave) {
+      const int j = i + wave * kWave;  // the same operand for all lanes
+      if (j >= kN + kM) break;
+      const int r = j >= kN ? min(j - kN + lane, tile.rows - 1)
+                            : weight_row(j + lane) + (kAct && lane >= 32 ? half : 0);
       load_word_to_lds(j < kN ? ws : xs, r * 4,
                        __builtin_amdgcn_readfirstlane(lds_scale + (turn * (kN + kM) + j) * 4));
     }
@@ -299,7 +312,11 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
   // first one and not used
   auto issue = [&](int s, int i) {
     const uint32_t back = s == steps - 1 && chunk >= tail ? chunk * 16 : 0;
-    load_to_lds((i < kLoadsN ? wbase : xbase) + static_cast<int64_t>(s) * kBk, off[i] - back,
+    const int8_t *base = i >= kLoadsN ? xbase
+                         : kAct && (i * kWaves + wave) * 8 % 64 >= 32
+                             ? wbase + static_cast<int64_t>(half) * a.K
+                             : wbase;
+    load_to_lds(base + static_cast<int64_t>(s) * kBk, off[i] - back,
                 __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * kBuf + (i * kWaves + wave) * 1024));
   };
   auto begin = [&](int item) {
@@ -312,20 +329,24 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
     }
   };
 
+  auto arrived = [&] {  // the first step's bytes are there
+    if (steps > 1)
+      asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  };
+
   int item = slot;
   if (item >= n_item) return;
   begin(item);
-  if (steps > 1)
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
-  else
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  arrived();
   while (true) {
     asm volatile("s_barrier" : : : "memory");
     v16i acc[kFn][kFm] = {};
     v4i fw[2][kFn], fx[2][kFm];
     // part f of the operands for 32 bytes kk of a step
     auto fetch = [&](int s, int kk, int f) {
-      const int8_t *b = s_buf[s & 1] + ((kk * 2 + hi) ^ (lr >> 1 & 7)) * 16;
+      const int8_t *b = s_lds + (s & 1) * kBuf + ((kk * 2 + hi) ^ (lr >> 1 & 7)) * 16;
       if (f < kFn)
         fw[kk & 1][f] = *reinterpret_cast<const v4i *>(b + (wn * kFn * 32 + f * 32 + lr) * kBk);
       else
@@ -334,15 +355,15 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
     };
     // One step, its first parts already in registers.  The products run in the
     // order that keeps the matrix unit fed: reads of the next parts, and at the
-    // step's end the loads of the step after the next, between them.  kAhead: how
+    // step's end the loads of the step after the next, between them.  kMore: how
     // many steps follow, up to 2.
     auto step = [&](int s, auto ahead) {
-      constexpr int kAhead = decltype(ahead)::value;
+      constexpr int kMore = decltype(ahead)::value;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         if (kk == 3)  // the next step's bytes are there, and nobody reads this step's any more
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-        if (kAhead == 0 && kk * 2 + 1 >= tail) {
+        if (kMore == 0 && kk * 2 + 1 >= tail) {
 #pragma unroll
           for (int j = 0; j < kFm; ++j)
             if (kk * 2 + hi >= tail) fx[kk & 1][j] = v4i{0, 0, 0, 0};
@@ -356,9 +377,9 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
           // spread evenly over the products
           for (int f = m * kParts / kAll; f < (m + 1) * kParts / kAll; ++f) {
             if (kk < 3) fetch(s, kk + 1, f);
-            else if (kAhead > 0) fetch(s + 1, 0, f);
+            else if (kMore > 0) fetch(s + 1, 0, f);
           }
-          if (kk == 3 && kAhead == 2)
+          if (kk == 3 && kMore == 2)
             for (int f = m * kLoads / kAll; f < (m + 1) * kLoads / kAll; ++f) issue(s + 2, f);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -372,20 +393,20 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
     if (s < steps - 1) step(s++, std::integral_constant<int, 1>());
     step(s, std::integral_constant<int, 0>());
 
-    // the next item's first loads fly while this one's results leave
+    // (kAhead) the next item's first loads fly while this one's results leave
     const RowTile out = tile;
     const int nw = n0 + wn * kOutW;  // the wave's first channel
     const int was = turn;
     item += gridDim.x;
     const bool more = item < n_item;
-    if (more) begin(item);
+    if (kAhead && more) begin(item);
 
     // 32 rows x 64 channels (32 in fp32) at a time through LDS, so that a row's
     // channels leave in whole lines
     constexpr int kParts = kOutW / 32;
     const int el = opaque(lane), er = el & 31, eh = el >> 5;
     const float *scale = s_scale[was];
-    int8_t *stage = s_out[wave];
+    int8_t *stage = s_lds + (kAhead ? 2 * kBuf : 0) + wave * 4096;
 #pragma unroll
     for (int j = 0; j < kFm; ++j) {
       const int r0 = (wm * kFm + j) * 32;
@@ -395,7 +416,7 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
       for (int i = 0; i < kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
       // before the last stores: all loads, and the earlier stores, are done (and
       // nothing read from LDS is held in registers from one part to the next)
-      if (j == kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      if (kAhead && j == kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       else asm volatile("" : : : "memory");
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
@@ -439,24 +460,174 @@ __global__ void __launch_bounds__(64 * kWn *kWm) k_matmul(MatmulArgs a, int32_t 
       }
     }
     if (!more) return;
+    if (!kAhead) {
+      __syncthreads();
+      begin(item);
+      arrived();
+    }
   }
 }
 
-template <int kN, int kM, int kWn, int kWm>
-static void start_matmul(const MatmulArgs &a, bool act, bool bf16, int n_cu, hipStream_t stream) {
+// Few rows a block: the weight's bytes bound the call.  A workgroup takes kRows weight
+// rows (with act half of them gates, then their partners) and up to kTok rows.  Its
+// waves share K in steps of 128 bytes in turn, each through an LDS ring of its own that
+// kDeep steps fill, so no wave waits for another until they add their sums.
+template <int kTok, int kRows, int kWaves, int kDeep, bool kAct, bool kBf16>
+__global__ void __launch_bounds__(64 * kWaves) k_matmul_thin(MatmulArgs a, int32_t n_col) {
+  constexpr int kThreads = 64 * kWaves, kFm = kTok / 16, kFn = kRows / 16;
+  constexpr int kOut = kAct ? kRows / 2 : kRows;
+  constexpr int kPitch = kRows + 4;  // words of a row's sums
+  constexpr int kStep = (kRows + kTok) * kBk, kLoadsN = kRows / 8, kLoads = (kRows + kTok) / 8;
+  constexpr int kRing = kDeep * kStep;
+  static_assert(kTok * kPitch * 4 <= kRing, "a wave's sums take the place of its ring");
+  __shared__ __align__(1024) int8_t s_ring[kWaves][kRing];
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lr = lane & 15, lc = lane >> 4;
+  const int half = a.N / 2;
+  RowTiles<kTok> tiles;
+  tiles.count(a, reinterpret_cast<int *>(s_ring[0]), wave, kWaves);
+  const int n_item = tiles.total * n_col;
+  const int n_chunk = a.K / 16, steps = (a.K + kBk - 1) / kBk;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(&s_ring[wave][0]));
+
+  for (int item = blockIdx.x; item < n_item; item += gridDim.x) {
+    const RowTile tile = tiles.find(a, item / n_col);
+    const int n0 = item % n_col * kOut;
+    const int8_t *w = uniform(a.wq + (static_cast<int64_t>(tile.w) * a.N + n0) * a.K);
+    const int8_t *x = uniform(a.xq + tile.row * a.K);
+    // byte offsets of this lane's rows: 8 rows of 8 chunks an instruction, chunk c of
+    // row r at c ^ (r / 2 % 8) as in the wide tiles
+    uint32_t off[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int j = (i < kLoadsN ? i : i - kLoadsN) * 8 + (lane >> 3);
+      const int r = i >= kLoadsN ? min(j, tile.rows - 1)
+                    : kAct       ? min(j % kOut, half - 1 - n0)
+                                 : min(j, a.N - 1 - n0);
+      off[i] = static_cast<uint32_t>(r) * a.K;
+    }
+    // step s of the wave into part s % kDeep of the ring; what lies past K is loaded
+    // from its last chunk and multiplied by 0
+    const int chunk = (lane & 7) ^ (lane >> 4);
+    auto issue = [&](int s, int slot) {
+      const uint32_t at[2] = {min(s * 8 + chunk, n_chunk - 1) * 16u, min(s * 8 + (chunk ^ 4), n_chunk - 1) * 16u};
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int8_t *base = i >= kLoadsN                   ? x
+                             : kAct && i >= kLoadsN / 2 ? w + static_cast<int64_t>(half) * a.K
+                                                            : w;
+        load_to_lds(base, off[i] + at[i & 1],
+                    __builtin_amdgcn_readfirstlane(lds0 + slot * kStep + i * 1024));
+      }
+    };
+
+    v4i acc[kFn][kFm] = {};
+#pragma unroll
+    for (int b = 0; b < kDeep; ++b) issue(wave + b * kWaves, b);
+    for (int s0 = wave; s0 < steps; s0 += kDeep * kWaves) {
+#pragma unroll
+      for (int b = 0; b < kDeep; ++b) {
+        const int s = s0 + b * kWaves;
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kDeep - 1) * kLoads) : "memory");
+        const int8_t *part = s_ring[wave] + b * kStep;
+        v4i fw[2][kFn], fx[2][kFm];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = lr * kBk + ((h * 4 + lc) ^ (lr >> 1)) * 16;
+#pragma unroll
+          for (int i = 0; i < kFn; ++i)
+            fw[h][i] = *reinterpret_cast<const v4i *>(part + i * 16 * kBk + at);
+#pragma unroll
+          for (int j = 0; j < kFm; ++j) {
+            fx[h][j] = *reinterpret_cast<const v4i *>(part + (kRows + j * 16) * kBk + at);
+            if (s * 8 + h * 4 + lc >= n_chunk) fx[h][j] = v4i{0, 0, 0, 0};
+          }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the part is free
+        issue(s + kDeep * kWaves, b);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < kFm; ++j)
+#pragma unroll
+            for (int i = 0; i < kFn; ++i)
+              acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[h][i], fx[h][j], acc[i][j], 0, 0, 0);
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+
+    // lane: row lr of a 16 x 16 part, weight rows 4 lc ..
+    int *sums = reinterpret_cast<int *>(s_ring[wave]);
+#pragma unroll
+    for (int i = 0; i < kFn; ++i)
+#pragma unroll
+      for (int j = 0; j < kFm; ++j)
+        *reinterpret_cast<v4i *>(sums + (j * 16 + lr) * kPitch + i * 16 + lc * 4) = acc[i][j];
+    __syncthreads();
+    const float *ws = a.ws + static_cast<int64_t>(tile.w) * a.N;
+    for (int o = tid; o < kTok * kOut / 4; o += kThreads) {  // four channels of a row
+      const int r = o / (kOut / 4), c = o % (kOut / 4) * 4, n = n0 + c;
+      if (r >= tile.rows || n >= a.n_out) continue;
+      const float xs = a.xs[tile.row + r];
+      auto scaled = [&](int at, int channel) {  // four of the row's products
+        v4i sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < kWaves; ++u)
+          sum += *reinterpret_cast<const v4i *>(reinterpret_cast<int *>(s_ring[u]) + r * kPitch + at);
+        v4f v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * xs * ws[channel + e];
+        return v;
+      };
+      v4f v = scaled(c, n);
+      if (kAct) {
+        const v4f up = scaled(c + kOut, half + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * up[e];
+      }
+      char *out = static_cast<char *>(a.y) + ((tile.row + r) * a.n_out + n) * (kBf16 ? 2 : 4);
+      if (kBf16)
+        *reinterpret_cast<v2u *>(out) = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+      else
+        *reinterpret_cast<v4f *>(out) = v;
+    }
+    __syncthreads();
+  }
+}
+
+// most row tiles that M rows in n_block blocks make: every block that has rows may
+// end in a part of a tile
+static int64_t most_tiles(const MatmulArgs &a, int tile_rows) {
+  return a.M / tile_rows + (a.M < a.n_block ? a.M : a.n_block);
+}
+
+#define UEP_LAUNCH_MATMUL(kernel, ...)                                                         \
+  if (act && bf16)                                                                             \
+    hipLaunchKernelGGL((kernel<__VA_ARGS__, true, true>), grid, block, 0, stream, a, n_col);   \
+  else if (act)                                                                                \
+    hipLaunchKernelGGL((kernel<__VA_ARGS__, true, false>), grid, block, 0, stream, a, n_col);  \
+  else if (bf16)                                                                               \
+    hipLaunchKernelGGL((kernel<__VA_ARGS__, false, true>), grid, block, 0, stream, a, n_col);  \
+  else                                                                                         \
+    hipLaunchKernelGGL((kernel<__VA_ARGS__, false, false>), grid, block, 0, stream, a, n_col)
+
+template <int kTok, int kRows, int kWaves, int kDeep>
+static void start_thin(const MatmulArgs &a, bool act, bool bf16, hipStream_t stream) {
+  const int out = act ? kRows / 2 : kRows;
+  const int32_t n_col = (a.n_out + out - 1) / out;
+  const int64_t items = most_tiles(a, kTok) * n_col;
+  const dim3 grid(static_cast<unsigned>(items < 1 << 16 ? items : 1 << 16)), block(64 * kWaves);
+  UEP_LAUNCH_MATMUL(k_matmul_thin, kTok, kRows, kWaves, kDeep);
+}
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead>
+static void start_matmul(const MatmulArgs &a, bool act, bool bf16, int n_wg, hipStream_t stream) {
   const int out = act ? kN / 2 : kN;
   const int32_t n_col = (a.n_out + out - 1) / out;
-  // every block may end in a part of a tile
-  const int64_t items = ((a.M + kM - 1) / kM + a.n_block) * n_col;
-  const dim3 grid(static_cast<unsigned>(items < n_cu ? (items + 7) / 8 * 8 : n_cu)), block(64 * kWn * kWm);
-  if (act && bf16)
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true, true>), grid, block, 0, stream, a, n_col);
-  else if (act)
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, true, false>), grid, block, 0, stream, a, n_col);
-  else if (bf16)
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false, true>), grid, block, 0, stream, a, n_col);
-  else
-    hipLaunchKernelGGL((k_matmul<kN, kM, kWn, kWm, false, false>), grid, block, 0, stream, a, n_col);
+  const int64_t items = most_tiles(a, kM) * n_col;
+  const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
+  UEP_LAUNCH_MATMUL(k_matmul, kN, kM, kWn, kWm, kAhead);
 }
 
 hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, const int8_t *wq,
@@ -466,7 +637,46 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
                                 hipStream_t stream) {
   const MatmulArgs a{xq, xs, wq, ws, block_off, block_w, y, status, M, n_w, N, K, n_block,
                      act ? N / 2 : N};
-  start_matmul<256, 256, 2, 2>(a, act, type == ULTRAEP_BF16, 256, stream);
+  const bool bf16 = type == ULTRAEP_BF16;
+  // Tiles of 256 x 256 where the blocks are large and fill the 256 compute units in
+  // nearly whole rounds; else smaller ones, so that there are enough of them and few
+  // rows are padding; else, for few rows, the kernel that shares K between waves.
+  // `rows`: mean of a block that has any; tiles: estimated row tiles, half a tile of
+  // padding a block.  Measured, us (256 x 256 / 128 x 128 / 128 x 64 / thin 64 / 32 / 16):
+  //   10 blocks, N = 4096, K = 7168, act: M = 8192 313 / 303 / 408 / 454 / 561 / 808,
+  //   2048 112 / 128 / 156 / 152 / 182 / 250, 1024 105 / 81 / 112 / 100 / 118 / 148,
+  //   512 102 / 76 / 71 / 76 / 83 / 96, 256 101 / 69 / 69 / 66 / 65 / 68, 64 98 / 67 / 65
+  //   / 64 / 58 / 51
+  //   1 block, the same: M = 4096 108 / 121 / 163 / 204, 1024 78 / 44 / 44 / 53 / 70, 256
+  //   79 / 38 / 34 / 18 / 22 / 26, 128 79 / 38 / 34 / 17 / 13 / 17, 16 78 / 37 / 34 / 16 / 11 / 9
+  //   64 blocks, N = 1024, K = 2048: M = 8192 45 / 51 / 56 / 64, 4096 40 / 29 / 40 / 44,
+  //   1024 34 / 25 / 25 / 30 / 29 / 28
+  //   6 blocks, N = 4096, K = 1408: M = 8192 76 / 74 / 99, 512 24 / 15 / 13 / 18 / 18 / 19,
+  //   256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11 / 11 / 11 / 10
+  const int64_t blocks = M < n_block ? M : n_block, rows = (M + blocks - 1) / blocks;
+  auto items = [&](int64_t tile_rows, int64_t channels) {
+    return (M / tile_rows + (blocks + 1) / 2) * ((N + channels - 1) / channels);
+  };
+  const int64_t big = items(256, 256), rounds = (big + 255) / 256;
+  const bool deep = K >= 4096;  // four waves' worth of steps
+  if (rows > 96 && big * 5 >= rounds * 256 * 4)
+    start_matmul<256, 256, 2, 2, true>(a, act, bf16, 256, stream);
+  else if (rows > 56 && items(128, 128) >= 256)
+    start_matmul<128, 128, 2, 2, false>(a, act, bf16, 512, stream);
+  else if (rows > 32 && items(64, 128) >= 320)
+    start_matmul<128, 64, 2, 1, false>(a, act, bf16, 768, stream);
+  else if (rows > 32 && items(64, 64) >= 256 && deep)
+    start_thin<64, 64, 4, 2>(a, act, bf16, stream);
+  else if (rows > 32 && items(64, 64) >= 256)
+    start_thin<64, 64, 2, 2>(a, act, bf16, stream);
+  else if (rows > 12 && items(32, 64) >= 256 && deep)
+    start_thin<32, 64, 4, 2>(a, act, bf16, stream);
+  else if (rows > 12 && items(32, 64) >= 256)
+    start_thin<32, 64, 2, 2>(a, act, bf16, stream);
+  else if (deep)
+    start_thin<16, 32, 4, 2>(a, act, bf16, stream);
+  else
+    start_thin<16, 64, 2, 2>(a, act, bf16, stream);
   return hipGetLastError();
 }
 
