@@ -228,42 +228,44 @@ __global__ void __launch_bounds__(kRtThreads) k_route(RouteArgs a) {
   }
 }
 
-// A sequence's partials, summed in chunk order by four waves.  64 experts a
-// workgroup; the first workgroup of a sequence also sums its tokens.
-__global__ void __launch_bounds__(kRtThreads)
+// A sequence's partials, 16 experts a workgroup: 64 threads an expert take the chunks in
+// turn, then the 64 sums are added in order of the thread.  The first workgroup of a
+// sequence also sums its tokens.
+constexpr int kRsThreads = 1024, kRsExperts = 16, kRsTurns = kRsThreads / kRsExperts;
+__global__ void __launch_bounds__(kRsThreads)
 k_route_sum(const int32_t *__restrict__ part_c, const float *__restrict__ part_p,
             const int32_t *__restrict__ part_n, int64_t n_chunk, int32_t E, int32_t n_eb,
             int32_t *__restrict__ counts, float *__restrict__ prob_sum,
             int32_t *__restrict__ tokens) {
-  __shared__ float s_p[kRtWaves][kWave];
-  __shared__ int s_c[kRtWaves][kWave];
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  __shared__ float s_p[kRsTurns][kRsExperts];
+  __shared__ int s_c[kRsTurns][kRsExperts];
   const int64_t seg = blockIdx.x / n_eb;
   const int eb = static_cast<int>(blockIdx.x - seg * n_eb);
-  const int e = eb * kWave + lane;
+  const int i = threadIdx.x % kRsExperts, turn = threadIdx.x / kRsExperts;
+  const int e = eb * kRsExperts + i;
   float p = 0.f;
   int c = 0;
   if (e < E)
-    for (int64_t j = wave; j < n_chunk; j += kRtWaves) {
+    for (int64_t j = turn; j < n_chunk; j += kRsTurns) {
       p += part_p[(seg * n_chunk + j) * E + e];
       c += part_c[(seg * n_chunk + j) * E + e];
     }
-  s_p[wave][lane] = p;
-  s_c[wave][lane] = c;
+  s_p[turn][i] = p;
+  s_c[turn][i] = c;
+  if (eb == 0 && threadIdx.x >= kRsThreads - kWave) {  // the last wave
+    int n = 0;
+    for (int64_t j = lane_id(); j < n_chunk; j += kWave) n += part_n[seg * n_chunk + j];
+    n = wave_sum(n);
+    if (lane_id() == 0) tokens[seg] = n;
+  }
   __syncthreads();
-  if (wave == 0 && e < E) {
-    for (int w = 1; w < kRtWaves; ++w) {
-      p += s_p[w][lane];
-      c += s_c[w][lane];
+  if (turn == 0 && e < E) {
+    for (int w = 1; w < kRsTurns; ++w) {
+      p += s_p[w][i];
+      c += s_c[w][i];
     }
     prob_sum[seg * E + e] = p;
     counts[seg * E + e] = c;
-  }
-  if (eb == 0 && wave == 1) {
-    int n = 0;
-    for (int64_t j = lane; j < n_chunk; j += kWave) n += part_n[seg * n_chunk + j];
-    n = wave_sum(n);
-    if (lane == 0) tokens[seg] = n;
   }
 }
 
@@ -423,7 +425,10 @@ RouteShape route_shape(int64_t T, const ultraep_router &r) {
   s.seq = r.seq_len > 0 ? r.seq_len : (T > 0 ? T : 1);
   if (s.seq > T && T > 0) s.seq = T;
   s.n_seg = T > 0 ? (T + s.seq - 1) / s.seq : 1;
-  s.chunk = 16;
+  // about 512 workgroups, and no partials where one workgroup has few tokens anyway
+  s.chunk = (T + 511) / 512;
+  s.chunk = s.chunk < 4 ? 4 : (s.chunk + 3) / 4 * 4;
+  if (s.seq <= 16) s.chunk = 16;
   s.n_chunk = (s.seq + s.chunk - 1) / s.chunk;
   return s;
 }
@@ -471,8 +476,8 @@ hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
     else start_route<false, false>(l.vpl, grid, stream, a);
   }
   if (stats && s.n_chunk > 1) {
-    const int n_eb = (r.E + kWave - 1) / kWave;
-    hipLaunchKernelGGL(k_route_sum, dim3(static_cast<unsigned>(s.n_seg * n_eb)), dim3(kRtThreads), 0,
+    const int n_eb = (r.E + kRsExperts - 1) / kRsExperts;
+    hipLaunchKernelGGL(k_route_sum, dim3(static_cast<unsigned>(s.n_seg * n_eb)), dim3(kRsThreads), 0,
                        stream, a.counts, a.prob_sum, a.tokens, s.n_chunk, r.E, n_eb, counts, prob_sum,
                        tokens);
   }
