@@ -68,34 +68,57 @@ __device__ __forceinline__ float readlane_f(float v, int l) {
   return __int_as_float(readlane(__float_as_int(v), l));
 }
 
-// Float reductions over the 64 lanes, each in one fixed order (DPP mirrors
-// inside rows of 16 lanes, then the four rows in order).  Every lane must be
-// active.
+// Reductions over rows of 16 lanes (DPP mirrors) or over the 64 of a wave (the rows'
+// results in order), each in one fixed order.  Every lane must be active.
 template <int kCtrl>
 __device__ __forceinline__ float dpp_f(float v) {
-  const int i = __float_as_int(v);
-  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, kCtrl, 0xF, 0xF, false));
+  // (each control used reads a lane of the row for every lane)
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kCtrl, 0xF, 0xF, true));
 }
-__device__ __forceinline__ float wave_sum_f(float v) {
+template <int kLanes>
+__device__ __forceinline__ float lanes_sum(float v) {
   v += dpp_f<0xB1>(v);   // quad_perm 1,0,3,2
   v += dpp_f<0x4E>(v);   // quad_perm 2,3,0,1
   v += dpp_f<0x141>(v);  // row_half_mirror
   v += dpp_f<0x140>(v);  // row_mirror
+  if (kLanes == 16) return v;
   return (readlane_f(v, 0) + readlane_f(v, 16)) + (readlane_f(v, 32) + readlane_f(v, 48));
 }
-__device__ __forceinline__ float wave_max_f(float v) {
-  v = fmaxf(v, dpp_f<0xB1>(v));
-  v = fmaxf(v, dpp_f<0x4E>(v));
-  v = fmaxf(v, dpp_f<0x141>(v));
-  v = fmaxf(v, dpp_f<0x140>(v));
-  return fmaxf(fmaxf(readlane_f(v, 0), readlane_f(v, 16)),
-               fmaxf(readlane_f(v, 32), readlane_f(v, 48)));
+// the larger, as one instruction (no NaN among them)
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
 }
+template <int kLanes>
+__device__ __forceinline__ float lanes_max(float v) {
+  v = larger(v, dpp_f<0xB1>(v));
+  v = larger(v, dpp_f<0x4E>(v));
+  v = larger(v, dpp_f<0x141>(v));
+  v = larger(v, dpp_f<0x140>(v));
+  if (kLanes == 16) return v;
+  return larger(larger(readlane_f(v, 0), readlane_f(v, 16)),
+                larger(readlane_f(v, 32), readlane_f(v, 48)));
+}
+template <int kLanes>
+__device__ __forceinline__ int lanes_max(int v) {
+  return kLanes == 16 ? row_max(v) : wave_max(v);
+}
+__device__ __forceinline__ float wave_sum_f(float v) { return lanes_sum<kWave>(v); }
+
+// exp by the hardware's exp2: a relative error of (|x| + 2) 2^-24 at most
+__device__ __forceinline__ float fast_exp(float x) {
+  return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
+}
+// 1 / x to 1 ulp, for x of ordinary size
+__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
 // 1 / (1 + exp(-z)), without overflow for any z
 __device__ __forceinline__ float sigmoid(float z) {
-  const float e = expf(-fabsf(z));
-  return (z >= 0.f ? 1.f : e) / (1.f + e);
+  const float e = fast_exp(-fabsf(z));
+  return (z >= 0.f ? 1.f : e) * fast_rcp(1.f + e);
+}
+// the same over exp(c), c <= 0: of weight where sigmoid(z) itself vanishes
+__device__ __forceinline__ float sigmoid_over(float z, float c) {
+  return fast_exp(fminf(z, 0.f) - c) * fast_rcp(1.f + fast_exp(-fabsf(z)));
 }
 
 }  // namespace uep

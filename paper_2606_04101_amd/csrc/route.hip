@@ -1,12 +1,12 @@
 // The router of an MoE layer: top-k ids and gates from the logits, the
 // statistics of its balance loss, the loss, and the logits' gradient.
 //
-// One wave takes one token.  Its E logits lie across the lanes in id order:
-// with groups, 2^n lanes share a group and each holds VPL neighbouring experts
-// of it; without, all 64 lanes share the one group.  So a group's sum of two
-// largest keys is a merge over neighbouring lanes, a tie goes to the lowest
-// lane and there to the lowest element, and nothing is sorted: k times the
-// largest key of the wave is found and taken out.
+// A row of 16 lanes, or a whole wave, takes one token.  Its E logits lie across
+// the lanes in id order: with groups, 2^n lanes share a group and each holds kVpl
+// neighbouring experts of it; without, all lanes share the one group.  So a
+// group's sum of two largest keys is a merge over neighbouring lanes.  Where a
+// group does not fill its lanes, the ends of them are holes: an expert's place
+// among lanes and holes is its slot, of the same order as the ids.
 #include "operators.hpp"
 
 namespace uep {
@@ -16,19 +16,6 @@ constexpr int kRtWaves = kRtThreads / kWave;
 constexpr int kRtMaxE = 1024;
 constexpr float kInf = __builtin_inff();
 
-// where a lane's experts lie
-struct RouteLanes {
-  int32_t lanes;  // lanes of a group, a power of two
-  int32_t vpl;    // experts of a lane
-};
-
-static RouteLanes route_lanes(int32_t E, int32_t n_group) {
-  int lanes = kWave;
-  while (lanes * n_group > kWave) lanes /= 2;
-  const int gsz = E / n_group;
-  return {lanes, (gsz + lanes - 1) / lanes};
-}
-
 struct RouteArgs {
   const void *logits;
   int64_t T, ld;
@@ -36,10 +23,16 @@ struct RouteArgs {
   const uint8_t *mask;
   int32_t *topk;
   float *gate;
-  int32_t E, k, sigmoid, renorm, n_group, top_group, lanes;
+  int32_t E, k, sigmoid, renorm, n_group, top_group;
+  int32_t group_lanes;  // lanes of a group, a power of two
+  int32_t wide;         // all lanes that have experts have kVpl, in aligned 16 bytes
+  int32_t wide_bias;    // and so with the bias
+  // the top_group groups spread over all lanes: lanes of one, a power of two, and slots
+  // of such a lane, a multiple of 4; 0 slots: they stay where they are
+  int32_t pick_lanes, pick;
   float scale;
   int64_t seq, chunk, n_chunk;
-  int32_t *counts;   // outputs, or the workspace's partials if n_chunk > 1
+  int32_t *counts;  // outputs, or the workspace's partials if n_chunk > 1
   float *prob_sum;
   int32_t *tokens;
   int32_t *status;
@@ -51,6 +44,32 @@ __device__ __forceinline__ float load_logit(const void *row, int e) {
   return static_cast<const float *>(row)[e];
 }
 
+// A lane's logits, -inf past the n it has.
+template <int kVpl, bool kBf16>
+__device__ __forceinline__ void load_logits(const void *row, int base, int n, bool wide,
+                                            float (&z)[kVpl]) {
+  constexpr int kVec = kBf16 ? 8 : 4;  // elements of 16 bytes
+  if constexpr (kVpl % kVec == 0) {
+    if (wide) {
+      const v4u *p = reinterpret_cast<const v4u *>(static_cast<const char *>(row) +
+                                                   static_cast<int64_t>(base) * (kBf16 ? 2 : 4));
+      v4u v[kVpl / kVec];
+#pragma unroll
+      for (int c = 0; c < kVpl / kVec; ++c) v[c] = n > 0 ? p[c] : v4u{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) {
+        const uint32_t w = v[i / kVec][kBf16 ? i % kVec / 2 : i % kVec];
+        z[i] = n <= 0 ? -kInf : !kBf16 ? __uint_as_float(w) : i % 2 ? bf16_at_high(w) : bf16_at_low(w);
+      }
+      return;
+    }
+  }
+  // (not 2 * kVpl scalar registers of comparisons held throughout a loop)
+  asm volatile("" : "+v"(n));
+#pragma unroll
+  for (int i = 0; i < kVpl; ++i) z[i] = i < n ? load_logit<kBf16>(row, base + i) : -kInf;
+}
+
 // fp32 as an integer of the same order (-0 as +0)
 __device__ __forceinline__ int order_of(float v) {
   const int i = __float_as_int(v + 0.f);
@@ -59,20 +78,153 @@ __device__ __forceinline__ int order_of(float v) {
 
 // the two largest of two pairs
 __device__ __forceinline__ void merge_two(float &a1, float &a2, float b1, float b2) {
-  a2 = fmaxf(fminf(a1, b1), fmaxf(a2, b2));
-  a1 = fmaxf(a1, b1);
+  a2 = larger(__builtin_amdgcn_fmed3f(a1, b1, -kInf), larger(a2, b2));
+  a1 = larger(a1, b1);
 }
 
-template <int kVpl, bool kBf16, bool kStats>
-__global__ void __launch_bounds__(kRtThreads) k_route(RouteArgs a) {
-  __shared__ float s_prob[kStats ? kRtWaves * kRtMaxE : 1];
-  __shared__ int s_count[kStats ? kRtMaxE : 1];
+// the lanes of this lane's token among those of a ballot, its first one at bit 0
+template <int kLanes>
+__device__ __forceinline__ uint64_t mine(uint64_t bits) {
+  if (kLanes == kWave) return bits;
+  return bits >> (lane_id() & ~(kLanes - 1)) & ((uint64_t(1) << (kLanes % kWave)) - 1);
+}
+
+// LDS writes of a wave's lanes before this are seen by its reads after it
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The k largest keys by taking out the largest k times: a tie goes to the lowest
+// lane and there to the lowest element, which is the lower id.  slots[j]: the j-th.
+template <int kLanes, int kVpl>
+__device__ void select_by_rounds(float (&key)[kVpl], int k, int *slots) {
+  const int l = lane_id() % kLanes;
+  for (int j = 0; j < k; ++j) {
+    float m = key[0];
+#pragma unroll
+    for (int i = 1; i < kVpl; ++i) m = larger(m, key[i]);
+    const float best = lanes_max<kLanes>(m);
+    const bool can = m == best && best > -kInf;
+    const uint64_t who = ballot(can);
+    if (!who) break;
+    const bool own = can && l == __builtin_ctzll(mine<kLanes>(who) | uint64_t(1) << 63);
+    const float wanted = own ? best : __builtin_nanf("");
+    int at = -1;
+#pragma unroll
+    for (int i = kVpl - 1; i >= 0; --i) at = key[i] == wanted ? i : at;
+#pragma unroll
+    for (int i = 0; i < kVpl; ++i) key[i] = at == i ? -kInf : key[i];
+    if (own) slots[j] = l * kVpl + at;
+  }
+}
+
+// The same for a token in 16 lanes, k <= 16, where few keys are likely to be among the
+// k largest: a key below the k-th largest of the lanes' largest keys is not.  What is left
+// (of 256 random keys 11, k = 8) goes to LDS, and each finds its place by counting those
+// ahead of it.  False (in the whole wave) where more than 32 are left.
+//   key   this lane's n keys, of slots from, from + 1 ..
+//   row   the token's keys in LDS by slot;  left: 32 pairs of words in LDS
+constexpr int kMostLeft = 32;
+template <int kVpl>
+__device__ bool select_by_rank(const float (&key)[kVpl], int n, int from, int k, const float *row,
+                               int64_t *left, int *slots) {
+  const int l = lane_id() % 16;
+  float m = -kInf;
+#pragma unroll
+  for (int c = 0; c < kVpl; c += 4)
+    if (c < n) {
+#pragma unroll
+      for (int i = c; i < c + 4; ++i) m = larger(m, key[i]);
+    }
+  int above = 0;  // lanes whose largest is larger
+#define UEP_TURN(i) above += dpp_f<0x120 + i>(m) > m;  // row_ror
+  UEP_TURN(1) UEP_TURN(2) UEP_TURN(3) UEP_TURN(4) UEP_TURN(5) UEP_TURN(6) UEP_TURN(7) UEP_TURN(8)
+  UEP_TURN(9) UEP_TURN(10) UEP_TURN(11) UEP_TURN(12) UEP_TURN(13) UEP_TURN(14) UEP_TURN(15)
+#undef UEP_TURN
+  // (at least the type's lowest value, so that no -inf is left)
+  const float least = larger(-lanes_max<16>(above < k ? -m : -kInf), -__FLT_MAX__);
+  uint32_t mask = 0;  // of the keys that are left
+#pragma unroll
+  for (int c = 0; c < kVpl; c += 4)
+    if (c < n) {
+#pragma unroll
+      for (int i = c; i < c + 4; ++i) mask |= key[i] >= least ? 1u << i : 0u;
+    }
+  const int some = __popc(mask);
+  int at = some;  // inclusive sum over the row
+  at += __builtin_amdgcn_update_dpp(0, at, 0x111, 0xF, 0xF, false);
+  at += __builtin_amdgcn_update_dpp(0, at, 0x112, 0xF, 0xF, false);
+  at += __builtin_amdgcn_update_dpp(0, at, 0x114, 0xF, 0xF, false);
+  at += __builtin_amdgcn_update_dpp(0, at, 0x118, 0xF, 0xF, false);
+  const int total = lanes_max<16>(at), most = wave_max(total);
+  if (most > kMostLeft) return false;
+  int *left_slot = reinterpret_cast<int *>(left) + 2 * (at - some);
+  while (ballot(mask != 0)) {
+    if (mask) {
+      *left_slot = from + __builtin_ctz(mask);
+      left_slot += 2;
+      mask &= mask - 1;
+    }
+  }
+  wave_sync();
+  // (key, lower slot first) as one number
+  int64_t v[2] = {INT64_MIN, INT64_MIN};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (u * 16 < most) {
+      if (u * 16 + l < total) {
+        const int slot = reinterpret_cast<int *>(left)[2 * (u * 16 + l)];
+        v[u] = static_cast<int64_t>(order_of(row[slot])) << 32 | static_cast<uint32_t>(~slot);
+      }
+      wave_sync();
+      left[u * 16 + l] = v[u];
+    }
+  wave_sync();
+  int place[2] = {0, 0};
+#pragma unroll 8
+  for (int j = 0; j < most; ++j) place[0] += left[j] > v[0];
+  if (v[0] != INT64_MIN && place[0] < k) slots[place[0]] = static_cast<int>(~static_cast<uint32_t>(v[0]));
+  if (most > 16) {
+#pragma unroll 8
+    for (int j = 0; j < most; ++j) place[1] += left[j] > v[1];
+    if (v[1] != INT64_MIN && place[1] < k) slots[place[1]] = static_cast<int>(~static_cast<uint32_t>(v[1]));
+  }
+  return true;
+}
+
+// a lane's values into its part of a row in LDS
+template <int kVpl>
+__device__ __forceinline__ void put_lane(float *row, int l, const float (&v)[kVpl]) {
+  if constexpr (kVpl % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < kVpl; i += 4)
+      *reinterpret_cast<v4f *>(row + l * kVpl + i) = v4f{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVpl; ++i) row[l * kVpl + i] = v[i];
+  }
+}
+
+template <int kLanes, int kVpl, bool kBf16, bool kStats>
+__global__ void __launch_bounds__(kRtThreads, kLanes == 16 && kVpl == 16 && !kStats ? 3 : 1)
+k_route(RouteArgs a) {
+  constexpr int kTok = kWave / kLanes;  // tokens of a wave
+  constexpr int kParts = kRtWaves * kTok;
+  constexpr int kSlots = kLanes * kVpl;
+  // a token's logits, and its keys, by slot; at the end the parts' sums of the scores
+  __shared__ __align__(16) float s_row[kParts * kSlots];
+  __shared__ __align__(16) float s_key[kLanes == 16 ? kParts * kSlots : 1];
+  __shared__ int64_t s_left[kLanes == 16 ? kParts * kMostLeft : 1];
+  __shared__ int s_slots[kRtWaves][kWave];
+  __shared__ int s_count[kStats ? kSlots : 1];
   __shared__ int s_tokens;
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int wave = threadIdx.x / kWave, l = lane_id() % kLanes, part = threadIdx.x / kLanes;
   const int gsz = a.E / a.n_group;
-  const int group = lane / a.lanes, sub = lane - group * a.lanes;
+  const int group = l / a.group_lanes, sub = l - group * a.group_lanes;
   const int base = group * gsz + sub * kVpl;
   const int n_mine = group < a.n_group ? min(max(gsz - sub * kVpl, 0), kVpl) : 0;
+  const int hole = a.group_lanes * kVpl - gsz;  // slots of a group without expert
   const bool by_score = a.sigmoid && (a.bias || a.n_group > 1);
 
   if (kStats) {
@@ -80,147 +232,175 @@ __global__ void __launch_bounds__(kRtThreads) k_route(RouteArgs a) {
     if (threadIdx.x == 0) s_tokens = 0;
     __syncthreads();
   }
-  float bias[kVpl];
+  float bias[kVpl] = {};
+  if (a.bias) {
+    load_logits<kVpl, false>(a.bias, base, n_mine, a.wide_bias, bias);
 #pragma unroll
-  for (int i = 0; i < kVpl; ++i) bias[i] = a.bias && i < n_mine ? a.bias[base + i] : 0.f;
+    for (int i = 0; i < kVpl; ++i) bias[i] = i < n_mine ? bias[i] : 0.f;
+  }
   float acc[kVpl] = {};
   int n_tokens = 0;
+  float *z_row = s_row + part * kSlots;
+  float *key_row = kLanes == 16 ? s_key + part * kSlots : nullptr;
 
   const int64_t seg = blockIdx.x / a.n_chunk;
   const int64_t t0 = seg * a.seq + (blockIdx.x - seg * a.n_chunk) * a.chunk;
   const int64_t t1 = min(min(t0 + a.chunk, (seg + 1) * a.seq), a.T);
-  for (int64_t t = t0 + wave; t < t1; t += kRtWaves) {
-    const char *row = static_cast<const char *>(a.logits) + t * a.ld * (kBf16 ? 2 : 4);
+  // (all of a wave's tokens are taken together, so every lane goes through all of this)
+  for (int64_t tw = t0 + wave * kTok; tw < t1; tw += kParts) {
+    const int64_t t = tw + (kTok > 1 ? lane_id() / kLanes : 0);
+    const bool here = t < t1;
+    const char *row = static_cast<const char *>(a.logits) + (here ? t : tw) * a.ld * (kBf16 ? 2 : 4);
     float z[kVpl];
-    bool bad = false;
-    float top = -kInf;
+    load_logits<kVpl, kBf16>(row, base, n_mine, a.wide, z);
+    bool on = here && (!a.mask || a.mask[t] != 0);
+    float top = -kInf, sum_z = 0.f;  // the sum is a NaN if a logit is (and cannot overflow)
 #pragma unroll
     for (int i = 0; i < kVpl; ++i) {
-      z[i] = i < n_mine ? load_logit<kBf16>(row, base + i) : -kInf;
-      bad |= !(z[i] < kInf);
-      top = fmaxf(top, z[i]);
+      top = larger(top, z[i]);
+      sum_z = fmaf(z[i], 0x1p-12f, sum_z);
     }
-    top = wave_max_f(top);
-    bool on = !a.mask || a.mask[t] != 0;
-    if (on && ballot(bad)) {
-      if (lane == 0) report(a.status, ULTRAEP_EDATA);
+    if (mine<kLanes>(ballot(!(sum_z < kInf))) && on) {
+      if (l == 0) report(a.status, ULTRAEP_EDATA);
       on = false;
     }
+    top = lanes_max<kLanes>(top);
     on = on && top > -kInf;
-    if (!on) {
-      if (lane < a.k) {
-        a.topk[t * a.k + lane] = -1;
-        a.gate[t * a.k + lane] = 0.f;
+    if (!ballot(on)) {
+      if (here && l < a.k) {
+        a.topk[t * a.k + l] = -1;
+        a.gate[t * a.k + l] = 0.f;
       }
       continue;
     }
+    put_lane<kVpl>(z_row, l, z);
 
-    int key[kVpl];
-    {
-      float f[kVpl];
+    float s[kVpl];  // scores (sigmoid)
+    if (a.sigmoid && (by_score || kStats)) {
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) f[i] = (by_score ? sigmoid(z[i]) : z[i]) + bias[i];
-      bool keep = true;
-      if (a.n_group > 1) {
-        float m1 = -kInf, m2 = -kInf;
+      for (int i = 0; i < kVpl; ++i) s[i] = sigmoid(z[i]);
+    }
+    float key[kVpl];  // -inf: not to be chosen
 #pragma unroll
-        for (int i = 0; i < kVpl; ++i) merge_two(m1, m2, z[i] > -kInf ? f[i] : -kInf, -kInf);
-        for (int d = 1; d < a.lanes; d *= 2)
-          merge_two(m1, m2, __shfl_xor(m1, d), __shfl_xor(m2, d));
-        const float score = m1 + m2;
-        int before = 0;  // groups ahead of this lane's
-        for (int g = 0; g < a.n_group; ++g) {
-          const float o = readlane_f(score, g * a.lanes);
-          before += o > score || (o == score && g < group);
-        }
-        keep = before < a.top_group;
+    for (int i = 0; i < kVpl; ++i) key[i] = (by_score && z[i] > -kInf ? s[i] : z[i]) + bias[i];
+    if (kLanes == 16) put_lane<kVpl>(key_row, l, key);
+    bool keep = on;
+    if (a.n_group > 1) {
+      float m1 = -kInf, m2 = -kInf;
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) {
+        m2 = __builtin_amdgcn_fmed3f(m1, m2, key[i]);
+        m1 = larger(m1, key[i]);
       }
-#pragma unroll
-      for (int i = 0; i < kVpl; ++i)
-        key[i] = keep && z[i] > -kInf ? order_of(f[i]) : INT32_MIN;
+      for (int d = 1; d < a.group_lanes; d *= 2)
+        merge_two(m1, m2, __shfl_xor(m1, d), __shfl_xor(m2, d));
+      const float score = m1 + m2;
+      int before = 0;  // groups ahead of this lane's
+      for (int g = 0; g < a.n_group; ++g) {
+        const float o = kLanes == kWave ? readlane_f(score, g * a.group_lanes)
+                                        : __shfl(score, g * a.group_lanes, kLanes);
+        before += o > score || (o == score && g < group);
+      }
+      keep = keep && group < a.n_group && before < a.top_group;
     }
 
-    // lane j ends up with the j-th id and its logit
-    int my_id = -1;
-    float my_z = -kInf;
-    for (int j = 0; j < a.k; ++j) {
-      int m = key[0];
+    int *slots = &s_slots[wave][lane_id() - l];
+    slots[l] = -1;
+    bool done = false;
+    if constexpr (kLanes == 16) {
+      float some[kVpl];
+      if (a.pick > 0) {  // the groups that are left, over all lanes: pick keys a lane
+        uint32_t left = static_cast<uint32_t>(mine<16>(ballot(keep && sub == 0)));
+        const int nth = l / a.pick_lanes;
+        for (int j = 0; j < nth; ++j) left &= left - 1;
+        const int from = (left ? __builtin_ctz(left) * kVpl : 0) + (l - nth * a.pick_lanes) * a.pick;
+        const bool has = nth < a.top_group && left;
+        wave_sync();
 #pragma unroll
-      for (int i = 1; i < kVpl; ++i) m = max(m, key[i]);
-      const int best = wave_max(m);
-      if (best == INT32_MIN) break;
-      const int owner = __builtin_ctzll(ballot(m == best));
-      int at = 0;
-      float v = z[0];
+        for (int c = 0; c < kVpl; c += 4)
+          if (c < a.pick) {
+            const v4f v = *reinterpret_cast<const v4f *>(key_row + (has ? from : 0) + c);
 #pragma unroll
-      for (int i = kVpl - 1; i >= 0; --i)
-        if (key[i] == best) {
-          at = i;
-          v = z[i];
-        }
-      const int id = readlane(base + at, owner);
-      v = readlane_f(v, owner);
-      if (lane == j) {
-        my_id = id;
-        my_z = v;
-      }
-      if (lane == owner) {
+            for (int i = 0; i < 4; ++i) some[c + i] = has ? v[i] : -kInf;
+          }
+        done = select_by_rank<kVpl>(some, a.pick, from, a.k, key_row, s_left + part * kMostLeft, slots);
+      } else {
 #pragma unroll
-        for (int i = 0; i < kVpl; ++i)
-          if (i == at) key[i] = INT32_MIN;
+        for (int i = 0; i < kVpl; ++i) some[i] = keep ? key[i] : -kInf;
+        done = select_by_rank<kVpl>(some, kVpl, l * kVpl, a.k, key_row, s_left + part * kMostLeft, slots);
       }
     }
-
+    if (!done) {
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) key[i] = keep ? key[i] : -kInf;
+      select_by_rounds<kLanes, kVpl>(key, a.k, slots);
+    }
+    wave_sync();
+    const int slot = l < a.k ? slots[l] : -1;
     // ids fill from the front: without a first one (every best group held only
     // -inf and lone experts) the token has none
-    on = readlane(my_id, 0) >= 0;
+    on = on && slots[0] >= 0;
+    const float my_z = slot >= 0 ? z_row[slot] : -kInf;
+    int my_id = slot;
+    if (hole > 0 && slot >= 0) my_id -= slot / (a.group_lanes * kVpl) * hole;
 
     // scores over all experts: u = s / exp(c), c so that no u of weight vanishes
     float g = 0.f;
     if (a.sigmoid) {
       if (a.renorm) {
-        const float c = wave_max_f(my_id >= 0 ? fminf(my_z, 0.f) : -kInf);
-        const float u = my_id >= 0 ? expf(fminf(my_z, 0.f) - c) / (1.f + expf(-fabsf(my_z))) : 0.f;
-        g = u / wave_sum_f(u);
+        const float c = lanes_max<kLanes>(slot >= 0 ? fminf(my_z, 0.f) : -kInf);
+        const float u = slot >= 0 ? sigmoid_over(my_z, c) : 0.f;
+        g = u * fast_rcp(lanes_sum<kLanes>(u));
       } else {
-        g = my_id >= 0 ? sigmoid(my_z) : 0.f;
+        g = slot >= 0 ? sigmoid(my_z) : 0.f;
       }
     } else if (a.renorm) {
-      const float c = wave_max_f(my_z);
-      const float u = my_id >= 0 ? expf(my_z - c) : 0.f;
-      g = u / wave_sum_f(u);
+      const float c = lanes_max<kLanes>(my_z);
+      const float u = slot >= 0 ? fast_exp(my_z - c) : 0.f;
+      g = u * fast_rcp(lanes_sum<kLanes>(u));
     }
-    if (on && (kStats || (!a.sigmoid && !a.renorm))) {
-      const float c = a.sigmoid ? fminf(top, 0.f) : top;
-      float u[kVpl], sum = 0.f;
+    if (kStats || (!a.sigmoid && !a.renorm)) {
+      float u[kVpl], sum = 0.f, c = 0.f;
+      if (!a.sigmoid) {
+        c = on ? top : 0.f;
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) {
-        u[i] = a.sigmoid ? expf(fminf(z[i], 0.f) - c) / (1.f + expf(-fabsf(z[i]))) : expf(z[i] - c);
-        sum += u[i];
+        for (int i = 0; i < kVpl; ++i) u[i] = fast_exp(z[i] - c);
+      } else if (ballot(on && top < -60.f)) {
+        c = on ? fminf(top, 0.f) : 0.f;
+#pragma unroll
+        for (int i = 0; i < kVpl; ++i) u[i] = sigmoid_over(z[i], c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVpl; ++i) u[i] = s[i];
       }
-      const float inv = 1.f / wave_sum_f(sum);
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) acc[i] += u[i] * inv;
-      if (!a.sigmoid && !a.renorm) g = my_id >= 0 ? expf(my_z - c) * inv : 0.f;
-      ++n_tokens;
+      for (int i = 0; i < kVpl; ++i) sum += u[i];
+      sum = lanes_sum<kLanes>(sum);
+      const float inv = on ? fast_rcp(sum) : 0.f;
+      if (kStats) {
+#pragma unroll
+        for (int i = 0; i < kVpl; ++i) acc[i] += on ? u[i] * inv : 0.f;
+        n_tokens += on;
+      }
+      if (!a.sigmoid && !a.renorm) g = slot >= 0 ? fast_exp(my_z - c) * inv : 0.f;
     }
-    if (lane < a.k) {
-      a.topk[t * a.k + lane] = my_id;
-      a.gate[t * a.k + lane] = my_id >= 0 ? g * a.scale : 0.f;
-      if (kStats && my_id >= 0) atomicAdd(&s_count[my_id], 1);
+    if (here && l < a.k) {
+      a.topk[t * a.k + l] = my_id;
+      a.gate[t * a.k + l] = slot >= 0 ? g * a.scale : 0.f;
+      if (kStats && slot >= 0) atomicAdd(&s_count[my_id], 1);
     }
+    wave_sync();
   }
 
   if (kStats) {
-#pragma unroll
-    for (int i = 0; i < kVpl; ++i)
-      if (i < n_mine) s_prob[wave * kRtMaxE + base + i] = acc[i];
-    if (lane == 0) atomicAdd(&s_tokens, n_tokens);
+    put_lane<kVpl>(z_row, l, acc);
+    if (l == 0 && n_tokens) atomicAdd(&s_tokens, n_tokens);
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += kRtThreads) {
+      const int slot = e + (hole > 0 ? e / gsz * hole : 0);
       float p = 0.f;
 #pragma unroll
-      for (int w = 0; w < kRtWaves; ++w) p += s_prob[w * kRtMaxE + e];
+      for (int w = 0; w < kParts; ++w) p += s_row[w * kSlots + slot];
       a.prob_sum[static_cast<int64_t>(blockIdx.x) * a.E + e] = p;
       a.counts[static_cast<int64_t>(blockIdx.x) * a.E + e] = s_count[e];
     }
@@ -228,39 +408,52 @@ __global__ void __launch_bounds__(kRtThreads) k_route(RouteArgs a) {
   }
 }
 
-// A sequence's partials, 16 experts a workgroup: 64 threads an expert take the chunks in
-// turn, then the 64 sums are added in order of the thread.  The first workgroup of a
-// sequence also sums its tokens.
-constexpr int kRsThreads = 1024, kRsExperts = 16, kRsTurns = kRsThreads / kRsExperts;
+// A sequence's partials, 8 experts a workgroup: 128 threads an expert take the chunks in
+// turn, and their sums are added over lanes 8 apart, then over waves in order.  The
+// first workgroup of a sequence also sums its tokens.
+constexpr int kRsThreads = 1024, kRsExperts = 8, kRsTurns = kRsThreads / kRsExperts;
 __global__ void __launch_bounds__(kRsThreads)
 k_route_sum(const int32_t *__restrict__ part_c, const float *__restrict__ part_p,
             const int32_t *__restrict__ part_n, int64_t n_chunk, int32_t E, int32_t n_eb,
             int32_t *__restrict__ counts, float *__restrict__ prob_sum,
             int32_t *__restrict__ tokens) {
-  __shared__ float s_p[kRsTurns][kRsExperts];
-  __shared__ int s_c[kRsTurns][kRsExperts];
+  constexpr int kWaves = kRsThreads / kWave;
+  __shared__ float s_p[kWaves][kRsExperts];
+  __shared__ int s_c[kWaves][kRsExperts];
   const int64_t seg = blockIdx.x / n_eb;
   const int eb = static_cast<int>(blockIdx.x - seg * n_eb);
   const int i = threadIdx.x % kRsExperts, turn = threadIdx.x / kRsExperts;
-  const int e = eb * kRsExperts + i;
+  const int e = min(eb * kRsExperts + i, E - 1);
   float p = 0.f;
   int c = 0;
-  if (e < E)
-    for (int64_t j = turn; j < n_chunk; j += kRsTurns) {
-      p += part_p[(seg * n_chunk + j) * E + e];
-      c += part_c[(seg * n_chunk + j) * E + e];
-    }
-  s_p[turn][i] = p;
-  s_c[turn][i] = c;
-  if (eb == 0 && threadIdx.x >= kRsThreads - kWave) {  // the last wave
+#pragma unroll 8
+  for (int64_t j = turn; j < n_chunk; j += kRsTurns) {
+    p += part_p[(seg * n_chunk + j) * E + e];
+    c += part_c[(seg * n_chunk + j) * E + e];
+  }
+#pragma unroll
+  for (int d = kRsExperts; d < kWave; d *= 2) {
+    p += __shfl_xor(p, d);
+    c += __shfl_xor(c, d);
+  }
+  const int wave = threadIdx.x / kWave;
+  if (lane_id() < kRsExperts) {
+    s_p[wave][i] = p;
+    s_c[wave][i] = c;
+  }
+  if (eb == 0 && wave == kWaves - 1) {
     int n = 0;
+#pragma unroll 8
     for (int64_t j = lane_id(); j < n_chunk; j += kWave) n += part_n[seg * n_chunk + j];
     n = wave_sum(n);
     if (lane_id() == 0) tokens[seg] = n;
   }
   __syncthreads();
-  if (turn == 0 && e < E) {
-    for (int w = 1; w < kRsTurns; ++w) {
+  if (turn == 0 && eb * kRsExperts + i < E) {
+    p = s_p[0][i];
+    c = s_c[0][i];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
       p += s_p[w][i];
       c += s_c[w][i];
     }
@@ -307,108 +500,135 @@ struct RouteGradArgs {
   const int32_t *topk;
   const float *dgate, *coef, *dloss;
   int32_t E, k, sigmoid, renorm;
+  int32_t wide, wide_coef;  // lanes have kVpl experts or none, in aligned 16 bytes
   float scale;
   int32_t *status;
 };
 
-// One wave a token, lane l holds experts l * VPL ..  With w the balance loss's
+// Lane l of a token's 16 or 64 holds experts l * kVpl ..  With w the balance loss's
 // gradient by p and d the gates' by the chosen scores' logits:
 //   softmax  dz = p (w - <w, p>) + d,  sigmoid  dz = p (1 - s) (w - <w, p>) + d
 // and without renorm a softmax gate is a p of its own, so scale * dgate joins w.
-template <int kVpl, bool kBf16>
+template <int kLanes, int kVpl, bool kBf16>
 __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
-  const int lane = lane_id();
-  const int base = lane * kVpl;
+  constexpr int kTok = kWave / kLanes, kParts = kRtWaves * kTok, kSlots = kLanes * kVpl;
+  __shared__ __align__(16) float s_d[kParts * kSlots];  // a token's d, by expert
+  const int wave = threadIdx.x / kWave, l = lane_id() % kLanes, part = threadIdx.x / kLanes;
+  const int base = l * kVpl;
   const int n_mine = min(max(a.E - base, 0), kVpl);
   const float dloss = a.dloss ? *a.dloss : 1.f;
-  const int64_t nw = static_cast<int64_t>(gridDim.x) * kRtWaves;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRtWaves + threadIdx.x / kWave; t < a.T;
-       t += nw) {
-    const char *row = static_cast<const char *>(a.logits) + t * a.ld * (kBf16 ? 2 : 4);
-    char *out = static_cast<char *>(a.dlogits) + t * a.ld * (kBf16 ? 2 : 4);
-    float z[kVpl];
-    bool bad = false;
-    float top = -kInf;
-#pragma unroll
-    for (int i = 0; i < kVpl; ++i) {
-      z[i] = i < n_mine ? load_logit<kBf16>(row, base + i) : -kInf;
-      bad |= !(z[i] < kInf);
-      top = fmaxf(top, z[i]);
+  float *d_row = s_d + part * kSlots;
+  for (int64_t tw = static_cast<int64_t>(blockIdx.x) * kParts + wave * kTok; tw < a.T;
+       tw += static_cast<int64_t>(gridDim.x) * kParts) {
+    const int64_t t = tw + (kTok > 1 ? lane_id() / kLanes : 0);
+    const bool here = t < a.T;
+    const int64_t at = (here ? t : tw) * a.ld * (kBf16 ? 2 : 4);
+    const char *row = static_cast<const char *>(a.logits) + at;
+    char *out = static_cast<char *>(a.dlogits) + at;
+    float z[kVpl], w[kVpl] = {};
+    load_logits<kVpl, kBf16>(row, base, n_mine, a.wide, z);
+    if (a.coef) {
+      const float *coef = a.coef + (here ? t : tw) / a.seq * a.E;
+      load_logits<kVpl, false>(coef, base, n_mine, a.wide_coef, w);
     }
-    top = wave_max_f(top);
-    bool on = !a.mask || a.mask[t] != 0;
+    bool on = here && (!a.mask || a.mask[t] != 0);
     int id = -1;
-    float dg = 0.f;
-    if (lane < a.k) {
-      id = a.topk[t * a.k + lane];
+    float dg = 0.f, my_z = -kInf;
+    if (here && l < a.k) {
+      id = a.topk[t * a.k + l];
       if (id < -1 || id >= a.E) {
         report(a.status, ULTRAEP_EDATA);
         id = -1;
       }
-      if (id >= 0 && a.dgate) dg = a.dgate[t * a.k + lane] * a.scale;
+      if (id >= 0) {
+        my_z = load_logit<kBf16>(row, id);
+        if (a.dgate) dg = a.dgate[t * a.k + l] * a.scale;
+      }
     }
-    if (on && ballot(bad)) {
-      if (lane == 0) report(a.status, ULTRAEP_EDATA);
+    float top = -kInf, sum_z = 0.f;  // the sum is a NaN if a logit is (and cannot overflow)
+#pragma unroll
+    for (int i = 0; i < kVpl; ++i) {
+      top = larger(top, z[i]);
+      sum_z = fmaf(z[i], 0x1p-12f, sum_z);
+      w[i] = i < n_mine ? w[i] * dloss : 0.f;
+    }
+    if (mine<kLanes>(ballot(!(sum_z < kInf))) && on) {
+      if (l == 0) report(a.status, ULTRAEP_EDATA);
       on = false;
     }
-    on = on && top > -kInf && readlane(id, 0) >= 0;
-    float dz[kVpl] = {};
-    if (on) {
-      const float c = a.sigmoid ? fminf(top, 0.f) : top;
-      float p[kVpl], w[kVpl], sum = 0.f;
+    top = lanes_max<kLanes>(top);
+    on = on && top > -kInf && (mine<kLanes>(ballot(id >= 0)) & 1);
+
+    // the chosen: this lane's is lane l's
+    const bool chosen = on && my_z > -kInf;
+    const float not_s = a.sigmoid ? 1.f - sigmoid(my_z) : 1.f;
+    float d;
+    if (a.renorm) {
+      const float c = lanes_max<kLanes>(chosen ? (a.sigmoid ? fminf(my_z, 0.f) : my_z) : -kInf);
+      const float u = !chosen ? 0.f : a.sigmoid ? sigmoid_over(my_z, c) : fast_exp(my_z - c);
+      const float us = lanes_sum<kLanes>(u);
+      const float q = us > 0.f ? u * fast_rcp(us) : 0.f;
+      d = q * (dg - lanes_sum<kLanes>(dg * q)) * not_s;
+    } else {
+      d = a.sigmoid ? sigmoid(my_z) * not_s * dg : dg;
+    }
+    const float zero[kVpl] = {};
+    put_lane<kVpl>(d_row, l, zero);
+    wave_sync();
+    if (chosen) atomicAdd(d_row + id, d);
+    wave_sync();
+    const bool joins_w = !a.sigmoid && !a.renorm;
+
+    const float c = !on ? 0.f : a.sigmoid ? fminf(top, 0.f) : top;
+    const bool low = ballot(on && a.sigmoid && top < -60.f);
+    float p[kVpl], s[kVpl], sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) {
-        p[i] = a.sigmoid ? expf(fminf(z[i], 0.f) - c) / (1.f + expf(-fabsf(z[i]))) : expf(z[i] - c);
-        sum += p[i];
+    for (int i = 0; i < kVpl; ++i) {
+      if (a.sigmoid) {
+        s[i] = sigmoid(z[i]);
+        p[i] = low ? sigmoid_over(z[i], c) : s[i];
+      } else {
+        p[i] = fast_exp(z[i] - c);
       }
-      const float inv = 1.f / wave_sum_f(sum);
-      const int64_t at = t / a.seq * a.E;
+      sum += p[i];
+    }
+    const float inv = fast_rcp(lanes_sum<kLanes>(sum));
+    float dd[kVpl], dot = 0.f;
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) {
-        p[i] *= inv;
-        w[i] = a.coef && i < n_mine ? dloss * a.coef[at + base + i] : 0.f;
+    for (int i = 0; i < kVpl; ++i) {
+      dd[i] = d_row[base + i];
+      if (joins_w) {
+        w[i] += dd[i];
+        dd[i] = 0.f;
       }
-      float d = dg;  // what joins the chosen expert's w or dz
-      float my_z = id >= 0 ? load_logit<kBf16>(row, id) : -kInf;
-      if (my_z == -kInf) {
-        d = 0.f;
-      } else if (a.sigmoid) {
-        d *= 1.f - sigmoid(my_z);
-      }
-      if (a.renorm) {
-        const float cc = wave_max_f(a.sigmoid ? (my_z > -kInf ? fminf(my_z, 0.f) : -kInf) : my_z);
-        float u = 0.f;
-        if (my_z > -kInf)
-          u = a.sigmoid ? expf(fminf(my_z, 0.f) - cc) / (1.f + expf(-fabsf(my_z))) : expf(my_z - cc);
-        const float us = wave_sum_f(u);
-        const float q = us > 0.f ? u / us : 0.f;
-        const float mean = wave_sum_f(dg * q);
-        d = q * (dg - mean);
-        if (a.sigmoid) d *= my_z > -kInf ? 1.f - sigmoid(my_z) : 0.f;
-      } else if (a.sigmoid) {
-        d *= my_z > -kInf ? sigmoid(my_z) : 0.f;
-      }
-      const bool joins_w = !a.sigmoid && !a.renorm;
-      for (int j = 0; j < a.k; ++j) {
-        const int e = readlane(id, j);
-        const float v = readlane_f(d, j);
-        if (e < 0) continue;
+      p[i] *= inv;
+      dot += w[i] * p[i];
+    }
+    dot = lanes_sum<kLanes>(dot);
+    float dz[kVpl];
 #pragma unroll
-        for (int i = 0; i < kVpl; ++i)
-          if (base + i == e) {
-            if (joins_w) w[i] += v;
-            else dz[i] += v;
+    for (int i = 0; i < kVpl; ++i) {
+      float v = p[i] * (w[i] - dot);
+      if (a.sigmoid) v *= 1.f - s[i];
+      dz[i] = on && z[i] > -kInf ? dd[i] + v : 0.f;
+    }
+    wave_sync();
+    if (!here) continue;
+    if constexpr (kVpl % (kBf16 ? 8 : 4) == 0) {
+      if (a.wide) {
+        if (n_mine > 0) {
+          v4u *o = reinterpret_cast<v4u *>(out + base * (kBf16 ? 2 : 4));
+#pragma unroll
+          for (int i = 0; i < kVpl; i += kBf16 ? 8 : 4) {
+            if (kBf16)
+              *o++ = v4u{pack_bf16(dz[i], dz[i + 1]), pack_bf16(dz[i + 2], dz[i + 3]),
+                         pack_bf16(dz[(i + 4) % kVpl], dz[(i + 5) % kVpl]),
+                         pack_bf16(dz[(i + 6) % kVpl], dz[(i + 7) % kVpl])};
+            else
+              *o++ = __builtin_bit_cast(v4u, v4f{dz[i], dz[i + 1], dz[i + 2], dz[i + 3]});
           }
-      }
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < kVpl; ++i) dot += w[i] * p[i];
-      dot = wave_sum_f(dot);
-#pragma unroll
-      for (int i = 0; i < kVpl; ++i) {
-        float v = p[i] * (w[i] - dot);
-        if (a.sigmoid) v *= 1.f - sigmoid(z[i]);
-        dz[i] = z[i] > -kInf ? dz[i] + v : 0.f;
+        }
+        continue;
       }
     }
 #pragma unroll
@@ -425,10 +645,13 @@ RouteShape route_shape(int64_t T, const ultraep_router &r) {
   s.seq = r.seq_len > 0 ? r.seq_len : (T > 0 ? T : 1);
   if (s.seq > T && T > 0) s.seq = T;
   s.n_seg = T > 0 ? (T + s.seq - 1) / s.seq : 1;
-  // about 512 workgroups, and no partials where one workgroup has few tokens anyway
-  s.chunk = (T + 511) / 512;
-  s.chunk = s.chunk < 4 ? 4 : (s.chunk + 3) / 4 * 4;
-  if (s.seq <= 16) s.chunk = 16;
+  // Workgroups of at least 16 tokens, about as many as run at once (two a compute unit,
+  // four with few experts): more make more partials, fewer take turns.  With 1024 and 512
+  // of them, us with the sums and the loss: E = 256, T = 16384 26.3 and 20.9, 65536 53.9
+  // and 48.7; E = 128, T = 16384 17.8 and 15.1; E = 64, T = 65536 21.7 and 26.9.
+  const int64_t n_wg = r.E > 64 ? 512 : 1024;
+  s.chunk = (T + n_wg - 1) / n_wg;
+  s.chunk = s.chunk < 16 ? 16 : (s.chunk + 15) / 16 * 16;
   s.n_chunk = (s.seq + s.chunk - 1) / s.chunk;
   return s;
 }
@@ -440,13 +663,15 @@ size_t route_ws_bytes(int64_t T, const ultraep_router &r) {
 }
 
 template <bool kBf16, bool kStats>
-static void start_route(int vpl, dim3 grid, hipStream_t stream, const RouteArgs &a) {
-#define UEP_CASE(n)                                                                            \
-  if (vpl <= n) {                                                                              \
-    hipLaunchKernelGGL((k_route<n, kBf16, kStats>), grid, dim3(kRtThreads), 0, stream, a);     \
+static void start_route(int lanes, int vpl, dim3 grid, hipStream_t stream, const RouteArgs &a) {
+#define UEP_CASE(m, n)                                                                         \
+  if (lanes == m && vpl == n) {                                                                \
+    hipLaunchKernelGGL((k_route<m, n, kBf16, kStats>), grid, dim3(kRtThreads), 0, stream, a);  \
     return;                                                                                    \
   }
-  UEP_CASE(1) UEP_CASE(2) UEP_CASE(4) UEP_CASE(8) UEP_CASE(16) UEP_CASE(32)
+  UEP_CASE(16, 4) UEP_CASE(16, 8) UEP_CASE(16, 12) UEP_CASE(16, 16) UEP_CASE(16, 24)
+  UEP_CASE(16, 32)
+  UEP_CASE(64, 1) UEP_CASE(64, 2) UEP_CASE(64, 4) UEP_CASE(64, 8) UEP_CASE(64, 16) UEP_CASE(64, 32)
 #undef UEP_CASE
 }
 
@@ -455,13 +680,46 @@ hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
                         int32_t *topk, float *gate, int32_t *counts, float *prob_sum,
                         int32_t *tokens, void *ws, int32_t *status, hipStream_t stream) {
   const RouteShape s = route_shape(T, r);
-  const int n_group = r.n_group > 0 ? r.n_group : 1;
-  const RouteLanes l = route_lanes(r.E, n_group);
-  RouteArgs a{logits, T, ld, bias, mask, topk, gate, r.E, r.k, r.score == ULTRAEP_SIGMOID, r.renorm,
-              n_group, r.top_group, l.lanes, r.scale, s.seq, s.chunk, s.n_chunk, counts, prob_sum,
-              tokens, status};
+  const int n_group = r.n_group > 0 ? r.n_group : 1, gsz = r.E / n_group;
+  // experts of a lane when a token takes `lanes`, and the lanes of a group
+  int group_lanes = 0;
+  auto spread = [&](int lanes) {
+    group_lanes = lanes;
+    while (group_lanes * n_group > lanes) group_lanes /= 2;
+    return group_lanes ? (gsz + group_lanes - 1) / group_lanes : 1 << 30;
+  };
+  int lanes = 16, vpl = r.k <= 16 ? spread(16) : 1 << 30;
+  // A wave a token where 2048 of them, two a SIMD, are all there are and no statistics are
+  // wanted: us of E = 256 with groups, 16 and 64 lanes a token: T = 1 6.0 and 5.2, 2048 7.1
+  // and 6.5, 4096 7.2 and 8.2, 65536 51 and 69 (with statistics 49 and 99); E = 64: 1 3.9 and
+  // 3.5, 4096 4.5 and 5.2, 65536 13.9 and 32.  Rows of over 24 experts a lane have one wave a
+  // SIMD: E = 512, T = 65536 175 and 103 (with statistics 132 and 176).
   const bool stats = counts != nullptr;
-  const int64_t n_wg = s.n_seg * s.n_chunk;
+  if (vpl > (stats ? 32 : 24) || (!stats && T <= 2048)) {
+    lanes = kWave;
+    vpl = spread(kWave);
+  }
+  if (lanes == 16) vpl = vpl <= 16 ? (vpl + 3) / 4 * 4 : (vpl + 7) / 8 * 8;
+  else vpl = vpl <= 1 ? 1 : 1 << (32 - __builtin_clz(vpl - 1));
+  const int esize = type == ULTRAEP_BF16 ? 2 : 4;
+  const bool wide = gsz == group_lanes * vpl && vpl * esize % 16 == 0 && ld * esize % 16 == 0 &&
+                    (reinterpret_cast<uintptr_t>(logits) & 15u) == 0;
+  const bool wide_bias = gsz == group_lanes * vpl && vpl % 4 == 0 &&
+                         (reinterpret_cast<uintptr_t>(bias) & 15u) == 0;
+  int pick_lanes = 16;
+  while (n_group > 1 && pick_lanes * r.top_group > 16) pick_lanes /= 2;
+  int pick = 0;
+  if (lanes == 16 && n_group > 1 && pick_lanes > 0 && vpl * group_lanes % (4 * pick_lanes) == 0)
+    pick = vpl * group_lanes / pick_lanes;
+  RouteArgs a{logits, T, ld, bias, mask, topk, gate, r.E, r.k, r.score == ULTRAEP_SIGMOID, r.renorm,
+              n_group, r.top_group, group_lanes, wide, wide_bias, pick_lanes, pick, r.scale, s.seq, s.chunk, s.n_chunk, counts,
+              prob_sum, tokens, status};
+  if (!stats) {  // no partials to keep few
+    a.seq = T;
+    a.chunk = kRtThreads / lanes;
+    a.n_chunk = (T + a.chunk - 1) / a.chunk;
+  }
+  const int64_t n_wg = stats ? s.n_seg * s.n_chunk : a.n_chunk;
   if (stats && s.n_chunk > 1) {
     a.prob_sum = static_cast<float *>(ws);
     a.counts = reinterpret_cast<int32_t *>(a.prob_sum + n_wg * r.E);
@@ -469,11 +727,11 @@ hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
   }
   const dim3 grid(static_cast<unsigned>(n_wg));
   if (type == ULTRAEP_BF16) {
-    if (stats) start_route<true, true>(l.vpl, grid, stream, a);
-    else start_route<true, false>(l.vpl, grid, stream, a);
+    if (stats) start_route<true, true>(lanes, vpl, grid, stream, a);
+    else start_route<true, false>(lanes, vpl, grid, stream, a);
   } else {
-    if (stats) start_route<false, true>(l.vpl, grid, stream, a);
-    else start_route<false, false>(l.vpl, grid, stream, a);
+    if (stats) start_route<false, true>(lanes, vpl, grid, stream, a);
+    else start_route<false, false>(lanes, vpl, grid, stream, a);
   }
   if (stats && s.n_chunk > 1) {
     const int n_eb = (r.E + kRsExperts - 1) / kRsExperts;
@@ -504,20 +762,30 @@ hipError_t launch_route_grad(const void *logits, int32_t type, int64_t T, int64_
                              const float *dgate, const float *coef, const float *dloss,
                              void *dlogits, int32_t *status, hipStream_t stream) {
   const RouteShape s = route_shape(T, r);
+  const int lanes = r.E <= 512 && r.k <= 16 ? 16 : kWave;
+  int vpl = (r.E + lanes - 1) / lanes;
+  vpl = lanes == 16 ? (vpl <= 16 ? (vpl + 3) / 4 * 4 : (vpl + 7) / 8 * 8) : vpl <= 8 ? 8 : 16;
+  const int esize = type == ULTRAEP_BF16 ? 2 : 4;
+  auto wide = [&](const void *p, int es, int64_t pitch) {
+    return r.E % vpl == 0 && vpl * es % 16 == 0 && pitch * es % 16 == 0 &&
+           (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+  };
   const RouteGradArgs a{logits, dlogits, T, ld, s.seq, mask, topk, dgate, coef, dloss, r.E, r.k,
-                        r.score == ULTRAEP_SIGMOID, r.renorm, r.scale, status};
-  const int vpl = (r.E + kWave - 1) / kWave;
-  const int64_t wg = (T + kRtWaves - 1) / kRtWaves;
-  const dim3 grid(static_cast<unsigned>(wg < 16384 ? wg : 16384));
-#define UEP_CASE(n)                                                                               \
-  if (vpl <= n) {                                                                                 \
-    if (type == ULTRAEP_BF16)                                                                     \
-      hipLaunchKernelGGL((k_route_grad<n, true>), grid, dim3(kRtThreads), 0, stream, a);          \
-    else                                                                                          \
-      hipLaunchKernelGGL((k_route_grad<n, false>), grid, dim3(kRtThreads), 0, stream, a);         \
-    return hipGetLastError();                                                                     \
+                        r.score == ULTRAEP_SIGMOID, r.renorm,
+                        wide(logits, esize, ld) && wide(dlogits, esize, ld), wide(coef, 4, r.E),
+                        r.scale, status};
+  const int64_t parts = kRtThreads / lanes, wg = (T + parts - 1) / parts;
+  const dim3 grid(static_cast<unsigned>(wg < 1 << 16 ? wg : 1 << 16));
+#define UEP_CASE(m, n)                                                                             \
+  if (lanes == m && vpl == n) {                                                                    \
+    if (type == ULTRAEP_BF16)                                                                      \
+      hipLaunchKernelGGL((k_route_grad<m, n, true>), grid, dim3(kRtThreads), 0, stream, a);        \
+    else                                                                                           \
+      hipLaunchKernelGGL((k_route_grad<m, n, false>), grid, dim3(kRtThreads), 0, stream, a);       \
+    return hipGetLastError();                                                                      \
   }
-  UEP_CASE(1) UEP_CASE(2) UEP_CASE(4) UEP_CASE(8) UEP_CASE(16)
+  UEP_CASE(16, 4) UEP_CASE(16, 8) UEP_CASE(16, 12) UEP_CASE(16, 16) UEP_CASE(16, 24)
+  UEP_CASE(16, 32) UEP_CASE(64, 8) UEP_CASE(64, 16)
 #undef UEP_CASE
   return hipErrorInvalidValue;
 }
