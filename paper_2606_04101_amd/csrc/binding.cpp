@@ -509,10 +509,11 @@ ENTRY(expert_matmul, 15, {
   });
 })
 
-// bind({entry point: address}, Group, Plan, PlanBuf, Router)
+// bind({entry point: address}, Group, Plan, PlanBuf[, Router]); without Router no call with
+// one is taken
 PyObject *py_bind(PyObject *, PyObject *args) {
-  PyObject *d, *g, *p, *b, *r;
-  if (!PyArg_ParseTuple(args, "O!OOOO", &PyDict_Type, &d, &g, &p, &b, &r)) return nullptr;
+  PyObject *d, *g, *p, *b, *r = nullptr;
+  if (!PyArg_ParseTuple(args, "O!OOO|O", &PyDict_Type, &d, &g, &p, &b, &r)) return nullptr;
 #define SET(n)                                                                        \
   {                                                                                   \
     PyObject *v = PyDict_GetItemString(d, "ultraep_" #n);                             \
@@ -524,7 +525,7 @@ PyObject *py_bind(PyObject *, PyObject *args) {
   Py_INCREF(g);
   Py_INCREF(p);
   Py_INCREF(b);
-  Py_INCREF(r);
+  Py_XINCREF(r);
   Py_XDECREF(t_group);
   Py_XDECREF(t_plan);
   Py_XDECREF(t_buf);
