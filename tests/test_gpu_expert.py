@@ -141,6 +141,39 @@ def test_matmul_blocks(sizes, of, act):
     products(max(1, sum(sizes)), 144, 160, sizes, n_w, act, False, seed=len(sizes), of=of)
 
 
+# (blocks' rows, N, K) that reach each of the tile shapes: few rows with K shared by
+# four waves and by two, 64, 128 and 256 rows a tile; with ends inside tiles and steps
+WIDE = [([3, 0, 40], 16416, 4112), ([41], 16400, 176), ([20], 16400, 4096), ([13, 9, 20], 5472, 272),
+        ([9, 70, 33, 50, 1, 0, 64, 65] * 5, 1040, 144), ([2050], 2064, 80), ([700, 64, 65, 300, 900], 1552, 400),
+        ([3500, 130], 4112, 144), ([257, 1000, 2300], 4112, 48), ([1030, 255, 256, 900, 5], 8208, 1040)]
+
+
+@pytest.mark.parametrize("act", [False, True])
+@pytest.mark.parametrize("sizes,N,K", WIDE)
+def test_matmul_tiles(sizes, N, K, act):
+    products(sum(sizes), N, K, sizes, len(sizes), act, N % 32 == 0 or K == 144, seed=N)
+
+
+def test_matmul_one_weight_past_32_bits():
+    """N * K over 4 GB: the last channels, for few rows and for many."""
+    N, K = 69_648, 65_536
+    wq = torch.zeros(1, N, K, dtype=torch.int8, device="cuda")
+    wq[0, -16:] = torch.randint(-127, 128, (16, K), dtype=torch.int8, device="cuda")
+    wq[0, N // 2 - 16:N // 2] = torch.randint(-127, 128, (16, K), dtype=torch.int8, device="cuda")
+    w = np.concatenate([wq[0, N // 2 - 16:N // 2].cpu().numpy(), wq[0, -16:].cpu().numpy()])[None]
+    for M in (2, 70, 400):
+        xq = torch.randint(-127, 128, (M, K), dtype=torch.int8, device="cuda")
+        xs, ws = torch.rand(M, device="cuda") * 1e-3, torch.rand(1, N, device="cuda") * 1e-3
+        s = torch.cat([ws[:, N // 2 - 16:N // 2], ws[:, -16:]], 1).cpu().numpy()
+        for act in (False, True):
+            y, st = torch.ones(M, N // 2 if act else N, device="cuda"), status()
+            uep.ultraep_expert_matmul(xq, xs, M, wq, ws, 1, N, K, torch.tensor([0, M], device="cuda"), None, 1, act, y, st)
+            want, rel = p64.expert_matmul(xq.cpu().numpy(), xs.cpu().numpy(), w, s, [0, M], None, act)
+            got = (y[:, -16:] if act else torch.cat([y[:, N // 2 - 16:N // 2], y[:, -16:]], 1)).double().cpu().numpy()
+            assert (np.abs(got - want) <= rel * np.abs(want) + 1e-37).all()
+            assert not y[:, :N // 2 - 16].any() and int(st.item()) == 0
+
+
 def test_matmul_part_of_the_blocks():
     """Blocks that begin and end inside the rows."""
     products(300, 80, 96, [40, 0, 100], 3, False, False, start=37)
@@ -150,6 +183,10 @@ def test_matmul_part_of_the_blocks():
 def test_matmul_largest_sums(M):
     """127 * 127 * K at the longest K: the sum just fits 32 bits."""
     products(M, 16, 1 << 16, [M], 1, False, True, extreme=True)
+
+
+def test_matmul_part_of_many_rows():
+    products(6000, 1040, 80, [1500, 0, 2100], 3, True, False, start=301)
 
 
 @pytest.mark.parametrize("M", [3, 400])

@@ -201,6 +201,47 @@ def test_gradient_against_differences(score, renorm):
             assert abs(got[t, e] - diff) <= 2 * SCORE_U * mag[e] + 1e-8  # differences: h^2, 1e-16 / h
 
 
+@pytest.mark.parametrize("E,k,score,ng,tg,bf16", [
+    (256, 8, "sigmoid", 8, 4, False), (128, 8, "softmax", 0, 0, True), (72, 6, "softmax", 8, 3, True),
+    (60, 16, "sigmoid", 0, 0, False), (384, 12, "softmax", 0, 0, False), (512, 8, "sigmoid", 16, 5, False),
+    (640, 8, "softmax", 0, 0, True), (64, 17, "softmax", 0, 0, True)])
+def test_many_tokens(E, k, score, ng, tg, bf16):
+    """With and without statistics, and in calls of fewer tokens: the same ids, and
+    equal sums for equal calls; a sample of the tokens against the plain form."""
+    rng = np.random.default_rng(E)
+    T = 4500
+    r = router(E=E, k=k, score=score, n_group=ng, top_group=tg, seq_len=2100, scale=1.5)
+    z = logits(rng, T, E, bf16, spread=1.0)
+    z[:, :E // 5] += np.float32(2)   # neighbouring experts that most tokens choose among
+    z = p64.bf16(z) if bf16 else z
+    z[100:140] = z[100]              # and tokens in a row that are alike
+    z[200:230] = 0.25                # or tie everywhere
+    sample = np.r_[0:20, 95:105, 198:204, 4480:4500]
+    z[sample] = apart(rng, z[sample], r, None, bf16)
+    mask = rng.random(T) > 0.1
+    o, st, lg, _ = run_route(z, r, bf16, mask=mask)
+    assert st == 0
+    ref = p64.route(z[sample], {**r, "seq_len": 0}, mask=mask[sample])
+    check_route(dict(topk=o["topk"][sample], gate=o["gate"][sample]), ref, stats=False)
+    seq = np.arange(T) // 2100
+    for s in range(3):
+        chosen = o["topk"][seq == s]
+        assert np.array_equal(o["counts"][s], np.bincount(chosen[chosen >= 0], minlength=E))
+        assert o["tokens"][s] == (chosen[:, 0] >= 0).sum() == mask[seq == s].sum()
+    p = np.exp(z.astype(np.float64) - z.max(1, keepdims=True).astype(np.float64)) if score == "softmax" \
+        else p64.sigmoid(z.astype(np.float64))
+    p = p / p.sum(1, keepdims=True) * mask[:, None]
+    psum = np.stack([p[seq == s].sum(0) for s in range(3)])
+    assert (np.abs(o["prob_sum"] - psum) <= (SCORE_U + p64.U32 * 2100) * psum).all()
+    again = run_route(z, r, bf16, mask=mask)[0]
+    assert all(o[n].tobytes() == again[n].tobytes() for n in o)
+    bare = run_route(z, r, bf16, mask=mask, stats=False)[0]
+    few = [run_route(z[a:a + 1500], r, bf16, mask=mask[a:a + 1500], stats=False)[0] for a in (0, 1500, 3000)]
+    for other in (bare, {n: np.concatenate([f[n] for f in few]) for n in ("topk", "gate")}):
+        assert np.array_equal(other["topk"], o["topk"])
+        assert (np.abs(other["gate"] - o["gate"]) <= 2 * SCORE_U * o["gate"]).all()
+
+
 def test_ties_go_to_the_lower_id_and_group():
     z = np.zeros((3, 64), np.float32)
     z[1, 10:20] = 1.0
