@@ -280,7 +280,7 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(lds), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 
 // the same for 4 bytes a lane
@@ -288,7 +288,7 @@ __device__ __forceinline__ void load_word_to_lds(const void *base, uint32_t off,
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                :
                : "s"(lds), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 template <class T>
 __device__ __forceinline__ uint32_t lds_address(T *p) {
