@@ -2,6 +2,13 @@
 // slots' rows y weighted by their gates, so with dout its gradient
 //   dy[row] = gate * dout[t],  dgate = <dout[t], y[row]>
 // in one pass: each y row is read once, each dy row written once, dout once.
+//
+// Bound by memory: one workgroup a token, so that dgate's sums stay in it, with up
+// to 8 of the token's rows' loads in flight together; y and dy pass the caches by.
+// The DeepSeek-V3-shaped training layer (4096 tokens of 8 x 7168, 999 MB) takes
+// 188 us, 5.3 TB/s, where a copy of 2 GiB reaches 5.0; 187-193 us with 64 to 512
+// threads, 201 with loads and 205 with stores that stay in the caches.  A small batch
+// is bound by its chain of loads: 333 tokens of 6 x 2880 (24 MB) take 8.5 us.
 #include "operators.hpp"
 
 namespace uep {

@@ -7,6 +7,11 @@
 // group's sum of two largest keys is a merge over neighbouring lanes.  Where a
 // group does not fill its lanes, the ends of them are holes: an expert's place
 // among lanes and holes is its slot, of the same order as the ids.
+//
+// A call reads little (4096 tokens of 256 experts: 4 MB), so instructions and the
+// chain of loads bound it, and launches: ids, gates and statistics of those 4096
+// tokens, by groups, take 8.8 us, their sums over the workgroups 2.6, the loss 2.4, the
+// gradient 6.7; 16384 tokens of 128 experts 9.4, 4.0, 2.2; one token of 256 4.6.
 #include "operators.hpp"
 
 namespace uep {
