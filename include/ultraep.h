@@ -481,10 +481,10 @@ int ultraep_quant_rows(const void *x, int32_t type, int64_t rows, int64_t K, int
  *   block_w    [n_block] int32, or null (block g takes weight g)
  *   y          [M][N], or [M][N / 2] with act
  * Blocks that are not in rising order within [0, M], and a nonempty block
- * whose weight is outside [0, n_w), raise ULTRAEP_EDATA and are skipped.
+ * whose weight is outside [0, n_w), raise ULTRAEP_EDATA; then no row is written.
  * 1 <= n_block <= 2048, n_w >= 1, M < 2^31; K % 16 == 0, K <= 2^16 (the sum
  * stays within 32 bits), N % 8 == 0 (N % 16 == 0 with act), N <= 2^20,
- * M * N < 2^40; 16-byte aligned xq, wq and y.  M = 1 is the decode form: any M takes any blocks. */
+ * M * N < 2^38; 16-byte aligned xq, wq and y.  M = 1 is the decode form: any M takes any blocks. */
 int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
                           const int8_t *wq, const float *w_scale, int32_t n_w, int32_t N,
                           int32_t K, const int64_t *block_off, const int32_t *block_w,

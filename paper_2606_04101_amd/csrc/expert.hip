@@ -208,9 +208,10 @@ struct RowTile {
 };
 
 // Row tiles are numbered block by block.  Blocks are looked at in runs of 64, one a
-// lane; a wave holds one run's blocks, and the runs' tile counts, in registers.  A
-// block that is out of order or out of [0, M], or has rows and no weight, is reported
-// and has no tile.  Every lane must be active in each call.
+// lane; a wave holds one run's blocks, and the runs' tile counts, in registers.  Where a
+// block is out of order or out of [0, M], or has rows and no weight, that is reported and
+// there are no tiles at all, so that what is numbered lies within M rows.  Every lane
+// must be active in each call.
 template <int kTileRows>
 struct RowTiles {
   int64_t lo;               // this lane's block of run `run`:
@@ -220,8 +221,10 @@ struct RowTiles {
   int run_before, run_tiles;  // of run `lane`
   int total;                // tiles in all
 
-  __device__ void load(const MatmulArgs &a, int r) {
+  // false (in the whole wave) if a block of run r is not sound
+  __device__ bool load(const MatmulArgs &a, int r) {
     run = r;
+    bool sound = true;
     const int g = r * kWave + lane_id();
     lo = 0;
     rows = w = 0;
@@ -229,33 +232,36 @@ struct RowTiles {
       lo = a.block_off[g];
       const int64_t hi = a.block_off[g + 1];
       w = a.block_w ? a.block_w[g] : g;
-      if (lo < 0 || hi < lo || hi > a.M || (hi > lo && (w < 0 || w >= a.n_w)))
-        report(a.status, ULTRAEP_EDATA);
-      else
+      sound = lo >= 0 && hi >= lo && hi <= a.M && (hi == lo || (w >= 0 && w < a.n_w));
+      if (sound)
         rows = static_cast<int>(hi - lo);
+      else
+        report(a.status, ULTRAEP_EDATA);
     }
     tiles = rows > 0 ? (rows - 1) / kTileRows + 1 : 0;
     before = wave_scan_incl(tiles) - tiles;
+    return !ballot(!sound);
   }
   // s_run: 32 words of LDS, free again after the call's last barrier
   __device__ void count(const MatmulArgs &a, int *s_run, int wave, int n_waves) {
     n_run = (a.n_block + kWave - 1) / kWave;
     if (n_run == 1) {
-      load(a, 0);
+      const bool sound = load(a, 0);
       run_before = 0;
-      total = readlane(before + tiles, kWave - 1);
+      total = sound ? readlane(before + tiles, kWave - 1) : 0;
       run_tiles = lane_id() == 0 ? total : 0;
       return;
     }
     for (int r = wave; r < n_run; r += n_waves) {
-      load(a, r);
-      if (lane_id() == kWave - 1) s_run[r] = before + tiles;
+      const bool sound = load(a, r);
+      if (lane_id() == kWave - 1) s_run[r] = sound ? before + tiles : -1;
     }
     __syncthreads();
     run_tiles = lane_id() < n_run ? s_run[lane_id()] : 0;
     __syncthreads();
     run_before = wave_scan_incl(run_tiles) - run_tiles;
     total = readlane(run_before, kWave - 1);  // (fewer than 64 runs)
+    if (ballot(run_tiles < 0)) total = 0;
     run = -1;
   }
   // tile < total
@@ -338,7 +344,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
   RowTiles<kM> tiles;
   tiles.count(a, s_run, wave, kWaves);
   const int n_tile = tiles.total;
-  const int n_item = n_tile * n_col;  // (a y that fits the memory has fewer than 2^31)
+  const int n_item = n_tile * n_col;  // (fewer than 2^31: M * N < 2^38)
 
   // the workgroups of one XCD (those of equal number modulo 8) take neighbouring
   // items, 8 row tiles by 4 column tiles at a time

@@ -122,7 +122,7 @@ int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
     return ULTRAEP_EINVAL;
   if (K < 16 || K % 16 != 0 || K > 1 << 16) return ULTRAEP_EINVAL;
   if (N < 8 || N % (act ? 16 : 8) != 0 || N > 1 << 20) return ULTRAEP_EINVAL;
-  if (M * static_cast<int64_t>(N) >= int64_t(1) << 40) return ULTRAEP_EINVAL;
+  if (M * static_cast<int64_t>(N) >= int64_t(1) << 38) return ULTRAEP_EINVAL;
   if (!wq || !aligned16(wq) || !w_scale) return ULTRAEP_EINVAL;
   if (M == 0) return ULTRAEP_OK;
   if (!xq || !aligned16(xq) || !x_scale || !y || !aligned16(y)) return ULTRAEP_EINVAL;

@@ -143,7 +143,7 @@ def test_matmul_blocks(sizes, of, act):
 
 # (blocks' rows, N, K) that reach each of the tile shapes: few rows with K shared by
 # four waves and by two, 64, 128 and 256 rows a tile; with ends inside tiles and steps
-WIDE = [([3, 0, 40], 16416, 4112), ([41], 16400, 176), ([20], 16400, 4096), ([13, 9, 20], 5472, 272),
+WIDE = [([3, 0, 40], 16416, 4112), ([45], 16400, 4112), ([41], 16400, 176), ([20], 16400, 4096), ([13, 9, 20], 5472, 272),
         ([9, 70, 33, 50, 1, 0, 64, 65] * 5, 1040, 144), ([2050], 2064, 80), ([700, 64, 65, 300, 900], 1552, 400),
         ([3500, 130], 4112, 144), ([257, 1000, 2300], 4112, 48), ([1030, 255, 256, 900, 5], 8208, 1040)]
 
@@ -191,7 +191,7 @@ def test_matmul_part_of_many_rows():
 
 @pytest.mark.parametrize("M", [3, 400])
 def test_matmul_bad_blocks(M):
-    """Out of order, out of range, or without a weight: reported, and skipped."""
+    """Out of order, out of range, or without a weight: reported, and nothing written."""
     N, K = 64, 64
     xq, wq = torch.ones(M, K, dtype=torch.int8, device="cuda"), torch.ones(2, N, K, dtype=torch.int8, device="cuda")
     xs, ws = torch.ones(M, device="cuda"), torch.ones(2, N, device="cuda")
@@ -200,7 +200,12 @@ def test_matmul_bad_blocks(M):
         y, st = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda"), status()
         uep.ultraep_expert_matmul(xq, xs, M, wq, ws, 2, N, K, dev(np.array(off, np.int64)),
                                   None if of is None else dev(np.array(of, np.int32)), 2, False, y, st)
-        assert int(st.item()) == uep.ULTRAEP_EDATA
+        assert int(st.item()) == uep.ULTRAEP_EDATA and not y.any()
+    off = np.full(201, M, np.int64)  # a bad block among several runs of 64
+    off[:101:2], off[1:101:2] = 0, M
+    y, st = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda"), status()
+    uep.ultraep_expert_matmul(xq, xs, M, wq, ws, 2, N, K, dev(off), dev(np.zeros(200, np.int32)), 200, False, y, st)
+    assert int(st.item()) == uep.ULTRAEP_EDATA and not y.any()
     y, st = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda"), status()
     uep.ultraep_expert_matmul(xq, xs, M, wq, ws, 2, N, K, dev(np.array([0, 2, 2], np.int64)),
                               dev(np.array([1, -1], np.int32)), 2, False, y, st)

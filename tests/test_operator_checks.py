@@ -126,7 +126,7 @@ def test_bad_arguments_are_refused():
 
     def mm(xq=p, xs=p, M=4, wq=p, ws=p, n_w=2, N=16, K=32, off=p, of=None, n=2, act=0, y=p, type=1, st=p):
         return L.ultraep_expert_matmul(xq, xs, M, wq, ws, n_w, N, K, off, of, n, act, y, type, st, None)
-    for kw in [dict(M=-1), dict(M=1 << 31), dict(n_w=0), dict(N=0), dict(N=12), dict(N=(1 << 20) + 8),
+    for kw in [dict(M=-1), dict(M=1 << 31), dict(M=1 << 30, N=256), dict(n_w=0), dict(N=0), dict(N=12), dict(N=(1 << 20) + 8),
                dict(N=8, act=1), dict(act=2), dict(K=0), dict(K=24), dict(K=(1 << 16) + 16), dict(n=0),
                dict(n=2049), dict(type=3), dict(xq=None), dict(xq=odd), dict(xs=None), dict(wq=None),
                dict(wq=odd), dict(ws=None), dict(off=None), dict(y=None), dict(y=odd), dict(st=None)]:
