@@ -1,4 +1,5 @@
-"""UltraEP per-microbatch balancing path for MI355X (gfx950).
+"""UltraEP per-microbatch balancing path for MI355X (gfx950), and the operators
+of the MoE layer around it.
 
 Thin ctypes binding of ``libultraep.so`` (C ABI in ``include/ultraep.h``).
 Every function has the name of the C entry point it calls and only marshals
