@@ -296,6 +296,11 @@ def test_combine_grad(T, k, H, masked, extra):
     assert (np.abs(g[slots] - (a * b).sum(1)) <= (H + 1) * p64.U32 * np.abs(a * b).sum(1)).all()
 
 
+@pytest.mark.parametrize("T,H", [(256, 4096), (256, 4104), (257, 4104), (40, 512), (40, 520), (700, 8)])
+def test_combine_grad_at_each_workgroup_size(T, H):
+    test_combine_grad(T, 3, H, 0.2, 2)
+
+
 def test_combine_grad_is_the_gradient_of_the_combine():
     """Of the objective sum dout * combine(y, gate), linear in y and in gate: the
     objective's change along random directions, in 64 bits."""
