@@ -317,41 +317,43 @@ constexpr int kBk = 128;  // bytes of K of a step
 // Loads go straight to LDS, two steps ahead, and a step has one barrier, before its
 // last quarter: by then its own bytes are in registers, and the next step's have come.
 // kAhead: the next tile's first two steps are loaded while the results leave.
-//   131072 rows of 10 blocks, N = 4096, K = 7168, act, bf16: 3.28 ms, 2.34 POP/s (a
-// library product of 8192^3 reaches 2.14 here); 32761 rows of 6 blocks, N = 4096,
-// K = 1408: 237 us, 1.60 POP/s.  Bound by power: 62 % of the matrix unit's cycles
-// at 1.6 GHz; with zeros as data the first takes 2.65 ms.
-template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kAct, bool kBf16>
-__global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t n_col) {
-  constexpr int kThreads = 64 * kWn * kWm, kWaves = kWn * kWm;
+//   Where the tiles of the last round are at most a quarter of the workgroups, these take
+// quarters of them: 4608 rows of one block, N = 4096, K = 7168, act, 288 tiles for 256
+// workgroups, take 144 us, with a second full round 184.  (Up to half the workgroups,
+// in two rounds of quarters: 289 us for 300 at 10240 rows, but 3395 for 3370 at 131072.)
+//   131072 rows of 10 blocks, N = 4096, K = 7168, act, bf16: 3.25 to 3.37 ms by the card,
+// 2.37 POP/s (a library product of 8192^3 reaches 2.14 here); 32761 rows of 6 blocks, N = 4096, K = 1408:
+// 229 us, 1.65 POP/s (239 without quarters).  Bound by power: 62 % of the matrix unit's
+// cycles at 1.6 GHz; with zeros as data the first takes 2.65 ms.
+template <int kN, int kM, int kWn, int kWm, bool kAhead>
+struct MatmulShape {
+  static constexpr int kBuf = (kN + kM) * kBk, kTurns = kAhead ? 2 : 1;
+  static constexpr int kWaves = kWn * kWm;
+  static constexpr int kLds = 2 * kBuf + (kAhead ? kWaves * 4096 : 0);
+  static constexpr int kScales = kTurns * (kN + kM);  // of this item, and of the next
+  static_assert(kAhead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
+};
+
+// Items item, item + stride, .. below n_item, item 0 being that numbered `first`.  An
+// item is a tile that `tiles` numbers, or (kPart = 2) a quarter of one, 2 x 2.
+template <int kN, int kM, int kWn, int kWm, bool kAhead, int kPart, bool kAct, bool kBf16>
+__device__ __forceinline__ void matmul_items(const MatmulArgs &a, int32_t n_col,
+                                             RowTiles<kM * kPart> &tiles, int8_t *s_lds,
+                                             float *s_scale, int first, int item, int stride, int n_item) {
+  constexpr int kWaves = kWn * kWm;
   constexpr int kFn = kN / kWn / 32, kFm = kM / kWm / 32;  // 32 x 32 parts of a wave
-  constexpr int kBuf = (kN + kM) * kBk;
+  constexpr int kBuf = MatmulShape<kN, kM, kWn, kWm, kAhead>::kBuf;
   constexpr int kLoads = kBuf / 1024 / kWaves;             // of a wave in a step
   constexpr int kLoadsN = kLoads * kN / (kN + kM);
-  constexpr int kOut = kAct ? kN / 2 : kN;                 // channels of a tile
+  constexpr int kOut = kAct ? kN / 2 : kN;                 // channels of an item
   constexpr int kOutW = kOut / kWn;                        // of a wave
-  constexpr int kTurns = kAhead ? 2 : 1;
   static_assert(!kAct || kFn % 2 == 0, "a wave has gates with their partners");
-  static_assert(kAhead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
-  __shared__ __align__(1024) int8_t s_lds[2 * kBuf + (kAhead ? kWaves * 4096 : 0)];
-  __shared__ __align__(16) float s_scale[kTurns][kN + kM];  // of this item, and of the next
-  __shared__ int s_run[32];
-  const int tid = threadIdx.x, lane = lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wn = wave % kWn, wm = wave / kWn;
   const int lr = lane & 31, hi = lane >> 5;
-  const int half = a.N / 2;
-  RowTiles<kM> tiles;
-  tiles.count(a, s_run, wave, kWaves);
-  const int n_tile = tiles.total;
-  const int n_item = n_tile * n_col;  // (fewer than 2^31: M * N < 2^38)
-
-  // the workgroups of one XCD (those of equal number modulo 8) take neighbouring
-  // items, 8 row tiles by 4 column tiles at a time
-  constexpr int kXcd = 8, kGroup = 8;
-  const int per_xcd = gridDim.x / kXcd;  // the grid is a multiple
-  const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
-  const uint32_t lds0 = lds_address(s_lds), lds_scale = lds_address(&s_scale[0][0]);
+  const int half = a.N / 2, n_tile = tiles.total;
+  const uint32_t lds0 = lds_address(s_lds), lds_scale = lds_address(s_scale);
   const int steps = (a.K + kBk - 1) / kBk;
   const int tail = (a.K - (steps - 1) * kBk) / 16;  // chunks of the last step
 
@@ -364,13 +366,22 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
   uint32_t off[kLoads];
   int turn = 0;  // which part of s_scale the item's scales are in
   const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
-  auto aim = [&](int item) {
+  // false for a quarter that has no rows or no channels
+  auto aim = [&](int id) {
+    const int item = first + id / (kPart * kPart), part = id % (kPart * kPart);
     const int lane = opaque(lane_id());
     const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    // 8 row tiles by all columns at a time
+    constexpr int kGroup = 8;
     const int group = item / (kGroup * n_col), rest = item - group * kGroup * n_col;
     const int high = min(kGroup, n_tile - group * kGroup);
     tile = tiles.find(a, group * kGroup + rest % high);
-    n0 = rest / high * kOut;
+    n0 = (rest / high * kPart + part / kPart) * kOut;
+    if (kPart > 1) {
+      tile.row += part % kPart * kM;
+      tile.rows = min(tile.rows - part % kPart * kM, kM);
+      if (tile.rows <= 0 || n0 >= a.n_out) return false;
+    }
     wbase = uniform(a.wq + (static_cast<int64_t>(tile.w) * a.N + n0) * a.K);
     xbase = uniform(a.xq + tile.row * a.K);
     // weight row of tile row j after the tile's first (with act, among the gates or
@@ -396,6 +407,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
       load_word_to_lds(j < kN ? ws : xs, r * 4,
                        __builtin_amdgcn_readfirstlane(lds_scale + (turn * (kN + kM) + j) * 4));
     }
+    return true;
   };
   // load i of a step; chunks past K (in the last step) are loaded from the step's
   // first one and not used
@@ -408,14 +420,18 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
     load_to_lds(base + static_cast<int64_t>(s) * kBk, off[i] - back,
                 __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * kBuf + (i * kWaves + wave) * 1024));
   };
-  auto begin = [&](int item) {
-    aim(item);
+  // the first item from `item` on that has work: false if there is none
+  auto begin = [&] {
+    do {
+      if (item >= n_item) return false;
+    } while (!aim(item) && (item += stride, true));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) issue(0, i);
     if (steps > 1) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) issue(1, i);
     }
+    return true;
   };
 
   auto arrived = [&] {  // the first step's bytes are there
@@ -425,9 +441,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   };
 
-  int item = slot;
-  if (item >= n_item) return;
-  begin(item);
+  if (!begin()) return;
   arrived();
   while (true) {
     asm volatile("s_barrier" : : : "memory");
@@ -486,15 +500,14 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
     const RowTile out = tile;
     const int nw = n0 + wn * kOutW;  // the wave's first channel
     const int was = turn;
-    item += gridDim.x;
-    const bool more = item < n_item;
-    if (kAhead && more) begin(item);
+    item += stride;
+    const bool more = kAhead && begin();
 
     // 32 rows x 64 channels (32 in fp32) at a time through LDS, so that a row's
     // channels leave in whole lines
     constexpr int kParts = kOutW / 32;
     const int el = opaque(lane), er = el & 31, eh = el >> 5;
-    const float *scale = s_scale[was];
+    const float *scale = s_scale + was * (kN + kM);
     int8_t *stage = s_lds + (kAhead ? 2 * kBuf : 0) + wave * 4096;
 #pragma unroll
     for (int j = 0; j < kFm; ++j) {
@@ -548,12 +561,37 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (!more) return;
-    if (!kAhead) {
+    if (kAhead) {
+      if (!more) return;
+    } else {
       __syncthreads();
-      begin(item);
+      if (!begin()) return;
       arrived();
     }
+  }
+}
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kAct, bool kBf16>
+__global__ void __launch_bounds__(64 * kWn * kWm) k_matmul(MatmulArgs a, int32_t n_col) {
+  using Shape = MatmulShape<kN, kM, kWn, kWm, kAhead>;
+  __shared__ __align__(1024) int8_t s_lds[Shape::kLds];
+  __shared__ __align__(16) float s_scale[Shape::kScales];
+  __shared__ int s_run[32];
+  RowTiles<kM> tiles;
+  tiles.count(a, s_run, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), Shape::kWaves);
+  const int n_item = tiles.total * n_col;  // (fewer than 2^31: M * N < 2^38)
+  // the workgroups of one XCD (those of equal number modulo 8) take neighbouring items
+  constexpr int kXcd = 8;
+  const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
+  const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
+  int last = 0;  // tiles of the last round that are taken by quarters
+  if (kAhead && n_item % grid * 4 <= grid) last = n_item % grid;
+  matmul_items<kN, kM, kWn, kWm, kAhead, 1, kAct, kBf16>(a, n_col, tiles, s_lds, s_scale, 0, slot,
+                                                         grid, n_item - last);
+  if constexpr (kAhead) {
+    __syncthreads();
+    matmul_items<kN / 2, kM / 2, kWn, kWm, false, 2, kAct, kBf16>(
+        a, n_col, tiles, s_lds, s_scale, n_item - last, slot, grid, last * 4);
   }
 }
 
@@ -731,28 +769,36 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
   const MatmulArgs a{xq, xs, wq, ws, block_off, block_w, y, status, M, n_w, N, K, n_block,
                      act ? N / 2 : N};
   const bool bf16 = type == ULTRAEP_BF16;
-  // Tiles of 256 x 256 where the blocks are large and fill the 256 compute units in
-  // nearly whole rounds; else smaller ones, so that there are enough of them and few
-  // rows are padding; else, for few rows, the kernel that shares K between waves.
-  // `rows`: mean of a block that has any; tiles: estimated row tiles, half a tile of
-  // padding a block.  Measured, us (256 x 256 / 128 x 128 / 128 x 64 / thin 64 / 32 / 16):
-  //   10 blocks, N = 4096, K = 7168, act: M = 8192 313 / 303 / 408 / 454 / 561 / 808,
-  //   2048 112 / 128 / 156 / 152 / 182 / 250, 1024 105 / 81 / 112 / 100 / 118 / 148,
+  // Tiles of 256 x 256 or 128 x 128 where the blocks are large, by the rounds that either
+  // takes; 128 x 64 where there are few of those; else, for few rows, the kernel that
+  // shares K between waves.  `rows`: mean of a block that has any; items: estimated
+  // tiles, half a tile of padding a block where there are several.
+  //   Times in tenths of a round of 256 x 256: 4 for the round of its quarters, 6 for a
+  // round of 128 x 128, two tiles a compute unit.
+  //   Measured, us (256 x 256 / 128 x 128 / 128 x 64 / thin 64 / 32 / 16):
+  //   10 blocks, N = 4096, K = 7168, act: M = 20480 584 / 646, 10240 326 / 354, 9216 317 /
+  //   309, 8192 300 / 299 / 408 / 454 / 561 / 808, 6144 213 / 246, 5120 215 / 194, 3328 156 /
+  //   138, 2048 112 / 128 / 156 / 152 / 182 / 250, 1024 105 / 81 / 112 / 100 / 118 / 148,
   //   512 102 / 76 / 71 / 76 / 83 / 96, 256 101 / 69 / 69 / 66 / 65 / 68, 64 98 / 67 / 65
   //   / 64 / 58 / 51
-  //   1 block, the same: M = 4096 108 / 121 / 163 / 204, 1024 78 / 44 / 44 / 53 / 70, 256
+  //   1 block, the same: M = 8704 246 / 291, 8192 207 / 237, 6144 204 / 177, 4608 139 / 170,
+  //   4096 105 / 119 / 163 / 204, 2048 89 / 62, 1024 78 / 44 / 44 / 53 / 70, 256
   //   79 / 38 / 34 / 18 / 22 / 26, 128 79 / 38 / 34 / 17 / 13 / 17, 16 78 / 37 / 34 / 16 / 11 / 9
   //   64 blocks, N = 1024, K = 2048: M = 8192 45 / 51 / 56 / 64, 4096 40 / 29 / 40 / 44,
   //   1024 34 / 25 / 25 / 30 / 29 / 28
-  //   6 blocks, N = 4096, K = 1408: M = 8192 76 / 74 / 99, 512 24 / 15 / 13 / 18 / 18 / 19,
-  //   256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11 / 11 / 11 / 10
+  //   6 blocks, N = 4096, K = 1408: M = 20480 154 / 171, 8192 69 / 76 / 99, 5120 53 / 45, 512
+  //   24 / 15 / 13 / 18 / 18 / 19, 256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11 / 11 / 11
+  //   / 10
   const int64_t blocks = M < n_block ? M : n_block, rows = (M + blocks - 1) / blocks;
   auto items = [&](int64_t tile_rows, int64_t channels) {
-    return (M / tile_rows + (blocks + 1) / 2) * ((N + channels - 1) / channels);
+    return (blocks > 1 ? M / tile_rows + (blocks + 1) / 2 : (M + tile_rows - 1) / tile_rows) *
+           ((N + channels - 1) / channels);
   };
-  const int64_t big = items(256, 256), rounds = (big + 255) / 256;
+  const int64_t big = items(256, 256), full = big / 256, last = big % 256;
+  const int64_t big_time = full * 10 + (last == 0 ? 0 : full && last <= 64 ? 4 : 10);
+  const int64_t mid_time = (items(128, 128) + 511) / 512 * 6;
   const bool deep = K >= 4096;  // four waves' worth of steps
-  if (rows > 96 && big * 5 >= rounds * 256 * 4)
+  if (rows > 96 && big_time < mid_time)
     start_matmul<256, 256, 2, 2, true>(a, act, bf16, 256, stream);
   else if (rows > 56 && items(128, 128) >= 256)
     start_matmul<128, 128, 2, 2, false>(a, act, bf16, 512, stream);

@@ -154,6 +154,18 @@ def test_matmul_tiles(sizes, N, K, act):
     products(sum(sizes), N, K, sizes, len(sizes), act, N % 32 == 0 or K == 144, seed=N)
 
 
+# several rounds of 256-row tiles over 256 workgroups, the last of them whole (442 and 680
+# tiles) or by quarters (289, 306, 279, 320), some of those with no rows or no channels
+ROUNDS = [([130, 5000, 3, 900], 4112, 80), ([10100], 4112, 16), ([4300], 4112, 48), ([100, 4200], 4112, 144),
+          ([7900], 2064, 272), ([5100], 4096, 96)]
+
+
+@pytest.mark.parametrize("act", [False, True])
+@pytest.mark.parametrize("sizes,N,K", ROUNDS)
+def test_matmul_rounds(sizes, N, K, act):
+    products(sum(sizes), N, K, sizes, len(sizes), act, K > 100, seed=N)
+
+
 def test_matmul_one_weight_past_32_bits():
     """N * K over 4 GB: the last channels, for few rows and for many."""
     N, K = 69_648, 65_536
