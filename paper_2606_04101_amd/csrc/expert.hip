@@ -321,9 +321,9 @@ constexpr int kBk = 128;  // bytes of K of a step
 // quarters of them: 4608 rows of one block, N = 4096, K = 7168, act, 288 tiles for 256
 // workgroups, take 144 us, with a second full round 184.  (Up to half the workgroups,
 // in two rounds of quarters: 289 us for 300 at 10240 rows, but 3395 for 3370 at 131072.)
-//   131072 rows of 10 blocks, N = 4096, K = 7168, act, bf16: 3.25 to 3.37 ms by the card,
-// 2.37 POP/s (a library product of 8192^3 reaches 2.14 here); 32761 rows of 6 blocks, N = 4096, K = 1408:
-// 229 us, 1.65 POP/s (239 without quarters).  Bound by power: 62 % of the matrix unit's
+//   131072 rows of 10 blocks, N = 4096, K = 7168, act, bf16: 3.23 to 3.37 ms by the card,
+// 2.38 POP/s (a library product of 8192^3 reaches 2.14 here); 32761 rows of 6 blocks,
+// N = 4096, K = 1408: 210 us, 1.80 POP/s.  Bound by power: 62 % of the matrix unit's
 // cycles at 1.6 GHz; with zeros as data the first takes 2.65 ms.
 template <int kN, int kM, int kWn, int kWm, bool kAhead>
 struct MatmulShape {
@@ -504,7 +504,9 @@ __device__ __forceinline__ void matmul_items(const MatmulArgs &a, int32_t n_col,
     const bool more = kAhead && begin();
 
     // 32 rows x 64 channels (32 in fp32) at a time through LDS, so that a row's
-    // channels leave in whole lines
+    // channels leave in whole lines, past the caches (228 us for 210 at 32761 x 4096 x
+    // 1408 where they stay; a quantisation of the result that follows at once reads at
+    // most 67 MB 1 us slower, and the pair takes as long)
     constexpr int kParts = kOutW / 32;
     const int el = opaque(lane), er = el & 31, eh = el >> 5;
     const float *scale = s_scale + was * (kN + kM);
@@ -555,8 +557,9 @@ __device__ __forceinline__ void matmul_items(const MatmulArgs &a, int32_t n_col,
           const int r = p * 8 + el / 8;  // (LDS takes a wave's accesses in order)
           const v4u o = *reinterpret_cast<const v4u *>(stage + r * 128 + ((el & 7) ^ (r & 7)) * 16);
           if (r0 + r < out.rows && c0 + c < min(a.n_out, nw + kOutW))
-            *reinterpret_cast<v4u *>(static_cast<char *>(a.y) +
-                                     ((out.row + r0 + r) * a.n_out + c0 + c) * esize) = o;
+            __builtin_nontemporal_store(
+                o, reinterpret_cast<v4u *>(static_cast<char *>(a.y) +
+                                           ((out.row + r0 + r) * a.n_out + c0 + c) * esize));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
