@@ -339,7 +339,8 @@ struct MatmulShape {
 template <int kN, int kM, int kWn, int kWm, bool kAhead, int kPart, bool kAct, bool kBf16>
 __device__ __forceinline__ void matmul_items(const MatmulArgs &a, int32_t n_col,
                                              RowTiles<kM * kPart> &tiles, int8_t *s_lds,
-                                             float *s_scale, int first, int item, int stride, int n_item) {
+                                             float *s_scale, int first, int item, int stride,
+                                             int n_item) {
   constexpr int kWaves = kWn * kWm;
   constexpr int kFn = kN / kWn / 32, kFm = kM / kWm / 32;  // 32 x 32 parts of a wave
   constexpr int kBuf = MatmulShape<kN, kM, kWn, kWm, kAhead>::kBuf;

@@ -77,6 +77,9 @@ __device__ __forceinline__ float dpp_f(float v) {
 }
 template <int kLanes>
 __device__ __forceinline__ float lanes_sum(float v) {
+  // (rounded before the first sum: fused into it, a product would be the exact one in one
+  // lane and the rounded one in its neighbour, and their sums two numbers)
+  asm("" : "+v"(v));
   v += dpp_f<0xB1>(v);   // quad_perm 1,0,3,2
   v += dpp_f<0x4E>(v);   // quad_perm 2,3,0,1
   v += dpp_f<0x141>(v);  // row_half_mirror

@@ -11,7 +11,7 @@
 // A call reads little (4096 tokens of 256 experts: 4 MB), so instructions and the
 // chain of loads bound it, and launches: ids, gates and statistics of those 4096
 // tokens, by groups, take 8.8 us, their sums over the workgroups 2.6, the loss 2.4, the
-// gradient 6.7; 16384 tokens of 128 experts 9.4, 4.0, 2.2; one token of 256 4.6.
+// gradient 4.7; 16384 tokens of 128 experts 9.4, 4.0, 2.2; one token of 256 4.6.
 #include "operators.hpp"
 
 namespace uep {
@@ -30,7 +30,7 @@ struct RouteArgs {
   float *gate;
   int32_t E, k, sigmoid, renorm, n_group, top_group;
   int32_t group_lanes;  // lanes of a group, a power of two
-  int32_t wide;         // all lanes that have experts have kVpl, in aligned 16 bytes
+  int32_t wide;         // all lanes that have experts have kVpl, in aligned chunks
   int32_t wide_bias;    // and so with the bias
   // the top_group groups spread over all lanes: lanes of one, a power of two, and slots
   // of such a lane, a multiple of 4; 0 slots: they stay where they are
@@ -49,22 +49,39 @@ __device__ __forceinline__ float load_logit(const void *row, int e) {
   return static_cast<const float *>(row)[e];
 }
 
-// A lane's logits, -inf past the n it has.
+// elements that a lane with kVpl of them loads at once: 16 bytes, or 8 in bf16
+constexpr int chunk_of(int vpl, bool bf16) { return bf16 && vpl % 8 == 0 ? 8 : 4; }
+
+// kC logits from element e on, together: aligned
+template <int kC, bool kBf16>
+__device__ __forceinline__ void load_chunk(const void *row, int64_t e, float *z) {
+  if constexpr (kBf16) {
+    typedef uint32_t raw __attribute__((ext_vector_type(kC / 2)));
+    const raw v = *reinterpret_cast<const raw *>(static_cast<const uint16_t *>(row) + e);
+#pragma unroll
+    for (int i = 0; i < kC; ++i) z[i] = i % 2 ? bf16_at_high(v[i / 2]) : bf16_at_low(v[i / 2]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < kC; c += 4) {
+      const v4f v = *reinterpret_cast<const v4f *>(static_cast<const float *>(row) + e + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[c + i] = v[i];
+    }
+  }
+}
+
+// A lane's logits, neighbours in the row, -inf past the n it has.
 template <int kVpl, bool kBf16>
 __device__ __forceinline__ void load_logits(const void *row, int base, int n, bool wide,
                                             float (&z)[kVpl]) {
-  constexpr int kVec = kBf16 ? 8 : 4;  // elements of 16 bytes
-  if constexpr (kVpl % kVec == 0) {
+  constexpr int kC = chunk_of(kVpl, kBf16);
+  if constexpr (kVpl % kC == 0) {
     if (wide) {
-      const v4u *p = reinterpret_cast<const v4u *>(static_cast<const char *>(row) +
-                                                   static_cast<int64_t>(base) * (kBf16 ? 2 : 4));
-      v4u v[kVpl / kVec];
 #pragma unroll
-      for (int c = 0; c < kVpl / kVec; ++c) v[c] = n > 0 ? p[c] : v4u{0, 0, 0, 0};
+      for (int i = 0; i < kVpl; ++i) z[i] = -kInf;
+      if (n > 0) {
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) {
-        const uint32_t w = v[i / kVec][kBf16 ? i % kVec / 2 : i % kVec];
-        z[i] = n <= 0 ? -kInf : !kBf16 ? __uint_as_float(w) : i % 2 ? bf16_at_high(w) : bf16_at_low(w);
+        for (int c = 0; c < kVpl; c += kC) load_chunk<kC, kBf16>(row, base + c, z + c);
       }
       return;
     }
@@ -505,22 +522,66 @@ struct RouteGradArgs {
   const int32_t *topk;
   const float *dgate, *coef, *dloss;
   int32_t E, k, sigmoid, renorm;
-  int32_t wide, wide_coef;  // lanes have kVpl experts or none, in aligned 16 bytes
+  int32_t wide, wide_coef;  // aligned chunks, the last one whole
   float scale;
   int32_t *status;
 };
 
-// Lane l of a token's 16 or 64 holds experts l * kVpl ..  With w the balance loss's
-// gradient by p and d the gates' by the chosen scores' logits:
+// The lanes of a token take chunks of its experts in turn, so that a load or store of
+// theirs is of neighbouring bytes (no order among the experts matters here): element i
+// of lane l is expert at(i).  `past` where there is none.
+constexpr int spread_chunk(int lanes, int vpl, bool bf16) {
+  return lanes == kWave && vpl % 8 == 0 && bf16 ? 8 : 4;
+}
+template <int kLanes, int kC>
+__device__ __forceinline__ int spread_at(int i) {
+  return (i / kC * kLanes + lane_id() % kLanes) * kC + i % kC;
+}
+template <int kLanes, int kVpl, int kC, bool kBf16>
+__device__ __forceinline__ void load_spread(const void *row, int E, bool wide, float past,
+                                            float (&z)[kVpl]) {
+#pragma unroll
+  for (int c = 0; c < kVpl; c += kC) {
+    const int e = spread_at<kLanes, kC>(c);
+#pragma unroll
+    for (int i = 0; i < kC; ++i) z[c + i] = past;
+    if (wide) {
+      if (e < E) load_chunk<kC, kBf16>(row, e, z + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kC; ++i)
+        if (e + i < E) z[c + i] = load_logit<kBf16>(row, e + i);
+    }
+  }
+}
+
+// Sum over a token's experts of chunk sums s, in an order that is the same with 16 lanes
+// and with 64 for up to 256 experts in chunks of 4: chunks 16 apart first, then the
+// lanes of a row.  So a token's gradient does not depend on how many others there are.
+template <int kLanes, int n>
+__device__ __forceinline__ float spread_sum(float (&s)[n]) {
+  static_assert(n <= 4);
+#pragma unroll
+  for (int c = 1; c < n; c += 2) s[c - 1] += s[c];
+  float v = n > 2 ? s[0] + s[2] : s[0];
+  if (kLanes == kWave) {
+    const v2u r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r.x) + __uint_as_float(r.y);
+    const v2u h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(h.x) + __uint_as_float(h.y);
+  }
+  return lanes_sum<16>(v);
+}
+
+// With w the balance loss's gradient by p and d the gates' by the chosen scores' logits:
 //   softmax  dz = p (w - <w, p>) + d,  sigmoid  dz = p (1 - s) (w - <w, p>) + d
 // and without renorm a softmax gate is a p of its own, so scale * dgate joins w.
 template <int kLanes, int kVpl, bool kBf16>
 __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
   constexpr int kTok = kWave / kLanes, kParts = kRtWaves * kTok, kSlots = kLanes * kVpl;
+  constexpr int kC = spread_chunk(kLanes, kVpl, kBf16);
   __shared__ __align__(16) float s_d[kParts * kSlots];  // a token's d, by expert
   const int wave = threadIdx.x / kWave, l = lane_id() % kLanes, part = threadIdx.x / kLanes;
-  const int base = l * kVpl;
-  const int n_mine = min(max(a.E - base, 0), kVpl);
   const float dloss = a.dloss ? *a.dloss : 1.f;
   float *d_row = s_d + part * kSlots;
   for (int64_t tw = static_cast<int64_t>(blockIdx.x) * kParts + wave * kTok; tw < a.T;
@@ -531,10 +592,10 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     const char *row = static_cast<const char *>(a.logits) + at;
     char *out = static_cast<char *>(a.dlogits) + at;
     float z[kVpl], w[kVpl] = {};
-    load_logits<kVpl, kBf16>(row, base, n_mine, a.wide, z);
+    load_spread<kLanes, kVpl, kC, kBf16>(row, a.E, a.wide, -kInf, z);
     if (a.coef) {
       const float *coef = a.coef + (here ? t : tw) / a.seq * a.E;
-      load_logits<kVpl, false>(coef, base, n_mine, a.wide_coef, w);
+      load_spread<kLanes, kVpl, kC, false>(coef, a.E, a.wide_coef, 0.f, w);
     }
     bool on = here && (!a.mask || a.mask[t] != 0);
     int id = -1;
@@ -555,7 +616,7 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     for (int i = 0; i < kVpl; ++i) {
       top = larger(top, z[i]);
       sum_z = fmaf(z[i], 0x1p-12f, sum_z);
-      w[i] = i < n_mine ? w[i] * dloss : 0.f;
+      w[i] *= dloss;
     }
     if (mine<kLanes>(ballot(!(sum_z < kInf))) && on) {
       if (l == 0) report(a.status, ULTRAEP_EDATA);
@@ -584,64 +645,65 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     wave_sync();
     const bool joins_w = !a.sigmoid && !a.renorm;
 
-    const float c = !on ? 0.f : a.sigmoid ? fminf(top, 0.f) : top;
-    const bool low = ballot(on && a.sigmoid && top < -60.f);
-    float p[kVpl], s[kVpl], sum = 0.f;
+    // (1 - s is 1 where all scores are so low that only their ratios can be told)
+    const bool low = on && a.sigmoid && top < -60.f;
+    const float c = on ? top : 0.f;
+    float p[kVpl], sum[kVpl / kC] = {};
+    if (a.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < kVpl; ++i) {
-      if (a.sigmoid) {
-        s[i] = sigmoid(z[i]);
-        p[i] = low ? sigmoid_over(z[i], c) : s[i];
-      } else {
-        p[i] = fast_exp(z[i] - c);
-      }
-      sum += p[i];
-    }
-    const float inv = fast_rcp(lanes_sum<kLanes>(sum));
-    float dd[kVpl], dot = 0.f;
+      for (int i = 0; i < kVpl; ++i) p[i] = sigmoid(z[i]);
+      if (ballot(low)) {
 #pragma unroll
-    for (int i = 0; i < kVpl; ++i) {
-      dd[i] = d_row[base + i];
-      if (joins_w) {
-        w[i] += dd[i];
-        dd[i] = 0.f;
+        for (int i = 0; i < kVpl; ++i) p[i] = low ? sigmoid_over(z[i], c) : p[i];
       }
-      p[i] *= inv;
-      dot += w[i] * p[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) p[i] = fast_exp(z[i] - c);
     }
-    dot = lanes_sum<kLanes>(dot);
+#pragma unroll
+    for (int i = 0; i < kVpl; ++i) sum[i / kC] += p[i];
+    const float inv = fast_rcp(spread_sum<kLanes>(sum));
+    const float own = low ? 0.f : -1.f;  // -s is own * p
+    if (joins_w) {
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) w[i] += d_row[spread_at<kLanes, kC>(i)];
+    }
+    float dots[kVpl / kC] = {};
+#pragma unroll
+    for (int i = 0; i < kVpl; ++i) dots[i / kC] = fmaf(w[i], p[i] * inv, dots[i / kC]);
+    const float dot = spread_sum<kLanes>(dots);
     float dz[kVpl];
 #pragma unroll
     for (int i = 0; i < kVpl; ++i) {
-      float v = p[i] * (w[i] - dot);
-      if (a.sigmoid) v *= 1.f - s[i];
-      dz[i] = on && z[i] > -kInf ? dd[i] + v : 0.f;
+      const float of = joins_w ? 0.f : d_row[spread_at<kLanes, kC>(i)];
+      const float v = p[i] * inv * (a.sigmoid ? fmaf(own, p[i], 1.f) : 1.f);
+      dz[i] = on ? fmaf(v, w[i] - dot, of) : 0.f;
     }
     wave_sync();
     if (!here) continue;
-    if constexpr (kVpl % (kBf16 ? 8 : 4) == 0) {
-      if (a.wide) {
-        if (n_mine > 0) {
-          v4u *o = reinterpret_cast<v4u *>(out + base * (kBf16 ? 2 : 4));
 #pragma unroll
-          for (int i = 0; i < kVpl; i += kBf16 ? 8 : 4) {
-            if (kBf16)
-              *o++ = v4u{pack_bf16(dz[i], dz[i + 1]), pack_bf16(dz[i + 2], dz[i + 3]),
-                         pack_bf16(dz[(i + 4) % kVpl], dz[(i + 5) % kVpl]),
-                         pack_bf16(dz[(i + 6) % kVpl], dz[(i + 7) % kVpl])};
-            else
-              *o++ = __builtin_bit_cast(v4u, v4f{dz[i], dz[i + 1], dz[i + 2], dz[i + 3]});
-          }
+    for (int c = 0; c < kVpl; c += kC) {
+      const int e = spread_at<kLanes, kC>(c);
+      if (a.wide) {
+        if (e >= a.E) continue;
+        if constexpr (kBf16) {
+          typedef uint32_t raw __attribute__((ext_vector_type(kC / 2)));
+          raw o;
+#pragma unroll
+          for (int i = 0; i < kC / 2; ++i) o[i] = pack_bf16(dz[c + 2 * i], dz[c + 2 * i + 1]);
+          *reinterpret_cast<raw *>(out + e * 2) = o;
+        } else {
+          *reinterpret_cast<v4f *>(out + e * 4) = v4f{dz[c], dz[c + 1], dz[c + 2], dz[c + 3]};
         }
-        continue;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+          if (e + i >= a.E) continue;
+          if (kBf16) reinterpret_cast<uint16_t *>(out)[e + i] = static_cast<uint16_t>(round_bf16(dz[c + i]));
+          else reinterpret_cast<float *>(out)[e + i] = dz[c + i];
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < kVpl; ++i)
-      if (i < n_mine) {
-        if (kBf16) reinterpret_cast<uint16_t *>(out)[base + i] = static_cast<uint16_t>(round_bf16(dz[i]));
-        else reinterpret_cast<float *>(out)[base + i] = dz[i];
-      }
   }
 }
 
@@ -707,10 +769,11 @@ hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
   if (lanes == 16) vpl = vpl <= 16 ? (vpl + 3) / 4 * 4 : (vpl + 7) / 8 * 8;
   else vpl = vpl <= 1 ? 1 : 1 << (32 - __builtin_clz(vpl - 1));
   const int esize = type == ULTRAEP_BF16 ? 2 : 4;
-  const bool wide = gsz == group_lanes * vpl && vpl * esize % 16 == 0 && ld * esize % 16 == 0 &&
-                    (reinterpret_cast<uintptr_t>(logits) & 15u) == 0;
-  const bool wide_bias = gsz == group_lanes * vpl && vpl % 4 == 0 &&
-                         (reinterpret_cast<uintptr_t>(bias) & 15u) == 0;
+  const int chunk = chunk_of(vpl, type == ULTRAEP_BF16);
+  const bool full = gsz % vpl == 0;
+  const bool wide = full && vpl % chunk == 0 && ld % chunk == 0 &&
+                    reinterpret_cast<uintptr_t>(logits) % (chunk * esize) == 0;
+  const bool wide_bias = full && vpl % 4 == 0 && reinterpret_cast<uintptr_t>(bias) % 16 == 0;
   int pick_lanes = 16;
   while (n_group > 1 && pick_lanes * r.top_group > 16) pick_lanes /= 2;
   int pick = 0;
@@ -767,18 +830,25 @@ hipError_t launch_route_grad(const void *logits, int32_t type, int64_t T, int64_
                              const float *dgate, const float *coef, const float *dloss,
                              void *dlogits, int32_t *status, hipStream_t stream) {
   const RouteShape s = route_shape(T, r);
-  const int lanes = r.E <= 512 && r.k <= 16 ? 16 : kWave;
+  // A wave a token for many experts or few tokens, where it shortens the chain; else its
+  // idle lanes and its sums over 64 lanes cost more.  us with 16 and 64 lanes, fp32:
+  //   E = 256: T = 1 5.3 and 3.6, 3000 6.5 and 5.0, 6144 7.2 and 6.2, 8192 7.8 and 7.8, 16384
+  //   11.0 and 12.1, 65536 35 and 38 (bf16 30 and 36); E = 128: 512 4.7 and 4.2, 3000 4.8 and
+  //   4.8, 6144 5.2 and 5.9, 16384 6.5 and 10.7; E = 384: 16384 19 and 17, 65536 66 and 54;
+  //   E = 512: 2048 10.1 and 5.3, 16384 27 and 19, 65536 103 and 63
+  // (16 lanes of neighbouring experts, whose loads lie 16 to 64 bytes apart, take 16 us at
+  // 16384 x 256 and 12.3 at 16384 x 192 in bf16, where chunks in turn take 11.0 and 7.1.)
+  const int lanes = r.E > 256 || r.k > 16 || T <= (r.E > 128 ? 6144 : 2048) ? kWave : 16;
   int vpl = (r.E + lanes - 1) / lanes;
-  vpl = lanes == 16 ? (vpl <= 16 ? (vpl + 3) / 4 * 4 : (vpl + 7) / 8 * 8) : vpl <= 8 ? 8 : 16;
-  const int esize = type == ULTRAEP_BF16 ? 2 : 4;
-  auto wide = [&](const void *p, int es, int64_t pitch) {
-    return r.E % vpl == 0 && vpl * es % 16 == 0 && pitch * es % 16 == 0 &&
-           (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+  vpl = lanes == 16 ? (vpl + 3) / 4 * 4 : vpl <= 4 ? 4 : vpl <= 8 ? 8 : 16;
+  const int esize = type == ULTRAEP_BF16 ? 2 : 4, chunk = spread_chunk(lanes, vpl, type == ULTRAEP_BF16);
+  auto wide = [&](const void *p, int bytes, int64_t pitch) {
+    return r.E % chunk == 0 && pitch % chunk == 0 && reinterpret_cast<uintptr_t>(p) % bytes == 0;
   };
   const RouteGradArgs a{logits, dlogits, T, ld, s.seq, mask, topk, dgate, coef, dloss, r.E, r.k,
                         r.score == ULTRAEP_SIGMOID, r.renorm,
-                        wide(logits, esize, ld) && wide(dlogits, esize, ld), wide(coef, 4, r.E),
-                        r.scale, status};
+                        wide(logits, chunk * esize, ld) && wide(dlogits, chunk * esize, ld),
+                        wide(coef, 16, r.E), r.scale, status};
   const int64_t parts = kRtThreads / lanes, wg = (T + parts - 1) / parts;
   const dim3 grid(static_cast<unsigned>(wg < 1 << 16 ? wg : 1 << 16));
 #define UEP_CASE(m, n)                                                                             \
@@ -789,8 +859,8 @@ hipError_t launch_route_grad(const void *logits, int32_t type, int64_t T, int64_
       hipLaunchKernelGGL((k_route_grad<m, n, false>), grid, dim3(kRtThreads), 0, stream, a);       \
     return hipGetLastError();                                                                      \
   }
-  UEP_CASE(16, 4) UEP_CASE(16, 8) UEP_CASE(16, 12) UEP_CASE(16, 16) UEP_CASE(16, 24)
-  UEP_CASE(16, 32) UEP_CASE(64, 8) UEP_CASE(64, 16)
+  UEP_CASE(16, 4) UEP_CASE(16, 8) UEP_CASE(16, 12) UEP_CASE(16, 16) UEP_CASE(64, 4)
+  UEP_CASE(64, 8) UEP_CASE(64, 16)
 #undef UEP_CASE
   return hipErrorInvalidValue;
 }

@@ -171,6 +171,52 @@ def test_route_loss_and_gradient(case):
         assert (np.abs(got[t, :E] - want) <= tol).all(), t
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("score,renorm", [("softmax", True), ("softmax", False), ("sigmoid", True)])
+@pytest.mark.parametrize("E,k,T,ld", [(3, 2, 2100, None), (16, 4, 2051, 20), (60, 4, 2100, None), (72, 6, 2500, 73),
+                                      (96, 12, 2049, 96), (127, 8, 2100, 128), (128, 16, 4001, None), (136, 8, 6150, None),
+                                      (192, 8, 6200, 200), (250, 5, 6145, None), (256, 8, 6200, 260)])
+def test_gradient_of_many_tokens(E, k, T, ld, score, renorm, bf16):
+    """Several tokens a wave: some masked, without ids, or of dead or very low logits."""
+    rng = np.random.default_rng(E + T)
+    r = router(E=E, k=k, score=score, renorm=renorm, scale=0.7, seq_len=1000)
+    z = logits(rng, T, E, bf16, dead=0.05)
+    look = np.unique(np.concatenate([[0, 1, 2, 3, T - 1], rng.integers(0, T, 40)]))
+    z[look[5]] = -np.inf
+    z[look[6::9]] = p64.bf16(z[look[6::9]] - 128)
+    mask = rng.random(T) > 0.1
+    ids = np.argsort(rng.random((T, E)), axis=1)[:, :k].astype(np.int32)
+    few = rng.integers(0, k + 1, T)
+    ids[np.arange(k) >= few[:, None]] = -1
+    rows = np.full((T, ld or E), np.nan, np.float32)
+    rows[:, :E] = z
+    lg = dev(p64.bf16_bits(rows).view(np.int16)) if bf16 else dev(rows)
+    dg = rng.standard_normal((T, k)).astype(np.float32)
+    w = (10 * rng.standard_normal((-(-T // 1000), E))).astype(np.float32)
+    rt = uep.Router(E, k, int(score == "sigmoid"), renorm, scale=0.7, seq_len=1000)
+    out, st = torch.full_like(lg, 5), torch.zeros(1, dtype=torch.int32, device="cuda")
+    uep.ultraep_route_grad(lg, T, ld or E, rt, dev(mask.astype(np.uint8)), dev(ids), dev(dg), dev(w), None, out, st)
+    assert int(st.item()) == 0
+    got = out.cpu().numpy()
+    assert (got[:, E:] == 5).all()
+    if bf16:
+        got = p64.from_bits(got.view(np.uint16))
+    # a few of them on their own: the same bits
+    some, one = torch.from_numpy(look).cuda(), torch.full_like(lg[:len(look)], 5)
+    rt.seq_len = 1
+    uep.ultraep_route_grad(lg[some].contiguous(), len(look), ld or E, rt, dev(mask[look].astype(np.uint8)), dev(ids[look]),
+                           dev(dg[look]), dev(w[look // 1000]), None, one, st)
+    assert torch.equal(one.view(torch.int16), out[some].view(torch.int16)) and int(st.item()) == 0
+    for t in look:
+        if not mask[t] or few[t] == 0 or np.isneginf(z[t]).all():
+            assert (got[t, :E] == 0).all(), t
+            continue
+        want, mag = p64.route_grad(z[t].astype(np.float64), ids[t], r, dg[t].astype(np.float64),
+                                   w[t // 1000].astype(np.float64))
+        tol = 2 * SCORE_U * mag + 1e-37 + (1.01 * p64.U16 * np.abs(want) if bf16 else 0)
+        assert (np.abs(got[t, :E] - want) <= tol).all(), t
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [True, False])
 def test_gradient_against_differences(score, renorm):
