@@ -71,9 +71,13 @@ __device__ __forceinline__ float readlane_f(float v, int l) {
 // Reductions over rows of 16 lanes (DPP mirrors) or over the 64 of a wave (the rows'
 // results in order), each in one fixed order.  Every lane must be active.
 template <int kCtrl>
-__device__ __forceinline__ float dpp_f(float v) {
+__device__ __forceinline__ int dpp_i(int v) {
   // (each control used reads a lane of the row for every lane)
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kCtrl, 0xF, 0xF, true));
+  return __builtin_amdgcn_mov_dpp(v, kCtrl, 0xF, 0xF, true);
+}
+template <int kCtrl>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __int_as_float(dpp_i<kCtrl>(__float_as_int(v)));
 }
 template <int kLanes>
 __device__ __forceinline__ float lanes_sum(float v) {

@@ -10,7 +10,7 @@
 //
 // A call reads little (4096 tokens of 256 experts: 4 MB), so instructions and the
 // chain of loads bound it, and launches: ids, gates and statistics of those 4096
-// tokens, by groups, take 8.8 us, their sums over the workgroups 2.6, the loss 2.4, the
+// tokens, by groups, take 8.2 us, their sums over the workgroups 2.6, the loss 2.4, the
 // gradient 4.7; 16384 tokens of 128 experts 9.4, 4.0, 2.2; one token of 256 4.6.
 #include "operators.hpp"
 
@@ -314,16 +314,33 @@ k_route(RouteArgs a) {
         m2 = __builtin_amdgcn_fmed3f(m1, m2, key[i]);
         m1 = larger(m1, key[i]);
       }
-      for (int d = 1; d < a.group_lanes; d *= 2)
+      if (a.group_lanes > 1) merge_two(m1, m2, dpp_f<0xB1>(m1), dpp_f<0xB1>(m2));
+      if (a.group_lanes > 2) merge_two(m1, m2, dpp_f<0x4E>(m1), dpp_f<0x4E>(m2));
+      if (a.group_lanes > 4) merge_two(m1, m2, dpp_f<0x141>(m1), dpp_f<0x141>(m2));
+      if (a.group_lanes > 8) merge_two(m1, m2, dpp_f<0x140>(m1), dpp_f<0x140>(m2));
+      for (int d = 16; d < a.group_lanes; d *= 2)
         merge_two(m1, m2, __shfl_xor(m1, d), __shfl_xor(m2, d));
       const float score = m1 + m2;
-      int before = 0;  // groups ahead of this lane's
-      for (int g = 0; g < a.n_group; ++g) {
-        const float o = kLanes == kWave ? readlane_f(score, g * a.group_lanes)
-                                        : __shfl(score, g * a.group_lanes, kLanes);
-        before += o > score || (o == score && g < group);
+      int before = 0, top = a.top_group;  // groups ahead of this lane's
+      if constexpr (kLanes == 16) {
+        // their lanes: of a larger score, or of the same one and in front of this group
+        const int mine = order_of(group < a.n_group ? score : -kInf);
+        int at = l;  // (not 15 of the comparisons below held throughout the loop)
+        asm volatile("" : "+v"(at));
+#define UEP_TURN(i) before += dpp_i<0x120 + i>(mine) >= mine + (at < i);  // row_ror
+        UEP_TURN(1) UEP_TURN(2) UEP_TURN(3) UEP_TURN(4) UEP_TURN(5) UEP_TURN(6) UEP_TURN(7)
+        UEP_TURN(8) UEP_TURN(9) UEP_TURN(10) UEP_TURN(11) UEP_TURN(12) UEP_TURN(13) UEP_TURN(14)
+        UEP_TURN(15)
+#undef UEP_TURN
+        before -= sub;
+        top *= a.group_lanes;
+      } else {
+        for (int g = 0; g < a.n_group; ++g) {
+          const float o = readlane_f(score, g * a.group_lanes);
+          before += o > score || (o == score && g < group);
+        }
       }
-      keep = keep && group < a.n_group && before < a.top_group;
+      keep = keep && group < a.n_group && before < top;
     }
 
     int *slots = &s_slots[wave][lane_id() - l];
