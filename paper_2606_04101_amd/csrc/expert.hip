@@ -780,19 +780,19 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
   //   Times in tenths of a round of 256 x 256: 4 for the round of its quarters, 6 for a
   // round of 128 x 128, two tiles a compute unit.
   //   Measured, us (256 x 256 / 128 x 128 / 128 x 64 / thin 64 / 32 / 16):
-  //   10 blocks, N = 4096, K = 7168, act: M = 20480 584 / 646, 10240 326 / 354, 9216 317 /
-  //   309, 8192 300 / 299 / 408 / 454 / 561 / 808, 6144 213 / 246, 5120 215 / 194, 3328 156 /
-  //   138, 2048 112 / 128 / 156 / 152 / 182 / 250, 1024 105 / 81 / 112 / 100 / 118 / 148,
-  //   512 102 / 76 / 71 / 76 / 83 / 96, 256 101 / 69 / 69 / 66 / 65 / 68, 64 98 / 67 / 65
+  //   10 blocks, N = 4096, K = 7168, act: M = 20480 590 / 646, 10240 323 / 355, 9216 315 /
+  //   311, 8192 303 / 298 / 351 / 454 / 561 / 808, 6144 219 / 245, 5120 212 / 190, 3328 156 /
+  //   140, 2048 109 / 127 / 139 / 152 / 182 / 250, 1024 103 / 79 / 89 / 100 / 118 / 148,
+  //   512 102 / 74 / 71 / 76 / 83 / 96, 256 103 / 70 / 68 / 66 / 65 / 68, 64 98 / 67 / 65
   //   / 64 / 58 / 51
-  //   1 block, the same: M = 8704 246 / 291, 8192 207 / 237, 6144 204 / 177, 4608 139 / 170,
-  //   4096 105 / 119 / 163 / 204, 2048 89 / 62, 1024 78 / 44 / 44 / 53 / 70, 256
-  //   79 / 38 / 34 / 18 / 22 / 26, 128 79 / 38 / 34 / 17 / 13 / 17, 16 78 / 37 / 34 / 16 / 11 / 9
-  //   64 blocks, N = 1024, K = 2048: M = 8192 45 / 51 / 56 / 64, 4096 40 / 29 / 40 / 44,
-  //   1024 34 / 25 / 25 / 30 / 29 / 28
-  //   6 blocks, N = 4096, K = 1408: M = 20480 154 / 171, 8192 69 / 76 / 99, 5120 53 / 45, 512
-  //   24 / 15 / 13 / 18 / 18 / 19, 256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11 / 11 / 11
-  //   / 10
+  //   1 block, the same: M = 8704 235 / 277, 8192 199 / 231, 6144 198 / 173, 4608 135 / 165,
+  //   4096 102 / 116 / 159 / 204, 2048 79 / 60, 1024 75 / 43 / 50 / 53 / 70, 256
+  //   75 / 37 / 34 / 18 / 22 / 26, 128 79 / 38 / 34 / 17 / 13 / 17, 16 78 / 37 / 34 / 16 / 11 / 9
+  //   64 blocks, N = 1024, K = 2048: M = 8704 56 / 49, 8192 40 / 50 / 49 / 64, 4608 39 / 42, 4096
+  //   38 / 29 / 33 / 44, 1024 37 / 25 / 29 / 30 / 29 / 28
+  //   6 blocks, N = 4096, K = 1408: M = 20480 138 / 144, 8704 75 / 70, 8192 61 / 67 / 77, 5120
+  //   50 / 44, 512 24 / 14 / 13 / 18 / 18 / 19, 256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11
+  //   / 11 / 11 / 10
   const int64_t blocks = M < n_block ? M : n_block, rows = (M + blocks - 1) / blocks;
   auto items = [&](int64_t tile_rows, int64_t channels) {
     return (blocks > 1 ? M / tile_rows + (blocks + 1) / 2 : (M + tile_rows - 1) / tile_rows) *
@@ -802,7 +802,7 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
   const int64_t big_time = full * 10 + (last == 0 ? 0 : full && last <= 64 ? 4 : 10);
   const int64_t mid_time = (items(128, 128) + 511) / 512 * 6;
   const bool deep = K >= 4096;  // four waves' worth of steps
-  if (rows > 96 && big_time < mid_time)
+  if (rows > 64 && big_time < mid_time)
     start_matmul<256, 256, 2, 2, true>(a, act, bf16, 256, stream);
   else if (rows > 56 && items(128, 128) >= 256)
     start_matmul<128, 128, 2, 2, false>(a, act, bf16, 512, stream);
