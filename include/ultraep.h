@@ -394,7 +394,8 @@ typedef struct {
  *   prob_sum  [n_seg][E] fp32: sum over tokens of p = s / (sum of all E s)
  *             (softmax: p = s)
  *   tokens    [n_seg] int32: tokens that have an id
- *   ws        workspace of ws_bytes >= ultraep_route_ws_bytes, 4-byte aligned
+ *   ws        workspace of ws_bytes >= ultraep_route_ws_bytes for this T or a
+ *             larger one, 4-byte aligned
  *             (may be null without statistics)
  * Sums run in one fixed order for given T and router: equal calls give equal
  * bits.  T <= 2^23. */
@@ -404,8 +405,9 @@ int ultraep_route(const void *logits, int32_t type, int64_t T, int64_t ld,
                   int32_t *tokens, void *ws, size_t ws_bytes, int32_t *status,
                   hipStream_t stream);
 
-/* Bytes of device workspace that ultraep_route needs for its statistics (host
- * only; 0 for unsupported arguments, at least 4 otherwise). */
+/* Bytes of device workspace that ultraep_route needs for its statistics with up
+ * to T tokens, so one workspace does for the largest batch and all smaller ones
+ * (host only; 0 for unsupported arguments, at least 4 otherwise). */
 size_t ultraep_route_ws_bytes(int64_t T, const ultraep_router *r);
 
 /* Balance loss over n_seg sequences: with c, F = counts, load_tokens (this

@@ -54,7 +54,7 @@ int ultraep_route(const void *logits, int32_t type, int64_t T, int64_t ld,
   if (T > 0 && (!topk || !gate)) return ULTRAEP_EINVAL;
   const bool stats = counts != nullptr;
   if (stats != (prob_sum != nullptr) || stats != (tokens != nullptr)) return ULTRAEP_EINVAL;
-  if (stats && (!ws || !aligned4(ws) || ws_bytes < uep::route_ws_bytes(T, *r)))
+  if (stats && (!ws || !aligned4(ws) || ws_bytes < uep::route_ws_need(T, *r)))
     return ULTRAEP_EINVAL;
   if (T == 0 && !stats) return ULTRAEP_OK;
   return rc(uep::launch_route(logits, type, T, ld, *r, bias, mask, topk, gate, counts, prob_sum,

@@ -19,7 +19,8 @@ struct RouteShape {
   int64_t n_chunk;  // workgroups of a sequence
 };
 RouteShape route_shape(int64_t T, const ultraep_router &r);
-size_t route_ws_bytes(int64_t T, const ultraep_router &r);
+size_t route_ws_need(int64_t T, const ultraep_router &r);   // of a call of T tokens
+size_t route_ws_bytes(int64_t T, const ultraep_router &r);  // of any of up to T
 
 hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
                         const ultraep_router &r, const float *bias, const uint8_t *mask,

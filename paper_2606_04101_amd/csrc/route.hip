@@ -724,26 +724,45 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
   }
 }
 
+constexpr int64_t kRtChunk = 16;  // a workgroup's tokens are a multiple of it
+static int64_t route_wg(const ultraep_router &r) { return r.E > 64 ? 512 : 1024; }
+
 RouteShape route_shape(int64_t T, const ultraep_router &r) {
   RouteShape s;
-  s.seq = r.seq_len > 0 ? r.seq_len : (T > 0 ? T : 1);
-  if (s.seq > T && T > 0) s.seq = T;
+  s.seq = r.seq_len > 0 && r.seq_len < T ? r.seq_len : T > 0 ? T : 1;
   s.n_seg = T > 0 ? (T + s.seq - 1) / s.seq : 1;
   // Workgroups of at least 16 tokens, about as many as run at once (two a compute unit,
   // four with few experts): more make more partials, fewer take turns.  With 1024 and 512
   // of them, us with the sums and the loss: E = 256, T = 16384 26.3 and 20.9, 65536 53.9
   // and 48.7; E = 128, T = 16384 17.8 and 15.1; E = 64, T = 65536 21.7 and 26.9.
-  const int64_t n_wg = r.E > 64 ? 512 : 1024;
+  const int64_t n_wg = route_wg(r);
   s.chunk = (T + n_wg - 1) / n_wg;
-  s.chunk = s.chunk < 16 ? 16 : (s.chunk + 15) / 16 * 16;
+  s.chunk = s.chunk < kRtChunk ? kRtChunk : (s.chunk + kRtChunk - 1) / kRtChunk * kRtChunk;
   s.n_chunk = (s.seq + s.chunk - 1) / s.chunk;
   return s;
 }
 
+static size_t partial_bytes(int64_t n, const ultraep_router &r) {
+  return n > 0 ? static_cast<size_t>(n) * (2 * static_cast<size_t>(r.E) + 1) * 4 : 4;
+}
+
+size_t route_ws_need(int64_t T, const ultraep_router &r) {
+  const RouteShape s = route_shape(T, r);
+  return partial_bytes(s.n_chunk > 1 ? s.n_seg * s.n_chunk : 0, r);
+}
+
+// At least what any T' <= T needs, so that a workspace for the largest batch does for all:
+// the partials of T' alone fall where its chunk grows (E = 256: 512 at 16384 tokens, 342 at
+// 16385).  With n workgroups aimed at, a chunk c >= 16 and c >= T' / n: one sequence has at
+// most min(n, ceil(T' / 16)) chunks.  Several of L tokens, cut where c < L, are s = ceil(T' / L)
+// <= n, and s * ceil(L / c) < (T' / L + 1) (L / c + 1) <= n + 1 + T' / L + n L / T' <= 2 n + 2,
+// and at most s * ceil(L / 16).  Neither bound falls with T.
 size_t route_ws_bytes(int64_t T, const ultraep_router &r) {
   const RouteShape s = route_shape(T, r);
-  if (s.n_chunk <= 1) return 4;
-  return static_cast<size_t>(s.n_seg) * s.n_chunk * (2 * static_cast<size_t>(r.E) + 1) * 4;
+  if (s.seq <= kRtChunk) return partial_bytes(0, r);
+  const int64_t n = route_wg(r), most = s.n_seg == 1 ? n : 2 * n + 2;
+  const int64_t small = s.n_seg * ((s.seq + kRtChunk - 1) / kRtChunk);
+  return partial_bytes(small < most ? small : most, r);
 }
 
 template <bool kBf16, bool kStats>
