@@ -119,12 +119,16 @@ __device__ __forceinline__ float fast_exp(float x) {
 // 1 / x to 1 ulp, for x of ordinary size
 __device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
-// 1 / (1 + exp(-z)), without overflow for any z
-__device__ __forceinline__ float sigmoid(float z) {
-  const float e = fast_exp(-fabsf(z));
-  return (z >= 0.f ? 1.f : e) * fast_rcp(1.f + e);
+// s = 1 / (1 + exp(-z)) and 1 - s, each without overflow or cancellation for any z
+struct Sigmoid {
+  float s, rest;
+};
+__device__ __forceinline__ Sigmoid sigmoid_both(float z) {
+  const float e = fast_exp(-fabsf(z)), r = fast_rcp(1.f + e), q = e * r;
+  return z >= 0.f ? Sigmoid{r, q} : Sigmoid{q, r};
 }
-// the same over exp(c), c <= 0: of weight where sigmoid(z) itself vanishes
+__device__ __forceinline__ float sigmoid(float z) { return sigmoid_both(z).s; }
+// s over exp(c), c <= 0: of weight where sigmoid(z) itself vanishes
 __device__ __forceinline__ float sigmoid_over(float z, float c) {
   return fast_exp(fminf(z, 0.f) - c) * fast_rcp(1.f + fast_exp(-fabsf(z)));
 }

@@ -595,6 +595,8 @@ __device__ __forceinline__ float spread_sum(float (&s)[n]) {
 // and without renorm a softmax gate is a p of its own, so scale * dgate joins w.
 template <int kLanes, int kVpl, bool kBf16>
 __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
+  // (the same roundings with 16 lanes and with 64: fused only where it says so)
+#pragma clang fp contract(off)
   constexpr int kTok = kWave / kLanes, kParts = kRtWaves * kTok, kSlots = kLanes * kVpl;
   constexpr int kC = spread_chunk(kLanes, kVpl, kBf16);
   __shared__ __align__(16) float s_d[kParts * kSlots];  // a token's d, by expert
@@ -644,7 +646,8 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
 
     // the chosen: this lane's is lane l's
     const bool chosen = on && my_z > -kInf;
-    const float not_s = a.sigmoid ? 1.f - sigmoid(my_z) : 1.f;
+    const Sigmoid score = sigmoid_both(my_z);
+    const float not_s = a.sigmoid ? score.rest : 1.f;
     float d;
     if (a.renorm) {
       const float c = lanes_max<kLanes>(chosen ? (a.sigmoid ? fminf(my_z, 0.f) : my_z) : -kInf);
@@ -653,7 +656,7 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
       const float q = us > 0.f ? u * fast_rcp(us) : 0.f;
       d = q * (dg - lanes_sum<kLanes>(dg * q)) * not_s;
     } else {
-      d = a.sigmoid ? sigmoid(my_z) * not_s * dg : dg;
+      d = a.sigmoid ? score.s * not_s * dg : dg;
     }
     const float zero[kVpl] = {};
     put_lane<kVpl>(d_row, l, zero);
@@ -665,36 +668,38 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     // (1 - s is 1 where all scores are so low that only their ratios can be told)
     const bool low = on && a.sigmoid && top < -60.f;
     const float c = on ? top : 0.f;
-    float p[kVpl], sum[kVpl / kC] = {};
-    if (a.sigmoid) {
+    float p[kVpl], sum[kVpl / kC] = {}, dots[kVpl / kC] = {};
+    if (a.sigmoid) {  // p: s (1 - s) from here on
+      const bool some_low = ballot(low) != 0;
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) p[i] = sigmoid(z[i]);
-      if (ballot(low)) {
-#pragma unroll
-        for (int i = 0; i < kVpl; ++i) p[i] = low ? sigmoid_over(z[i], c) : p[i];
+      for (int i = 0; i < kVpl; ++i) {
+        const Sigmoid of = sigmoid_both(z[i]);
+        float s = of.s;
+        p[i] = of.s * of.rest;
+        if (some_low) {
+          const float over = sigmoid_over(z[i], c);
+          s = low ? over : s;
+          p[i] = low ? over : p[i];
+        }
+        sum[i / kC] += s;
+        dots[i / kC] = fmaf(w[i], s, dots[i / kC]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kVpl; ++i) p[i] = fast_exp(z[i] - c);
+      for (int i = 0; i < kVpl; ++i) {
+        p[i] = fast_exp(z[i] - c);
+        sum[i / kC] += p[i];
+        if (joins_w) w[i] += d_row[spread_at<kLanes, kC>(i)];
+        dots[i / kC] = fmaf(w[i], p[i], dots[i / kC]);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < kVpl; ++i) sum[i / kC] += p[i];
     const float inv = fast_rcp(spread_sum<kLanes>(sum));
-    const float own = low ? 0.f : -1.f;  // -s is own * p
-    if (joins_w) {
-#pragma unroll
-      for (int i = 0; i < kVpl; ++i) w[i] += d_row[spread_at<kLanes, kC>(i)];
-    }
-    float dots[kVpl / kC] = {};
-#pragma unroll
-    for (int i = 0; i < kVpl; ++i) dots[i / kC] = fmaf(w[i], p[i] * inv, dots[i / kC]);
-    const float dot = spread_sum<kLanes>(dots);
+    const float dot = spread_sum<kLanes>(dots) * inv;
     float dz[kVpl];
 #pragma unroll
     for (int i = 0; i < kVpl; ++i) {
       const float of = joins_w ? 0.f : d_row[spread_at<kLanes, kC>(i)];
-      const float v = p[i] * inv * (a.sigmoid ? fmaf(own, p[i], 1.f) : 1.f);
-      dz[i] = on ? fmaf(v, w[i] - dot, of) : 0.f;
+      dz[i] = on ? fmaf(p[i] * inv, w[i] - dot, of) : 0.f;
     }
     wave_sync();
     if (!here) continue;
