@@ -395,7 +395,7 @@ k_route(RouteArgs a) {
       }
     } else if (a.renorm) {
       const float c = lanes_max<kLanes>(my_z);
-      const float u = slot >= 0 ? fast_exp(my_z - c) : 0.f;
+      const float u = slot >= 0 ? exp_neg(my_z - c) : 0.f;
       g = u * fast_rcp(lanes_sum<kLanes>(u));
     }
     if (kStats || (!a.sigmoid && !a.renorm)) {
@@ -403,7 +403,7 @@ k_route(RouteArgs a) {
       if (!a.sigmoid) {
         c = on ? top : 0.f;
 #pragma unroll
-        for (int i = 0; i < kVpl; ++i) u[i] = fast_exp(z[i] - c);
+        for (int i = 0; i < kVpl; ++i) u[i] = exp_neg(z[i] - c);
       } else if (ballot(on && top < -60.f)) {
         c = on ? fminf(top, 0.f) : 0.f;
 #pragma unroll
@@ -421,7 +421,7 @@ k_route(RouteArgs a) {
         for (int i = 0; i < kVpl; ++i) acc[i] += on ? u[i] * inv : 0.f;
         n_tokens += on;
       }
-      if (!a.sigmoid && !a.renorm) g = slot >= 0 ? fast_exp(my_z - c) * inv : 0.f;
+      if (!a.sigmoid && !a.renorm) g = slot >= 0 ? exp_neg(my_z - c) * inv : 0.f;
     }
     if (here && l < a.k) {
       a.topk[t * a.k + l] = my_id;
@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     float d;
     if (a.renorm) {
       const float c = lanes_max<kLanes>(chosen ? (a.sigmoid ? fminf(my_z, 0.f) : my_z) : -kInf);
-      const float u = !chosen ? 0.f : a.sigmoid ? sigmoid_over(my_z, c) : fast_exp(my_z - c);
+      const float u = !chosen ? 0.f : a.sigmoid ? sigmoid_over(my_z, c) : exp_neg(my_z - c);
       const float us = lanes_sum<kLanes>(u);
       const float q = us > 0.f ? u * fast_rcp(us) : 0.f;
       d = q * (dg - lanes_sum<kLanes>(dg * q)) * not_s;
@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kRtThreads) k_route_grad(RouteGradArgs a) {
     } else {
 #pragma unroll
       for (int i = 0; i < kVpl; ++i) {
-        p[i] = fast_exp(z[i] - c);
+        p[i] = exp_neg(z[i] - c);
         sum[i / kC] += p[i];
         if (joins_w) w[i] += d_row[spread_at<kLanes, kC>(i)];
         dots[i / kC] = fmaf(w[i], p[i], dots[i / kC]);

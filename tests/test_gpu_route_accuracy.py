@@ -91,3 +91,51 @@ def test_gradient_of_high_logits(E, k, T, parts, renorm, bf16):
     tol = 2 * SCORE_U * mag + 1e-37 + (1.01 * p64.U16 * np.abs(want) if bf16 else 0)
     bad = np.abs(got - want) > tol
     assert not bad.any(), (int(bad.sum()), float((np.abs(got - want) / mag.clip(1e-300)).max() / p64.U32))
+
+
+def scores(z, score, renorm, k, st):
+    """Gates and a token's own p by the kernel: every token a sequence."""
+    T, E = z.shape
+    r = uep.Router(E, k, uep.ULTRAEP_SIGMOID if score == "sigmoid" else uep.ULTRAEP_SOFTMAX, renorm, seq_len=1)
+    i, f = torch.int32, torch.float32
+    o = [torch.empty(s, dtype=d, device="cuda") for s, d in
+         (((T, k), i), ((T, k), f), ((T, E), i), ((T, E), f), ((T,), i))]
+    ws = torch.empty(uep.ultraep_route_ws_bytes(T, r), dtype=torch.uint8, device="cuda")
+    uep.ultraep_route(dev(z), T, E, r, None, None, *o, ws, st)
+    return o[0].cpu().numpy(), o[1].cpu().numpy(), o[3].cpu().numpy()
+
+
+@pytest.mark.parametrize("E", [24, 256, 512])
+def test_sigmoid_scores_of_low_and_high_logits(E):
+    """Gates that are scores: exp within 2 ulp (4 u), 1 + exp (1 u and at most half of
+    exp's), the reciprocal 1 ulp, a product; 10 u whatever the logit."""
+    rng = np.random.default_rng(E)
+    z = rng.uniform(-80, 20, (300, E)).astype(np.float32)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    k = min(E, 64)
+    ids, gate, _ = scores(z, "sigmoid", False, k, st)
+    want = p64.sigmoid(np.take_along_axis(z, ids, 1).astype(np.float64))
+    assert int(st.item()) == 0 and (ids >= 0).all()
+    assert (np.abs(gate - want) <= 10 * p64.U32 * want).all()
+    low = np.where(rng.random((300, E)) < 0.5, z, z - np.float32(20)).clip(max=-2)  # down to -100, where exp is 0
+    ids, gate, _ = scores(low, "sigmoid", False, k, st)
+    want = p64.sigmoid(np.take_along_axis(low, ids, 1).astype(np.float64))
+    assert (np.abs(gate - want) <= 10 * p64.U32 * want + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("E", [24, 256, 512])
+def test_softmax_scores_far_below_the_largest(E):
+    """One logit 30 to 80 above the others, differences exact: the sum is 1, a score exp
+    (4 u), the reciprocal and a product (3 u); 8 u however small."""
+    rng = np.random.default_rng(E)
+    z = -rng.integers(30 * 16, 80 * 16, (300, E)).astype(np.float32) / 16
+    z[np.arange(300), rng.integers(0, E, 300)] = 0
+    z += rng.integers(-20, 20, (300, 1)).astype(np.float32)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ids, gate, p = scores(z, "softmax", False, 4, st)
+    want = np.exp(z.astype(np.float64) - z.max(1, keepdims=True))
+    want /= want.sum(1, keepdims=True)
+    assert int(st.item()) == 0
+    assert (np.abs(p - want) <= 8 * p64.U32 * want).all()
+    want = np.take_along_axis(want, ids, 1)
+    assert (np.abs(gate - want) <= 8 * p64.U32 * want).all()
