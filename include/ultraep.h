@@ -357,7 +357,8 @@ enum {
  *   top_group  contiguous groups of at least two (n_group <= 64 divides E);
  *              a group scores the sum of its two largest keys and the
  *              token's ids come from its top_group best (ties: the lower
- *              group; k <= top_group * E / n_group)
+ *              group; k <= top_group * E / n_group).  One with fewer than two
+ *              experts that can be chosen scores -inf.  1, 1 is as 0, 0
  *   scale      finite
  *   seq_len    tokens of a sequence for the statistics: token t belongs to
  *              sequence t / seq_len.  0: all T tokens are one */
@@ -376,15 +377,16 @@ typedef struct {
  * equal keys by rising id, where the key is
  *   softmax  z + bias
  *   sigmoid  s + bias; z itself where there is neither bias nor groups
- * in fp32 (bias enters the selection only).  An expert whose logit is -inf is
- * never chosen: the ids left over are -1, their gates 0.  A token that is
+ * in fp32 (bias enters the selection only).  An expert whose logit or bias is
+ * -inf is never chosen: the ids left over are -1, their gates 0.  A token that is
  * masked, or has no logit above -inf, gets ids -1 and gates 0 and counts in no
  * statistic; so does one with a NaN or +inf logit, which raises ULTRAEP_EDATA.
  * The ids are what ultraep_count and ultraep_dispatch take, the gates what
  * ultraep_combine takes, and counts (with seq_len 0) this rank's row of the
  * load matrix.
  *   logits    [T] rows of E elements of `type`, ld elements apart (E <= ld <= 2^20)
- *   bias      [E] fp32, or null
+ *   bias      [E] fp32, or null.  +inf is as the largest finite number; a NaN
+ *             raises ULTRAEP_EDATA, and its expert is not chosen
  *   mask      [T] bytes, 0 = masked; or null
  *   topk      [T][k] int32
  *   gate      [T][k] fp32

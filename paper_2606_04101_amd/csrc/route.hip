@@ -257,8 +257,22 @@ k_route(RouteArgs a) {
   float bias[kVpl] = {};
   if (a.bias) {
     load_logits<kVpl, false>(a.bias, base, n_mine, a.wide_bias, bias);
+    float odd = 0.f;  // a NaN if a bias is no finite number
 #pragma unroll
-    for (int i = 0; i < kVpl; ++i) bias[i] = i < n_mine ? bias[i] : 0.f;
+    for (int i = 0; i < kVpl; ++i) {
+      bias[i] = i < n_mine ? bias[i] : 0.f;
+      odd = fmaf(bias[i], 0.f, odd);
+    }
+    if (ballot(odd != 0.f)) {  // no key is to be a NaN, also where +inf meets a logit of -inf
+      bool nan = false;
+#pragma unroll
+      for (int i = 0; i < kVpl; ++i) {
+        const bool bad = bias[i] != bias[i];
+        nan |= bad;
+        bias[i] = bad ? -kInf : fminf(bias[i], __FLT_MAX__);
+      }
+      if (nan && blockIdx.x == 0) report(a.status, ULTRAEP_EDATA);
+    }
   }
   float acc[kVpl] = {};
   int n_tokens = 0;
@@ -320,7 +334,7 @@ k_route(RouteArgs a) {
       if (a.group_lanes > 8) merge_two(m1, m2, dpp_f<0x140>(m1), dpp_f<0x140>(m2));
       for (int d = 16; d < a.group_lanes; d *= 2)
         merge_two(m1, m2, __shfl_xor(m1, d), __shfl_xor(m2, d));
-      const float score = m1 + m2;
+      const float score = m2 > -kInf ? m1 + m2 : -kInf;  // (-inf, not a NaN, of +inf alone)
       int before = 0, top = a.top_group;  // groups ahead of this lane's
       if constexpr (kLanes == 16) {
         // their lanes: of a larger score, or of the same one and in front of this group
