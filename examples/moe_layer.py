@@ -24,7 +24,9 @@ DEV, BF16, F32, I32, I64 = "cuda", torch.bfloat16, torch.float32, torch.int32, t
 
 
 class Layer:
-    """The plan's buffers and what a step writes, made once."""
+    """The plan's buffers and workspaces, made once, and what the latest forward pass
+    left: new tensors each time, since earlier ones may still wait for their backward
+    pass (whose functions hold on to theirs)."""
 
     def __init__(self, R, E, n_slot, k, T, H, F, seq_len=0, score=uep.ULTRAEP_SOFTMAX, seed=0):
         self.T, self.k, self.H, self.F, self.E = T, k, H, F, E
@@ -36,21 +38,26 @@ class Layer:
         other = torch.rand(R, E, device=DEV, generator=gen) + 0.5
         self.load = (other / other.sum(1, keepdim=True) * T * k).to(I32)  # the other ranks' rows
         self.gen = gen
-        n = self.r.n_seg(T)
-        self.n_seg = n
+        self.n_seg = self.r.n_seg(T)
+        self.route_ws = self.empty(torch.uint8, uep.ultraep_route_ws_bytes(T, self.r))
+        self.ws = self.empty(torch.uint8, uep.ultraep_dispatch_ws_bytes(T, k, self.g))
 
-        def empty(dtype, *shape):
-            return torch.empty(*shape, dtype=dtype, device=DEV)
-        self.topk, self.gate = empty(I32, T, k), empty(F32, T, k)
-        self.counts, self.prob_sum = empty(I32, n, E), empty(F32, n, E)
-        self.tokens, self.coef = empty(I32, n), empty(F32, n, E)
-        self.route_ws = empty(torch.uint8, uep.ultraep_route_ws_bytes(T, self.r))
-        self.rows, self.off = empty(I32, T * k), empty(I64, R * self.g.S + 1)
-        self.ws = empty(torch.uint8, uep.ultraep_dispatch_ws_bytes(T, k, self.g))
+    def empty(self, dtype, *shape):
+        return torch.empty(*shape, dtype=dtype, device=DEV)
+
+    def route(self, logits):
+        """Ids, gates and statistics of a microbatch."""
+        n, E, T, k = self.n_seg, self.E, self.T, self.k
+        self.topk, self.gate = self.empty(I32, T, k), self.empty(F32, T, k)
+        self.counts, self.prob_sum = self.empty(I32, n, E), self.empty(F32, n, E)
+        self.tokens = self.empty(I32, n)
+        uep.ultraep_route(logits, T, E, self.r, None, None, self.topk, self.gate, self.counts, self.prob_sum,
+                          self.tokens, self.route_ws, self.status)
 
     def make_plan(self, rank=0):
         """The load matrix's row of this rank is the router's counts (summed over its
         sequences); then the plan and the dispatch's layout."""
+        self.rows, self.off = self.empty(I32, self.T * self.k), self.empty(I64, self.g.R * self.g.S + 1)
         torch.sum(self.counts, 0, dtype=I32, out=self.load[rank])
         uep.ultraep_plan(self.load, self.g, self.plan)
         uep.ultraep_dispatch_layout(self.topk, self.T, self.k, rank, self.g, self.plan, self.rows, self.off, self.ws,
@@ -72,18 +79,19 @@ class Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, layer, alpha):
         m, loss = layer, torch.empty(1, device=DEV)
-        uep.ultraep_route(logits, m.T, m.E, m.r, None, None, m.topk, m.gate, m.counts, m.prob_sum, m.tokens,
-                          m.route_ws, m.status)
-        uep.ultraep_balance_loss(m.counts, m.tokens, m.prob_sum, m.tokens, m.n_seg, m.r, alpha, loss, m.coef)
-        ctx.save_for_backward(logits)
+        m.route(logits)
+        coef = m.empty(F32, m.n_seg, m.E)
+        uep.ultraep_balance_loss(m.counts, m.tokens, m.prob_sum, m.tokens, m.n_seg, m.r, alpha, loss, coef)
+        ctx.save_for_backward(logits, m.topk, coef)
         ctx.layer = m
-        return m.gate.clone(), loss
+        gate, m.gate = m.gate, m.gate.detach()  # (the layer holds no graph)
+        return gate, loss
 
     @staticmethod
     def backward(ctx, dgate, dloss):
-        (logits,), m = ctx.saved_tensors, ctx.layer
+        (logits, topk, coef), m = ctx.saved_tensors, ctx.layer
         dlogits = torch.empty_like(logits)
-        uep.ultraep_route_grad(logits, m.T, m.E, m.r, None, m.topk, dgate.contiguous(), m.coef, dloss.contiguous(),
+        uep.ultraep_route_grad(logits, m.T, m.E, m.r, None, topk, dgate.contiguous(), coef, dloss.contiguous(),
                                dlogits, m.status)
         return dlogits, None, None
 
@@ -94,15 +102,16 @@ class Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, layer):
         m = ctx.layer = layer
+        ctx.save_for_backward(m.rows)
         send = torch.empty(m.T * m.k, m.H, dtype=BF16, device=DEV)
         uep.ultraep_dispatch_scatter(x, m.T, m.k, m.H, m.rows, m.off[-1:], send)
         return send
 
     @staticmethod
     def backward(ctx, dsend):
-        m = ctx.layer
+        (rows,), m = ctx.saved_tensors, ctx.layer
         dx, one = torch.empty(m.T, m.H, dtype=BF16, device=DEV), torch.ones(m.T, m.k, device=DEV)
-        uep.ultraep_combine(dsend.contiguous(), m.T * m.k, one, m.rows, m.T, m.k, m.H, dx, m.status)
+        uep.ultraep_combine(dsend.contiguous(), m.T * m.k, one, rows, m.T, m.k, m.H, dx, m.status)
         return dx, None
 
 
@@ -112,16 +121,16 @@ class Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, gate, layer):
         m = ctx.layer = layer
-        ctx.save_for_backward(y, gate)
+        ctx.save_for_backward(y, gate, m.rows, m.off)
         out = torch.empty(m.T, m.H, dtype=BF16, device=DEV)
         uep.ultraep_combine(y, m.T * m.k, gate, m.rows, m.T, m.k, m.H, out, m.status)
         return out
 
     @staticmethod
     def backward(ctx, dout):
-        (y, gate), m = ctx.saved_tensors, ctx.layer
+        (y, gate, rows, off), m = ctx.saved_tensors, ctx.layer
         dy, dgate = torch.empty_like(y), torch.empty_like(gate)
-        uep.ultraep_combine_grad(dout.contiguous(), y, m.T * m.k, gate, m.rows, m.T, m.k, m.H, m.off[-1:], dy, dgate,
+        uep.ultraep_combine_grad(dout.contiguous(), y, m.T * m.k, gate, rows, m.T, m.k, m.H, off[-1:], dy, dgate,
                                  m.status)
         return dy, dgate, None
 
@@ -174,9 +183,7 @@ class Int8Experts:
 
 def serve(layer, x, wg, experts):
     m = layer
-    logits = (x.float() @ wg.t()).contiguous()
-    uep.ultraep_route(logits, m.T, m.E, m.r, None, None, m.topk, m.gate, m.counts, m.prob_sum, m.tokens, m.route_ws,
-                      m.status)
+    m.route((x.float() @ wg.t()).contiguous())
     m.make_plan()
     send = torch.empty(m.T * m.k, m.H, dtype=BF16, device=DEV)
     uep.ultraep_dispatch_scatter(x, m.T, m.k, m.H, m.rows, m.off[-1:], send)
