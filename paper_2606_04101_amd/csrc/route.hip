@@ -228,6 +228,10 @@ __device__ __forceinline__ void put_lane(float *row, int l, const float (&v)[kVp
   }
 }
 
+// 16 experts a lane without statistics would take 186 registers; held to 168, with 4 words
+// spilled, a SIMD has three waves instead of two.  us with 168 and 186: 65536 tokens of 256
+// experts in groups 36 and 44, without groups 26 and 34, 16384 in groups 13.0 and 13.9, 4096
+// 6.5 and 6.3.
 template <int kLanes, int kVpl, bool kBf16, bool kStats>
 __global__ void __launch_bounds__(kRtThreads, kLanes == 16 && kVpl == 16 && !kStats ? 3 : 1)
 k_route(RouteArgs a) {
@@ -752,8 +756,8 @@ RouteShape route_shape(int64_t T, const ultraep_router &r) {
   s.n_seg = T > 0 ? (T + s.seq - 1) / s.seq : 1;
   // Workgroups of at least 16 tokens, about as many as run at once (two a compute unit,
   // four with few experts): more make more partials, fewer take turns.  With 1024 and 512
-  // of them, us with the sums and the loss: E = 256, T = 16384 26.3 and 20.9, 65536 53.9
-  // and 48.7; E = 128, T = 16384 17.8 and 15.1; E = 64, T = 65536 21.7 and 26.9.
+  // of them, us with the sums, one sequence: E = 256, T = 16384 23.5 and 18.6, 65536 50.0 and
+  // 45.6; E = 128, T = 16384 16.1 and 13.0; E = 64, T = 16384 10.7 and 10.6, 65536 19.4 and 24.3.
   const int64_t n_wg = route_wg(r);
   s.chunk = (T + n_wg - 1) / n_wg;
   s.chunk = s.chunk < kRtChunk ? kRtChunk : (s.chunk + kRtChunk - 1) / kRtChunk * kRtChunk;
@@ -792,7 +796,9 @@ static void start_route(int lanes, int vpl, dim3 grid, hipStream_t stream, const
     return;                                                                                    \
   }
   UEP_CASE(16, 4) UEP_CASE(16, 8) UEP_CASE(16, 12) UEP_CASE(16, 16) UEP_CASE(16, 24)
-  UEP_CASE(16, 32)
+  if constexpr (kStats) {  // (a wave takes a token of so many experts otherwise)
+    UEP_CASE(16, 32)
+  }
   UEP_CASE(64, 1) UEP_CASE(64, 2) UEP_CASE(64, 4) UEP_CASE(64, 8) UEP_CASE(64, 16) UEP_CASE(64, 32)
 #undef UEP_CASE
 }
@@ -812,10 +818,10 @@ hipError_t launch_route(const void *logits, int32_t type, int64_t T, int64_t ld,
   };
   int lanes = 16, vpl = r.k <= 16 ? spread(16) : 1 << 30;
   // A wave a token where 2048 of them, two a SIMD, are all there are and no statistics are
-  // wanted: us of E = 256 with groups, 16 and 64 lanes a token: T = 1 6.0 and 5.2, 2048 7.1
-  // and 6.5, 4096 7.2 and 8.2, 65536 51 and 69 (with statistics 49 and 99); E = 64: 1 3.9 and
-  // 3.5, 4096 4.5 and 5.2, 65536 13.9 and 32.  Rows of over 24 experts a lane have one wave a
-  // SIMD: E = 512, T = 65536 175 and 103 (with statistics 132 and 176).
+  // wanted: us of E = 256 with groups, 16 and 64 lanes a token: T = 1 5.3 and 4.6, 2048 6.4
+  // and 5.9, 4096 6.5 and 7.8, 65536 36 and 71 (with statistics 47 and 124); E = 64: 1 3.6 and
+  // 3.2, 4096 4.2 and 4.9, 65536 16 and 35.  Rows of over 24 experts a lane have one wave a
+  // SIMD: E = 512, T = 65536 98 and 75 (with statistics 99 and 142).
   const bool stats = counts != nullptr;
   if (vpl > (stats ? 32 : 24) || (!stats && T <= 2048)) {
     lanes = kWave;
