@@ -377,7 +377,10 @@ typedef struct {
  * equal keys by rising id, where the key is
  *   softmax  z + bias
  *   sigmoid  s + bias; z itself where there is neither bias nor groups
- * in fp32 (bias enters the selection only).  An expert whose logit or bias is
+ * in fp32 (bias enters the selection only).  So a softmax's bias is on the
+ * logits' scale, and its groups rank by sums of two logits: a router that adds
+ * its bias to the probabilities, or ranks groups by their largest one, chooses
+ * other ids.  An expert whose logit or bias is
  * -inf is never chosen: the ids left over are -1, their gates 0.  A token that is
  * masked, or has no logit above -inf, gets ids -1 and gates 0 and counts in no
  * statistic; so does one with a NaN or +inf logit, which raises ULTRAEP_EDATA.

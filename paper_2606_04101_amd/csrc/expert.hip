@@ -279,8 +279,9 @@ struct RowTiles {
 };
 
 // v / (1 + exp(-v)) by the hardware's exp2 and reciprocal: a relative error of
-// (|v| + 5) 2^-24 at most.  With expf and a division the epilogue's arithmetic costs
-// 65 us of 3350 at 131072 x 4096 x 7168.
+// (|v| + 5) 2^-24 at most for v >= -87; below, where it is under 2e-36 in magnitude, it
+// becomes 0.  |v| 2^-24 is far below the rounding of the 8-bit operands; with
+// expf and a division the epilogue's arithmetic costs 65 us of 3350 at 131072 x 4096 x 7168.
 __device__ __forceinline__ float silu(float v) { return v * fast_rcp(1.f + fast_exp(-v)); }
 
 // 16 bytes a lane from base + off straight into LDS, lane l's at lds + 16 l.
@@ -775,8 +776,10 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
   const bool bf16 = type == ULTRAEP_BF16;
   // Tiles of 256 x 256 or 128 x 128 where the blocks are large, by the rounds that either
   // takes; 128 x 64 where there are few of those; else, for few rows, the kernel that
-  // shares K between waves.  `rows`: mean of a block that has any; items: estimated
-  // tiles, half a tile of padding a block where there are several.
+  // shares K between waves.  `rows`: M over the blocks, of which the host cannot know how
+  // many are empty (a list that is mostly empty, or an M above the rows that the blocks
+  // hold, is taken for small or large blocks: the result is the same, the time is not); items:
+  // estimated tiles, half a tile of padding a block where there are several.
   //   Times in tenths of a round of 256 x 256: 4 for the round of its quarters, 6 for a
   // round of 128 x 128, two tiles a compute unit.
   //   Measured, us (256 x 256 / 128 x 128 / 128 x 64 / thin 64 / 32 / 16):
@@ -793,6 +796,8 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
   //   6 blocks, N = 4096, K = 1408: M = 20480 138 / 144, 8704 75 / 70, 8192 61 / 67 / 77, 5120
   //   50 / 44, 512 24 / 14 / 13 / 18 / 18 / 19, 256 23 / 13 / 14 / 12 / 12 / 13, 64 22 / 12 / 11
   //   / 11 / 11 / 10
+  //   (The rule misses the best of a line by up to a sixth: 64 blocks of 16 rows, N = 1024,
+  //   K = 2048, go to thin 32, 29, where 128 x 128 takes 25.)
   const int64_t blocks = M < n_block ? M : n_block, rows = (M + blocks - 1) / blocks;
   auto items = [&](int64_t tile_rows, int64_t channels) {
     return (blocks > 1 ? M / tile_rows + (blocks + 1) / 2 : (M + tile_rows - 1) / tile_rows) *

@@ -10,8 +10,10 @@
 //
 // A call reads little (4096 tokens of 256 experts: 4 MB), so instructions and the
 // chain of loads bound it, and launches: ids, gates and statistics of those 4096
-// tokens, by groups, take 8.2 us, their sums over the workgroups 2.6, the loss 2.4, the
-// gradient 4.7; 16384 tokens of 128 experts 9.4, 4.0, 2.2; one token of 256 4.6.
+// tokens, by groups, take 8.4 us, their sums over the workgroups 2.8, the loss 2.5, the
+// gradient 4.8; 16384 tokens of 128 experts 9.4, 3.8, 1.8; one token of 256 4.6.  Prompts are
+// bound by instructions: 65536 tokens of 256 in groups take 36 us, 47 with statistics, where
+// their 71 MB take 14.
 #include "operators.hpp"
 
 namespace uep {
@@ -893,10 +895,10 @@ hipError_t launch_route_grad(const void *logits, int32_t type, int64_t T, int64_
   const RouteShape s = route_shape(T, r);
   // A wave a token for many experts or few tokens, where it shortens the chain; else its
   // idle lanes and its sums over 64 lanes cost more.  us with 16 and 64 lanes, fp32:
-  //   E = 256: T = 1 5.3 and 3.6, 3000 6.5 and 5.0, 6144 7.2 and 6.2, 8192 7.8 and 7.8, 16384
-  //   11.0 and 12.1, 65536 35 and 38 (bf16 30 and 36); E = 128: 512 4.7 and 4.2, 3000 4.8 and
-  //   4.8, 6144 5.2 and 5.9, 16384 6.5 and 10.7; E = 384: 16384 19 and 17, 65536 66 and 54;
-  //   E = 512: 2048 10.1 and 5.3, 16384 27 and 19, 65536 103 and 63
+  //   E = 256: T = 1 5.0 and 3.1, 3000 6.4 and 4.4, 6144 8.0 and 6.7, 8192 8.3 and 8.2, 16384
+  //   11.6 and 12.6, 65536 40 and 39; E = 128: 512 3.9 and 3.5, 3000 4.1 and 4.2, 6144 4.6 and
+  //   5.7, 16384 7.2 and 11.5; E = 384: 16384 19 and 18; E = 512: 2048 10.1 and 4.9, 16384 27
+  //   and 19, 65536 103 and 71
   // (16 lanes of neighbouring experts, whose loads lie 16 to 64 bytes apart, take 16 us at
   // 16384 x 256 and 12.3 at 16384 x 192 in bf16, where chunks in turn take 11.0 and 7.1.)
   const int lanes = r.E > 256 || r.k > 16 || T <= (r.E > 128 ? 6144 : 2048) ? kWave : 16;
