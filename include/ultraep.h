@@ -25,6 +25,12 @@
  *   8. ultraep_combine_grad   backward pass of the combine
  *   9. ultraep_quant_rows     rows to 8-bit integers with a scale each, and
  *      ultraep_expert_matmul  the experts' products on them, block by block
+ *  10. ultraep_expert_matmul_bf16   the experts' products in bf16, forward and
+ *                             for the gradient of their input, and
+ *      ultraep_expert_weight_grad   the gradient of their weights
+ *  11. ultraep_quant_blocks   rows to 8-bit floating point with a scale for each
+ *                             128 elements, and
+ *      ultraep_expert_matmul_fp8    the experts' products on them
  *
  * Conventions for every call:
  *   - Buffer pointers are DEVICE pointers unless marked "host".  The caller
@@ -497,6 +503,117 @@ int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
                           int32_t K, const int64_t *block_off, const int32_t *block_w,
                           int32_t n_block, int32_t act, void *y, int32_t type,
                           int32_t *status, hipStream_t stream);
+
+enum {
+  ULTRAEP_NO_ACT = 0,
+  ULTRAEP_SWIGLU = 1,
+  ULTRAEP_SWIGLU_GRAD = 2
+};
+
+/* The experts' products in bf16.  Row m of block g (rows block_off[g] to
+ * block_off[g + 1] - 1, as the dispatch writes them) meets weight
+ * w = block_w[g]:
+ *   trans 0  v[n] = sum_k x[m][k] * w[n][k], weights [N][K]: the forward product
+ *   trans 1  v[n] = sum_k x[m][k] * w[k][n], weights [K][N]: on the forward
+ *            product's own weights this is the gradient of its input, x being
+ *            the gradient of its output
+ * exact products summed in fp32.  What leaves is
+ *   ULTRAEP_NO_ACT       y[m][n] = v[n]
+ *   ULTRAEP_SWIGLU       y[m][n] = v[n] / (1 + exp(-v[n])) * v[N/2 + n], n < N/2
+ *                        (gates first), and pre[m] = v unless pre is null
+ *   ULTRAEP_SWIGLU_GRAD  v is the gradient of such a y; with a, b = pre[m][n],
+ *                        pre[m][N + n] and s = 1 / (1 + exp(-a)),
+ *                        y[m][n]     = v[n] * b * s * (1 + a * (1 - s))
+ *                        y[m][N + n] = v[n] * a * s
+ * in fp32 (the SwiGLU of v itself, not of the rounded pre), rounded to
+ * nearest-even to `type`, pre to bf16.
+ *   x          [M][K] bf16
+ *   w          n_w weights of N * K bf16, w_stride elements apart (so they may
+ *              lie in blobs that hold an expert's other weights too)
+ *   block_off  [n_block + 1] int64 (a part of the dispatch's is fine: rows
+ *              outside the blocks are neither read nor written)
+ *   block_w    [n_block] int32, or null (block g takes weight g)
+ *   pre        SWIGLU: [M][N] bf16, written, or null; SWIGLU_GRAD: [M][2 N]
+ *              bf16, read; NO_ACT: null
+ *   y          rows of N, N / 2 (SWIGLU) or 2 N (SWIGLU_GRAD) elements; with
+ *              SWIGLU_GRAD and bf16 it may be pre itself, else it aliases nothing
+ * Blocks that are not in rising order within [0, M], and a nonempty block
+ * whose weight is outside [0, n_w), raise ULTRAEP_EDATA; then no row is written.
+ * 1 <= n_block <= 2048, n_w >= 1, M < 2^31; K, N % 8 == 0 (N % 16 == 0 with
+ * SWIGLU), 8 <= K, N <= 2^20, M * N < 2^38; N * K <= w_stride <= 2^40,
+ * w_stride % 8 == 0; 16-byte aligned x, w, pre and y. */
+int ultraep_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_t *w, int32_t n_w,
+                               int64_t w_stride, int32_t N, int32_t K, int32_t trans,
+                               const int64_t *block_off, const int32_t *block_w,
+                               int32_t n_block, int32_t act, uint16_t *pre, void *y,
+                               int32_t type, int32_t *status, hipStream_t stream);
+
+/* Gradient of the weights of y = x w^T: for every weight w of n_w
+ *   dw[w][n][k] = sum over the blocks g with block_w[g] = w, in rising order,
+ *                 and their rows m, of dy[m][n] * x[m][k]
+ * exact products summed in fp32, rounded to nearest-even to `type`; with
+ * accumulate 1 added to the dw that is there (in fp32).  A weight without rows
+ * gets zeros (accumulate: stays as it is).  dw are weights [N][K]; where the
+ * forward pass keeps [K][N], swap dy and x.  fp32 gradients dw_stride apart are
+ * what ultraep_grad_reduce takes.
+ *   dy         [M][N] bf16, x [M][K] bf16 (they may be the same)
+ *   block_off, block_w, n_block  as for ultraep_expert_matmul_bf16
+ *   dw         n_w gradients of N * K elements of `type`, dw_stride elements
+ *              apart; what lies between them is not written
+ *   ws         workspace of ws_bytes >= ultraep_expert_weight_grad_ws_bytes,
+ *              16-byte aligned, or null: where the weights are few and small,
+ *              their rows are summed in parts, side by side, with it (the
+ *              result then differs in the order of the sums)
+ * Equal calls give equal bits.  An unsound list raises ULTRAEP_EDATA as there;
+ * then nothing is written to dw.
+ * N, K % 8 == 0, 8 <= N, K <= 2^20, n_w <= 2^20, ceil(N / 64) * ceil(K / 64) *
+ * n_w < 2^31, M < 2^31; N * K <= dw_stride <= 2^40, dw_stride % 8 == 0;
+ * 16-byte aligned dy, x and dw. */
+int ultraep_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M, int32_t N,
+                               int32_t K, const int64_t *block_off, const int32_t *block_w,
+                               int32_t n_block, int32_t n_w, int64_t dw_stride,
+                               int32_t accumulate, void *dw, int32_t type, void *ws,
+                               size_t ws_bytes, int32_t *status, hipStream_t stream);
+
+/* Bytes of that workspace for up to M rows (host only; 0 for unsupported
+ * arguments, at least 16 otherwise). */
+size_t ultraep_expert_weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w);
+
+/* Rows to 8-bit floating point (e4m3: 4 bits of exponent, 3 of mantissa, largest
+ * 448, no infinities) with a power-of-two scale for each 128 elements.  In each
+ * block of 128 (the row's last may be shorter), e is the least integer with
+ * |x| <= 448 * 2^e throughout, -127 at least, and
+ *   q = x * 2^-e rounded to nearest-even to e4m3,  scale byte = e + 127
+ * (the value of q is q * 2^e; scale bytes are e8m0).  A block with an infinity
+ * or a NaN has every q NaN (0x7F) and scale byte 255 (NaN).  A weight [n][N][K]
+ * takes n * N rows.
+ *   x      rows of K elements of `type`, ld elements apart
+ *   q      rows of ldq bytes, ldq >= K: K values, then zeros
+ *   scale  rows of 4 * ceil(K / 512) bytes: ceil(K / 128) scales, then zeros;
+ *          4-byte aligned
+ * K, ld % 8 == 0, ldq % 16 == 0, ld, ldq <= 2^20, rows < 2^31, 16-byte aligned x
+ * and q. */
+int ultraep_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
+                         uint8_t *q, int64_t ldq, uint8_t *scale, hipStream_t stream);
+
+/* The experts' products on such values.  Row m of block g meets weight
+ * w = block_w[g]; with b = k / 128,
+ *   v[n] = sum_k xq[m][k] * wq[w][n][k] * 2^(x_scale[m][b] + w_scale[w][n][b] - 254)
+ * in fp32 by the matrix unit, which applies the scales.  y[m] = v, or with act
+ * ULTRAEP_SWIGLU
+ *   y[m][n] = v[n] / (1 + exp(-v[n])) * v[N/2 + n],  n < N/2
+ * rounded to nearest-even to `type`.  A weight whose scales are held for blocks
+ * of 128 x 128 repeats each for 128 rows.
+ *   xq         [M][K] e4m3, x_scale [M][4 * ceil(K / 512)] bytes
+ *   wq         [n_w][N][K] e4m3, w_scale [n_w][N][4 * ceil(K / 512)] bytes
+ *   block_off, block_w, n_block, y, errors  as for ultraep_expert_matmul
+ * K % 16 == 0, N % 8 == 0 (N % 16 == 0 with act), 16 <= K <= 2^20, 8 <= N <= 2^20,
+ * M < 2^31, M * N < 2^38; 16-byte aligned xq, wq and y, 4-byte aligned scales. */
+int ultraep_expert_matmul_fp8(const uint8_t *xq, const uint8_t *x_scale, int64_t M,
+                              const uint8_t *wq, const uint8_t *w_scale, int32_t n_w, int32_t N,
+                              int32_t K, const int64_t *block_off, const int32_t *block_w,
+                              int32_t n_block, int32_t act, void *y, int32_t type,
+                              int32_t *status, hipStream_t stream);
 
 /* Host only.  Static description of a status code. */
 const char *ultraep_strerror(int code);

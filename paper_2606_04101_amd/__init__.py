@@ -70,6 +70,7 @@ class PlanBuf(ctypes.Structure):
 
 ULTRAEP_F32, ULTRAEP_BF16 = 0, 1
 ULTRAEP_SOFTMAX, ULTRAEP_SIGMOID = 0, 1
+ULTRAEP_NO_ACT, ULTRAEP_SWIGLU, ULTRAEP_SWIGLU_GRAD = 0, 1, 2
 
 
 class Router(ctypes.Structure):
@@ -143,6 +144,15 @@ def lib():
         L.ultraep_quant_rows.argtypes = [_P, i32, i64, i64, i64, _P, i64, _P, _P]
         L.ultraep_expert_matmul.argtypes = [_P, _P, i64, _P, _P, i32, i32, i32, _P, _P, i32, i32,
                                             _P, i32, _P, _P]
+        L.ultraep_expert_matmul_bf16.argtypes = [_P, i64, _P, i32, i64, i32, i32, i32, _P, _P, i32,
+                                                 i32, _P, _P, i32, _P, _P]
+        L.ultraep_expert_weight_grad.argtypes = [_P, _P, i64, i32, i32, _P, _P, i32, i32, i64, i32,
+                                                 _P, i32, _P, sz, _P, _P]
+        L.ultraep_expert_weight_grad_ws_bytes.argtypes = [i64, i32, i32, i32]
+        L.ultraep_expert_weight_grad_ws_bytes.restype = sz
+        L.ultraep_quant_blocks.argtypes = [_P, i32, i64, i64, i64, _P, i64, _P, _P]
+        L.ultraep_expert_matmul_fp8.argtypes = [_P, _P, i64, _P, _P, i32, i32, i32, _P, _P, i32, i32,
+                                                _P, i32, _P, _P]
         L.ultraep_strerror.argtypes = [ctypes.c_int]
         L.ultraep_strerror.restype = ctypes.c_char_p
         for f in ("ultraep_plan_sizes", "ultraep_count", "ultraep_plan",
@@ -152,7 +162,9 @@ def lib():
                   "ultraep_reroute_and_pack", "ultraep_relay_plan",
                   "ultraep_pack_relay", "ultraep_combine", "ultraep_grad_reduce",
                   "ultraep_route", "ultraep_balance_loss", "ultraep_route_grad",
-                  "ultraep_combine_grad", "ultraep_quant_rows", "ultraep_expert_matmul"):
+                  "ultraep_combine_grad", "ultraep_quant_rows", "ultraep_expert_matmul",
+                  "ultraep_expert_matmul_bf16", "ultraep_expert_weight_grad",
+                  "ultraep_quant_blocks", "ultraep_expert_matmul_fp8"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -190,7 +202,8 @@ def _load_native():
                           "dispatch", "dispatch_layout", "dispatch_scatter", "pack_replicas",
                           "reroute_and_pack", "relay_plan", "pack_relay", "combine",
                           "grad_reduce", "route", "balance_loss", "route_grad",
-                          "combine_grad", "quant_rows", "expert_matmul")},
+                          "combine_grad", "quant_rows", "expert_matmul", "expert_matmul_bf16",
+                          "expert_weight_grad", "quant_blocks", "expert_matmul_fp8")},
                Group, Plan, PlanBuf, Router)
     _native = m
     return m
@@ -610,6 +623,101 @@ def ultraep_expert_matmul(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, blo
         _ptr(xq), _ptr(x_scale), M, _ptr(wq), _ptr(w_scale), n_w, N, K, _ptr(block_off),
         _ptr(block_w), n_block, int(act), _ptr(y), type_, _ptr(status), _stream(stream)),
         "ultraep_expert_matmul")
+
+
+def _need_blocks(block_off, block_w, n_block, status):
+    _need(block_off, n_block + 1, 8, "block_off")
+    _need(block_w, n_block if block_w is not None else 0, 4, "block_w")
+    _need(status, 1, 4, "status")
+
+
+def ultraep_expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans, block_off, block_w, n_block, act,
+                               pre, y, status, stream=None):
+    """act: ULTRAEP_NO_ACT, ULTRAEP_SWIGLU or ULTRAEP_SWIGLU_GRAD.  block_w may be None
+    (block g takes weight g), pre where act does not read it; y is float32 or bfloat16."""
+    rc = (_native or _load_native()).expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans,
+                                                       block_off, block_w, n_block, act, pre, y,
+                                                       status, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_matmul_bf16")
+    type_ = _row_type(y, "y") if M > 0 else ULTRAEP_BF16
+    _need(x, M * K, 2, "x")
+    _need(w, (n_w - 1) * w_stride + N * K if n_w > 0 else 0, 2, "w")
+    _need_blocks(block_off, block_w, n_block, status)
+    grad = act == ULTRAEP_SWIGLU_GRAD
+    _need(pre, M * (2 * N if grad else N) if grad or pre is not None else 0, 2, "pre")
+    _need(y, M * (2 * N if grad else N // 2 if act == ULTRAEP_SWIGLU else N),
+          4 if type_ == ULTRAEP_F32 else 2, "y")
+    return _check(lib().ultraep_expert_matmul_bf16(
+        _ptr(x), M, _ptr(w), n_w, w_stride, N, K, int(trans), _ptr(block_off), _ptr(block_w),
+        n_block, int(act), _ptr(pre), _ptr(y), type_, _ptr(status), _stream(stream)),
+        "ultraep_expert_matmul_bf16")
+
+
+def ultraep_expert_weight_grad_ws_bytes(M, N, K, n_w) -> int:
+    return int(lib().ultraep_expert_weight_grad_ws_bytes(M, N, K, n_w))
+
+
+def ultraep_expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block, n_w, dw_stride,
+                               accumulate, dw, ws, status, stream=None):
+    """block_w and ws may be None; dw is float32 or bfloat16."""
+    rc = (_native or _load_native()).expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block,
+                                                       n_w, dw_stride, accumulate, dw, ws, status,
+                                                       stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_weight_grad")
+    type_ = _row_type(dw, "dw")
+    _need(dy, M * N, 2, "dy")
+    _need(x, M * K, 2, "x")
+    _need_blocks(block_off, block_w, n_block, status)
+    _need(dw, (n_w - 1) * dw_stride + N * K if n_w > 0 else 0, 4 if type_ == ULTRAEP_F32 else 2,
+          "dw")
+    return _check(lib().ultraep_expert_weight_grad(
+        _ptr(dy), _ptr(x), M, N, K, _ptr(block_off), _ptr(block_w), n_block, n_w, dw_stride,
+        int(accumulate), _ptr(dw), type_, _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0, _ptr(status), _stream(stream)),
+        "ultraep_expert_weight_grad")
+
+
+def ultraep_quant_blocks(x, rows, K, ld, q, ldq, scale, stream=None):
+    """q and scale have one-byte elements (uint8, or torch's float8 types)."""
+    rc = (_native or _load_native()).quant_blocks(x, rows, K, ld, q, ldq, scale, stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_quant_blocks")
+    type_ = _row_type(x, "x") if rows > 0 else ULTRAEP_BF16
+    _need_rows(x, rows, K, ld, type_, "x")
+    _need(q, rows * ldq, 1, "q")
+    _need(scale, rows * scale_pitch(K), 1, "scale")
+    return _check(lib().ultraep_quant_blocks(_ptr(x), type_, rows, K, ld, _ptr(q), ldq, _ptr(scale),
+                                             _stream(stream)), "ultraep_quant_blocks")
+
+
+def scale_pitch(K):
+    """Bytes of a row's scales in 8-bit floating point: one for each 128 elements,
+    and zeros up to a multiple of 4."""
+    return 4 * -(-K // 512)
+
+
+def ultraep_expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w, n_block, act,
+                              y, status, stream=None):
+    """xq, wq and the scales have one-byte elements; block_w may be None (block g takes
+    weight g); act: ULTRAEP_NO_ACT or ULTRAEP_SWIGLU; y is float32 or bfloat16."""
+    rc = (_native or _load_native()).expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K,
+                                                      block_off, block_w, n_block, act, y, status,
+                                                      stream)
+    if rc is not None:
+        return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_matmul_fp8")
+    type_ = _row_type(y, "y") if M > 0 else ULTRAEP_BF16
+    _need(xq, M * K, 1, "xq")
+    _need(x_scale, M * scale_pitch(K), 1, "x_scale")
+    _need(wq, n_w * N * K, 1, "wq")
+    _need(w_scale, n_w * N * scale_pitch(K), 1, "w_scale")
+    _need_blocks(block_off, block_w, n_block, status)
+    _need(y, M * (N // 2 if act else N), 4 if type_ == ULTRAEP_F32 else 2, "y")
+    return _check(lib().ultraep_expert_matmul_fp8(
+        _ptr(xq), _ptr(x_scale), M, _ptr(wq), _ptr(w_scale), n_w, N, K, _ptr(block_off),
+        _ptr(block_w), n_block, int(act), _ptr(y), type_, _ptr(status), _stream(stream)),
+        "ultraep_expert_matmul_fp8")
 
 
 def build():

@@ -13,14 +13,15 @@ LIB = os.path.join(HERE, "libultraep.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["abi.hip", "count.hip", "plan.hip", "dispatch.hip", "pack.hip",
            "relay.hip", "combine.hip", "reduce.hip",
-           "operators.hip", "route.hip", "combine_grad.hip", "expert.hip"]
+           "operators.hip", "route.hip", "combine_grad.hip", "expert.hip", "products.hip",
+           "weight_grad.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions are disabled for all device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # the fp32 steps of the path round every product and sum on its own: no contraction
 # into fused multiply-adds.  The path's other sources have no fp32 arithmetic to fuse; the
-# operators' may (route.hip, combine_grad.hip, expert.hip) but for the kernels that say no.
+# operators' may but for the kernels that say no.
 EXTRA = {"combine.hip": ["-ffp-contract=off"], "reduce.hip": ["-ffp-contract=off"]}
 
 

@@ -22,7 +22,8 @@ typedef __int128 wide;  // products of caller-given sizes
   X(count) X(plan) X(plan_noalloc) X(plan_replicate) X(plan_reroute) X(dispatch)             \
   X(dispatch_layout) X(dispatch_scatter) X(pack_replicas) X(reroute_and_pack) X(relay_plan)  \
   X(pack_relay) X(combine) X(grad_reduce) X(route) X(balance_loss) X(route_grad)             \
-  X(combine_grad) X(quant_rows) X(expert_matmul)
+  X(combine_grad) X(quant_rows) X(expert_matmul) X(expert_matmul_bf16)                       \
+  X(expert_weight_grad) X(quant_blocks) X(expert_matmul_fp8)
 
 struct Library {
 #define FIELD(n) decltype(&ultraep_##n) n = nullptr;
@@ -187,6 +188,8 @@ wide loads(const ultraep_group *g) { return wide(g->R) * g->E; }
 wide mains(const ultraep_group *g) { return g->E / g->R; }
 // elements that T rows of n, ld apart, take
 wide strided(int64_t T, int64_t n, int64_t ld) { return T > 0 ? (wide(T) - 1) * ld + n : 0; }
+// bytes of a row's scales in 8-bit floating point
+wide scale_pitch(int64_t K) { return K > 0 ? (wide(K) + 511) / 512 * 4 : 0; }
 wide sequences(const ultraep_router *r, int64_t T) {
   return r->seq_len > 0 && T > 0 ? (wide(T) + r->seq_len - 1) / r->seq_len : 1;
 }
@@ -509,6 +512,77 @@ ENTRY(expert_matmul, 15, {
   });
 })
 
+// x, M, w, n_w, w_stride, N, K, trans, block_off, block_w, n_block, act, pre, y, status, stream
+ENTRY(expert_matmul_bf16, 16, {
+  const int64_t M = v.i64(1), stride = v.i64(4);
+  const int32_t n_w = v.i32(3), N = v.i32(5), K = v.i32(6), trans = v.flag(7), n = v.i32(10);
+  const int32_t act = v.flag(11);
+  const bool grad = act == ULTRAEP_SWIGLU_GRAD;
+  auto *x = v.tensor<uint16_t>(0, wide(M) * K);
+  auto *w = v.tensor<uint16_t>(2, n_w > 0 ? (wide(n_w) - 1) * stride + wide(N) * K : 0);
+  auto *off = v.tensor<int64_t>(8, wide(n) + 1);
+  auto *bw = v.maybe<int32_t>(9, n);
+  auto *pre = grad ? v.tensor<uint16_t>(12, wide(M) * 2 * N) : v.maybe<uint16_t>(12, wide(M) * N);
+  int32_t type;
+  void *y = v.rows(13, wide(M) * (grad ? 2 * wide(N) : act == ULTRAEP_SWIGLU ? N / 2 : N), type);
+  auto *status = v.tensor<int32_t>(14, 1);
+  hipStream_t s = v.stream(15);
+  return finish(v, [&] {
+    return lib.expert_matmul_bf16(x, M, w, n_w, stride, N, K, trans, off, bw, n, act, pre, y, type,
+                                  status, s);
+  });
+})
+
+// dy, x, M, N, K, block_off, block_w, n_block, n_w, dw_stride, accumulate, dw, ws, status, stream
+ENTRY(expert_weight_grad, 15, {
+  const int64_t M = v.i64(2), stride = v.i64(9);
+  const int32_t N = v.i32(3), K = v.i32(4), n = v.i32(7), n_w = v.i32(8), acc = v.flag(10);
+  auto *dy = v.tensor<uint16_t>(0, wide(M) * N);
+  auto *x = v.tensor<uint16_t>(1, wide(M) * K);
+  auto *off = v.tensor<int64_t>(5, wide(n) + 1);
+  auto *bw = v.maybe<int32_t>(6, n);
+  int32_t type;
+  void *dw = v.rows(11, n_w > 0 ? (wide(n_w) - 1) * stride + wide(N) * K : 0, type);
+  size_t ws_bytes = 0;
+  void *ws = v.ok && argv[12] != Py_None ? v.workspace(12, -1, ws_bytes) : nullptr;
+  auto *status = v.tensor<int32_t>(13, 1);
+  hipStream_t s = v.stream(14);
+  return finish(v, [&] {
+    return lib.expert_weight_grad(dy, x, M, N, K, off, bw, n, n_w, stride, acc, dw, type, ws, ws_bytes,
+                                  status, s);
+  });
+})
+
+// x, rows, K, ld, q, ldq, scale, stream
+ENTRY(quant_blocks, 8, {
+  const int64_t rows = v.i64(1), K = v.i64(2), ld = v.i64(3), ldq = v.i64(5);
+  int32_t type;
+  void *x = v.rows(0, strided(rows, K, ld), type);
+  auto *q = v.tensor<uint8_t>(4, wide(rows) * ldq);
+  auto *scale = v.tensor<uint8_t>(6, wide(rows) * scale_pitch(K));
+  hipStream_t s = v.stream(7);
+  return finish(v, [&] { return lib.quant_blocks(x, type, rows, K, ld, q, ldq, scale, s); });
+})
+
+// xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w, n_block, act, y, status, stream
+ENTRY(expert_matmul_fp8, 15, {
+  const int64_t M = v.i64(2);
+  const int32_t n_w = v.i32(5), N = v.i32(6), K = v.i32(7), n = v.i32(10), act = v.flag(11);
+  auto *xq = v.tensor<uint8_t>(0, wide(M) * K);
+  auto *xs = v.tensor<uint8_t>(1, wide(M) * scale_pitch(K));
+  auto *wq = v.tensor<uint8_t>(3, wide(n_w) * N * K);
+  auto *ws = v.tensor<uint8_t>(4, wide(n_w) * N * scale_pitch(K));
+  auto *off = v.tensor<int64_t>(8, wide(n) + 1);
+  auto *bw = v.maybe<int32_t>(9, n);
+  int32_t type;
+  void *y = v.rows(12, wide(M) * (act ? N / 2 : N), type);
+  auto *status = v.tensor<int32_t>(13, 1);
+  hipStream_t s = v.stream(14);
+  return finish(v, [&] {
+    return lib.expert_matmul_fp8(xq, xs, M, wq, ws, n_w, N, K, off, bw, n, act, y, type, status, s);
+  });
+})
+
 // bind({entry point: address}, Group, Plan, PlanBuf[, Router]); without Router no call with
 // one is taken
 PyObject *py_bind(PyObject *, PyObject *args) {
@@ -547,7 +621,8 @@ PyMethodDef methods[] = {FAST(count), FAST(plan), FAST(plan_noalloc), FAST(plan_
                          FAST(dispatch_scatter), FAST(pack_replicas), FAST(reroute_and_pack),
                          FAST(relay_plan), FAST(pack_relay), FAST(combine), FAST(grad_reduce),
                          FAST(route), FAST(balance_loss), FAST(route_grad), FAST(combine_grad),
-                         FAST(quant_rows), FAST(expert_matmul),
+                         FAST(quant_rows), FAST(expert_matmul), FAST(expert_matmul_bf16),
+                         FAST(expert_weight_grad), FAST(quant_blocks), FAST(expert_matmul_fp8),
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,

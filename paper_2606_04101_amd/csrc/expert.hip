@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "operators.hpp"
+#include "tiles.hpp"
 
 namespace uep {
 
@@ -178,132 +179,11 @@ struct MatmulArgs {
   int32_t n_w, N, K, n_block, n_out;
 };
 
-constexpr int kMmMaxBlocks = 2048;
-
-// v, with what follows from it computed where it is used: a persistent loop would
-// otherwise hold every lane's address of its rare parts in registers throughout
-__device__ __forceinline__ int opaque(int v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
-
-__device__ __forceinline__ int64_t readlane64(int64_t v, int l) {
-  const uint32_t lo = readlane(static_cast<int>(v), l), hi = readlane(static_cast<int>(v >> 32), l);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-
-// an address that is the same in all lanes, in scalar registers
-template <class T>
-__device__ __forceinline__ T *uniform(T *p) {
-  const uintptr_t v = reinterpret_cast<uintptr_t>(p);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
-  return reinterpret_cast<T *>(static_cast<uintptr_t>(hi) << 32 | lo);
-}
-
-// A tile of rows of one block: its first row, rows and weight.
-struct RowTile {
-  int64_t row;
-  int32_t rows, w;
-};
-
-// Row tiles are numbered block by block.  Blocks are looked at in runs of 64, one a
-// lane; a wave holds one run's blocks, and the runs' tile counts, in registers.  Where a
-// block is out of order or out of [0, M], or has rows and no weight, that is reported and
-// there are no tiles at all, so that what is numbered lies within M rows.  Every lane
-// must be active in each call.
-template <int kTileRows>
-struct RowTiles {
-  int64_t lo;               // this lane's block of run `run`:
-  int rows, w;              //   its first row, rows, weight
-  int before, tiles;        //   its tiles, and the run's before it
-  int run, n_run;
-  int run_before, run_tiles;  // of run `lane`
-  int total;                // tiles in all
-
-  // false (in the whole wave) if a block of run r is not sound
-  __device__ bool load(const MatmulArgs &a, int r) {
-    run = r;
-    bool sound = true;
-    const int g = r * kWave + lane_id();
-    lo = 0;
-    rows = w = 0;
-    if (g < a.n_block) {
-      lo = a.block_off[g];
-      const int64_t hi = a.block_off[g + 1];
-      w = a.block_w ? a.block_w[g] : g;
-      sound = lo >= 0 && hi >= lo && hi <= a.M && (hi == lo || (w >= 0 && w < a.n_w));
-      if (sound)
-        rows = static_cast<int>(hi - lo);
-      else
-        report(a.status, ULTRAEP_EDATA);
-    }
-    tiles = rows > 0 ? (rows - 1) / kTileRows + 1 : 0;
-    before = wave_scan_incl(tiles) - tiles;
-    return !ballot(!sound);
-  }
-  // s_run: 32 words of LDS, free again after the call's last barrier
-  __device__ void count(const MatmulArgs &a, int *s_run, int wave, int n_waves) {
-    n_run = (a.n_block + kWave - 1) / kWave;
-    if (n_run == 1) {
-      const bool sound = load(a, 0);
-      run_before = 0;
-      total = sound ? readlane(before + tiles, kWave - 1) : 0;
-      run_tiles = lane_id() == 0 ? total : 0;
-      return;
-    }
-    for (int r = wave; r < n_run; r += n_waves) {
-      const bool sound = load(a, r);
-      if (lane_id() == kWave - 1) s_run[r] = sound ? before + tiles : -1;
-    }
-    __syncthreads();
-    run_tiles = lane_id() < n_run ? s_run[lane_id()] : 0;
-    __syncthreads();
-    run_before = wave_scan_incl(run_tiles) - run_tiles;
-    total = readlane(run_before, kWave - 1);  // (fewer than 64 runs)
-    if (ballot(run_tiles < 0)) total = 0;
-    run = -1;
-  }
-  // tile < total
-  __device__ RowTile find(const MatmulArgs &a, int tile) {
-    int t = tile;
-    if (n_run > 1) {
-      const int r = __builtin_ctzll(ballot(tile >= run_before && tile < run_before + run_tiles));
-      t -= readlane(run_before, r);
-      if (r != run) load(a, r);
-    }
-    const int l = __builtin_ctzll(ballot(t >= before && t < before + tiles));
-    const int first = (t - readlane(before, l)) * kTileRows;
-    return {readlane64(lo, l) + first, min(readlane(rows, l) - first, kTileRows), readlane(w, l)};
-  }
-};
-
 // v / (1 + exp(-v)) by the hardware's exp2 and reciprocal: a relative error of
 // (|v| + 5) 2^-24 at most for v >= -87; below, where it is under 2e-36 in magnitude, it
 // becomes 0.  |v| 2^-24 is far below the rounding of the 8-bit operands; with
 // expf and a division the epilogue's arithmetic costs 65 us of 3350 at 131072 x 4096 x 7168.
 __device__ __forceinline__ float silu(float v) { return v * fast_rcp(1.f + fast_exp(-v)); }
-
-// 16 bytes a lane from base + off straight into LDS, lane l's at lds + 16 l.
-// The wait for it is the caller's (vmcnt).
-__device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(lds), "v"(off), "s"(base)
-               : "memory", "m0");
-}
-
-// the same for 4 bytes a lane
-__device__ __forceinline__ void load_word_to_lds(const void *base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               :
-               : "s"(lds), "v"(off), "s"(base)
-               : "memory", "m0");
-}
-template <class T>
-__device__ __forceinline__ uint32_t lds_address(T *p) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) T *)p));
-}
 
 constexpr int kBk = 128;  // bytes of K of a step
 

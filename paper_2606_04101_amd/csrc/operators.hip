@@ -36,6 +36,22 @@ bool logits_ok(const void *logits, int32_t type, int64_t T, int64_t ld, const ul
   return (reinterpret_cast<uintptr_t>(logits) & (type == ULTRAEP_BF16 ? 1u : 3u)) == 0;
 }
 
+// M rows in blocks of n_w weights
+bool blocks_ok(int64_t M, int32_t n_w, const int64_t *block_off, int32_t n_block) {
+  return M >= 0 && M < (int64_t(1) << 31) && n_w >= 1 && n_block >= 1 &&
+         n_block <= uep::kMaxBlocks && block_off;
+}
+bool extent_ok(int32_t n, int32_t step) { return n >= step && n % step == 0 && n <= 1 << 20; }
+// elements from one weight to the next
+bool stride_ok(int64_t stride, int32_t N, int32_t K) {
+  return stride >= static_cast<int64_t>(N) * K && stride % 8 == 0 && stride <= int64_t(1) << 40;
+}
+// gradients of n_w weights: their tiles are numbered in 31 bits
+bool weights_ok(int32_t n_w, int32_t N, int32_t K) {
+  return n_w >= 1 && n_w <= 1 << 20 && extent_ok(N, 8) && extent_ok(K, 8) &&
+         int64_t(n_w) * ((N + 63) / 64) * ((K + 63) / 64) < int64_t(1) << 31;
+}
+
 }  // namespace
 
 extern "C" {
@@ -117,7 +133,7 @@ int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
                           int32_t K, const int64_t *block_off, const int32_t *block_w,
                           int32_t n_block, int32_t act, void *y, int32_t type,
                           int32_t *status, hipStream_t stream) {
-  if (M < 0 || M >= (int64_t(1) << 31) || n_w < 1 || n_block < 1 || n_block > 2048 ||
+  if (M < 0 || M >= (int64_t(1) << 31) || n_w < 1 || n_block < 1 || n_block > uep::kMaxBlocks ||
       !type_ok(type) || (act != 0 && act != 1) || !block_off || !status)
     return ULTRAEP_EINVAL;
   if (K < 16 || K % 16 != 0 || K > 1 << 16) return ULTRAEP_EINVAL;
@@ -128,6 +144,74 @@ int ultraep_expert_matmul(const int8_t *xq, const float *x_scale, int64_t M,
   if (!xq || !aligned16(xq) || !x_scale || !y || !aligned16(y)) return ULTRAEP_EINVAL;
   return rc(uep::launch_expert_matmul(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w,
                                       n_block, act, y, type, status, stream));
+}
+
+int ultraep_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_t *w, int32_t n_w,
+                               int64_t w_stride, int32_t N, int32_t K, int32_t trans,
+                               const int64_t *block_off, const int32_t *block_w,
+                               int32_t n_block, int32_t act, uint16_t *pre, void *y,
+                               int32_t type, int32_t *status, hipStream_t stream) {
+  if (!blocks_ok(M, n_w, block_off, n_block) || !type_ok(type) || !status) return ULTRAEP_EINVAL;
+  if (trans != 0 && trans != 1) return ULTRAEP_EINVAL;
+  if (act != ULTRAEP_NO_ACT && act != ULTRAEP_SWIGLU && act != ULTRAEP_SWIGLU_GRAD)
+    return ULTRAEP_EINVAL;
+  if (!extent_ok(K, 8) || !extent_ok(N, act == ULTRAEP_SWIGLU ? 16 : 8)) return ULTRAEP_EINVAL;
+  if (M * static_cast<int64_t>(N) >= int64_t(1) << 38) return ULTRAEP_EINVAL;
+  if (!stride_ok(w_stride, N, K) || !w || !aligned16(w)) return ULTRAEP_EINVAL;
+  if ((act == ULTRAEP_NO_ACT && pre) || !aligned16(pre)) return ULTRAEP_EINVAL;
+  if (M == 0) return ULTRAEP_OK;
+  if (act == ULTRAEP_SWIGLU_GRAD && !pre) return ULTRAEP_EINVAL;
+  if (!x || !aligned16(x) || !y || !aligned16(y)) return ULTRAEP_EINVAL;
+  return rc(uep::launch_expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans, block_off, block_w,
+                                           n_block, act, pre, y, type, status, stream));
+}
+
+size_t ultraep_expert_weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w) {
+  if (M < 0 || M >= int64_t(1) << 31 || !weights_ok(n_w, N, K)) return 0;
+  return uep::weight_grad_ws_bytes(M, N, K, n_w);
+}
+
+int ultraep_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M, int32_t N,
+                               int32_t K, const int64_t *block_off, const int32_t *block_w,
+                               int32_t n_block, int32_t n_w, int64_t dw_stride,
+                               int32_t accumulate, void *dw, int32_t type, void *ws,
+                               size_t ws_bytes, int32_t *status, hipStream_t stream) {
+  if (!blocks_ok(M, n_w, block_off, n_block) || !type_ok(type) || !status) return ULTRAEP_EINVAL;
+  if ((accumulate != 0 && accumulate != 1) || !weights_ok(n_w, N, K)) return ULTRAEP_EINVAL;
+  if (!stride_ok(dw_stride, N, K) || !dw || !aligned16(dw)) return ULTRAEP_EINVAL;
+  if (ws && (!aligned16(ws) || ws_bytes < uep::weight_grad_ws_bytes(M, N, K, n_w)))
+    return ULTRAEP_EINVAL;
+  if (M > 0 && (!dy || !aligned16(dy) || !x || !aligned16(x))) return ULTRAEP_EINVAL;
+  return rc(uep::launch_expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block, n_w,
+                                           dw_stride, accumulate, dw, type, ws, status, stream));
+}
+
+int ultraep_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
+                         uint8_t *q, int64_t ldq, uint8_t *scale, hipStream_t stream) {
+  if (!type_ok(type) || rows < 0 || rows >= (int64_t(1) << 31)) return ULTRAEP_EINVAL;
+  if (K < 8 || K % 8 != 0 || ld < K || ld % 8 != 0 || ld > 1 << 20) return ULTRAEP_EINVAL;
+  if (ldq < K || ldq % 16 != 0 || ldq > 1 << 20) return ULTRAEP_EINVAL;
+  if (rows == 0) return ULTRAEP_OK;
+  if (!x || !q || !scale || !aligned16(x) || !aligned16(q) || !aligned4(scale))
+    return ULTRAEP_EINVAL;
+  return rc(uep::launch_quant_blocks(x, type, rows, K, ld, q, ldq, scale, stream));
+}
+
+int ultraep_expert_matmul_fp8(const uint8_t *xq, const uint8_t *x_scale, int64_t M,
+                              const uint8_t *wq, const uint8_t *w_scale, int32_t n_w, int32_t N,
+                              int32_t K, const int64_t *block_off, const int32_t *block_w,
+                              int32_t n_block, int32_t act, void *y, int32_t type,
+                              int32_t *status, hipStream_t stream) {
+  if (!blocks_ok(M, n_w, block_off, n_block) || !type_ok(type) || !status) return ULTRAEP_EINVAL;
+  if (act != ULTRAEP_NO_ACT && act != ULTRAEP_SWIGLU) return ULTRAEP_EINVAL;
+  if (!extent_ok(K, 16) || !extent_ok(N, act ? 16 : 8)) return ULTRAEP_EINVAL;
+  if (M * static_cast<int64_t>(N) >= int64_t(1) << 38) return ULTRAEP_EINVAL;
+  if (!wq || !aligned16(wq) || !w_scale || !aligned4(w_scale)) return ULTRAEP_EINVAL;
+  if (M == 0) return ULTRAEP_OK;
+  if (!xq || !aligned16(xq) || !x_scale || !aligned4(x_scale) || !y || !aligned16(y))
+    return ULTRAEP_EINVAL;
+  return rc(uep::launch_expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off,
+                                          block_w, n_block, act, y, type, status, stream));
 }
 
 }  // extern "C"

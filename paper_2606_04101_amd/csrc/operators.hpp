@@ -1,5 +1,5 @@
 // Launchers of the operators around the balancing path (router, combine's
-// backward pass, 8-bit expert products) and the numeric helpers they share.
+// backward pass, the experts' products) and the numeric helpers they share.
 // Internal header; the C ABI in operators.hip validates arguments and calls
 // these.
 #pragma once
@@ -45,6 +45,32 @@ hipError_t launch_expert_matmul(const int8_t *xq, const float *xs, int64_t M, co
                                 const int64_t *block_off, const int32_t *block_w, int32_t n_block,
                                 int32_t act, void *y, int32_t type, int32_t *status,
                                 hipStream_t stream);
+
+hipError_t launch_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_t *w, int32_t n_w,
+                                     int64_t w_stride, int32_t N, int32_t K, int32_t trans,
+                                     const int64_t *block_off, const int32_t *block_w,
+                                     int32_t n_block, int32_t act, uint16_t *pre, void *y,
+                                     int32_t type, int32_t *status, hipStream_t stream);
+size_t weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w);
+hipError_t launch_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M, int32_t N,
+                                     int32_t K, const int64_t *block_off, const int32_t *block_w,
+                                     int32_t n_block, int32_t n_w, int64_t dw_stride,
+                                     int32_t accumulate, void *dw, int32_t type, void *ws,
+                                     int32_t *status, hipStream_t stream);
+hipError_t launch_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
+                               uint8_t *q, int64_t ldq, uint8_t *scale, hipStream_t stream);
+hipError_t launch_expert_matmul_fp8(const uint8_t *xq, const uint8_t *xs, int64_t M,
+                                    const uint8_t *wq, const uint8_t *ws, int32_t n_w, int32_t N,
+                                    int32_t K, const int64_t *block_off, const int32_t *block_w,
+                                    int32_t n_block, int32_t act, void *y, int32_t type,
+                                    int32_t *status, hipStream_t stream);
+
+constexpr int kMaxBlocks = 2048;  // blocks of a call
+constexpr int kScaleBlock = 128;  // elements that share a scale in 8-bit floating point
+// bytes of a row's scales
+__host__ __device__ constexpr int scale_pitch(int64_t K) {
+  return static_cast<int>((K + 4 * kScaleBlock - 1) / (4 * kScaleBlock)) * 4;
+}
 
 __device__ __forceinline__ float bf16_at_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_at_high(uint32_t w) {
