@@ -607,7 +607,7 @@ int ultraep_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, i
  *   xq         [M][K] e4m3, x_scale [M][4 * ceil(K / 512)] bytes
  *   wq         [n_w][N][K] e4m3, w_scale [n_w][N][4 * ceil(K / 512)] bytes
  *   block_off, block_w, n_block, y, errors  as for ultraep_expert_matmul
- * K % 16 == 0, N % 8 == 0 (N % 16 == 0 with act), 16 <= K <= 2^20, 8 <= N <= 2^20,
+ * K % 16 == 0, N % 8 == 0 (N % 16 == 0 with act), 16 <= K <= 2^18, 8 <= N <= 2^20,
  * M < 2^31, M * N < 2^38; 16-byte aligned xq, wq and y, 4-byte aligned scales. */
 int ultraep_expert_matmul_fp8(const uint8_t *xq, const uint8_t *x_scale, int64_t M,
                               const uint8_t *wq, const uint8_t *w_scale, int32_t n_w, int32_t N,

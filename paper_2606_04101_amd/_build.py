@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libultraep.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["abi.hip", "count.hip", "plan.hip", "dispatch.hip", "pack.hip",
            "relay.hip", "combine.hip", "reduce.hip",
-           "operators.hip", "route.hip", "combine_grad.hip", "expert.hip", "products.hip",
+           "operators.hip", "route.hip", "combine_grad.hip", "expert.hip", "products_bf16.hip",
+           "products_trans.hip", "products_fp8.hip",
            "weight_grad.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -179,12 +179,6 @@ struct MatmulArgs {
   int32_t n_w, N, K, n_block, n_out;
 };
 
-// v / (1 + exp(-v)) by the hardware's exp2 and reciprocal: a relative error of
-// (|v| + 5) 2^-24 at most for v >= -87; below, where it is under 2e-36 in magnitude, it
-// becomes 0.  |v| 2^-24 is far below the rounding of the 8-bit operands; with
-// expf and a division the epilogue's arithmetic costs 65 us of 3350 at 131072 x 4096 x 7168.
-__device__ __forceinline__ float silu(float v) { return v * fast_rcp(1.f + fast_exp(-v)); }
-
 constexpr int kBk = 128;  // bytes of K of a step
 
 // Output tile of kN weight rows x kM rows, K in steps of 128 bytes through two

@@ -204,7 +204,7 @@ int ultraep_expert_matmul_fp8(const uint8_t *xq, const uint8_t *x_scale, int64_t
                               int32_t *status, hipStream_t stream) {
   if (!blocks_ok(M, n_w, block_off, n_block) || !type_ok(type) || !status) return ULTRAEP_EINVAL;
   if (act != ULTRAEP_NO_ACT && act != ULTRAEP_SWIGLU) return ULTRAEP_EINVAL;
-  if (!extent_ok(K, 16) || !extent_ok(N, act ? 16 : 8)) return ULTRAEP_EINVAL;
+  if (!extent_ok(K, 16) || K > 1 << 18 || !extent_ok(N, act ? 16 : 8)) return ULTRAEP_EINVAL;
   if (M * static_cast<int64_t>(N) >= int64_t(1) << 38) return ULTRAEP_EINVAL;
   if (!wq || !aligned16(wq) || !w_scale || !aligned4(w_scale)) return ULTRAEP_EINVAL;
   if (M == 0) return ULTRAEP_OK;

@@ -1,0 +1,621 @@
+// The tile loop of the floating-point products (bf16, and e4m3 with a scale for each 128
+// elements) and what they share.  Internal header.
+//
+// An output tile is kN "channels" x kM "rows": sums over a common index of channel side A
+// times row side B.  The matrix unit's first operand is A, so a lane holds 4 neighbouring
+// channels of one row.  Either side may lie with the common index contiguous, or (kTrans)
+// with its channels or rows contiguous; such a side is transposed on its way from LDS.
+//   The loop is the one of the 8-bit integer products: steps of 128 bytes of the common
+// index through two LDS buffers, loads straight to LDS two steps ahead, one barrier a
+// step, kWn x kWm waves that stay and take tile after tile, and (kAhead) the next tile's
+// first loads in flight while the results leave.
+#pragma once
+
+#include <type_traits>
+
+#include "operators.hpp"
+#include "tiles.hpp"
+
+namespace uep {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int32_t v8i __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+constexpr int kBk = 128;  // bytes of a step: of a contiguous side's row
+
+template <int N, int M, int Wn, int Wm, bool Ahead, bool Fp8, bool TransA, bool TransB>
+struct Tile {
+  static constexpr int kN = N, kM = M, kWn = Wn, kWm = Wm;
+  static constexpr bool kAhead = Ahead, kFp8 = Fp8, kTransA = TransA, kTransB = TransB;
+  static constexpr int kWaves = Wn * Wm, kThreads = kWaves * kWave;
+  static constexpr int kFn = N / Wn / 32, kFm = M / Wm / 32;  // 32 x 32 parts of a wave
+  static constexpr int kBuf = (N + M) * kBk;
+  static constexpr int kLoads = kBuf / 1024 / kWaves, kLoadsA = N / 8 / kWaves;  // of a wave in a step
+  static constexpr int kStep = Fp8 ? 128 : 64;  // elements of the common index in a step
+  static constexpr int kDepths = Fp8 ? 2 : 4;   // products of a pair of parts in a step
+  static constexpr int kScaleAt = 2 * kBuf + (Ahead ? kWaves * 4096 : 0);
+  static constexpr int kLds = kScaleAt + (Fp8 ? 2 * (N + M) * 4 : 0);
+  using Part = std::conditional_t<Fp8, v8i, v4i>;
+  static_assert(kLoadsA * kWaves * 8 == N && kWaves % 2 == 0, "whole loads of each side");
+  static_assert(Ahead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
+  static_assert(!Fp8 || !(TransA || TransB), "the transposing read is one of 16-bit elements");
+  // a transposed side's loads cover whole groups of 4 of the common index
+  static_assert(!(TransA || TransB) || kWaves * 512 / (N > M ? N : M) % 4 == 0, "");
+};
+
+// A transposed side of kW channels lies in LDS as the rows of its memory, kW * 2 bytes
+// each, chunk c (of 16 bytes) of row r at c ^ flip: the reads of 4 rows by 64 bytes that
+// half a wave makes meet all banks.
+template <int kW>
+__device__ __forceinline__ int flip(int r) {
+  return kW >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2;
+}
+
+// Work: the items and their addresses.
+//   next_item()      to the next one, false if there is none
+//   more(), advance()  whether it has a further step to load; pa, pa2, pb, left are that
+//                    step's: addresses of A (pa2: of load units for which second(unit)),
+//                    B, and elements of the common index (kStep, or fewer)
+//   row_a(j), row_b(j), pitch  of contiguous sides: memory row of tile row j, bytes a row
+//   chunk_a(c), chunk_b(c), pitch_a, pitch_b  of transposed sides: byte offset of tile
+//                    chunk c, bytes a row
+//   tail             elements of the last step;  kRagged: any step may have fewer
+//   out(), early(), results()  what the finished tile needs
+template <class S, class Work>
+__device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
+  using Part = typename S::Part;
+  constexpr int kFn = S::kFn, kFm = S::kFm, kLoads = S::kLoads, kLoadsA = S::kLoadsA;
+  constexpr int kWaves = S::kWaves, kBuf = S::kBuf, kDepths = S::kDepths;
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wn = wave % S::kWn, wm = wave / S::kWn;
+  const int lr = lane & 31, hi = lane >> 5;
+  const uint32_t lds0 = lds_address(s_lds);
+
+  // A wave's load of 1 KiB: of a contiguous side 8 rows of 8 chunks, chunk c of row r at
+  // c ^ (r / 2 % 8); of a transposed side whole rows.  This lane's chunk and, of a
+  // transposed side, row in the first load:
+  const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+  constexpr int kRowsA = 512 / S::kN, kRowsB = 512 / S::kM;  // of a load
+  const int first_a = wave * kRowsA + lane / (S::kN / 8);
+  const int first_b = wave * kRowsB + lane / (S::kM / 8);
+  uint32_t off[kLoads];
+  uint32_t at_a = 0, at_b = 0;  // of the lane's chunk in row 0 (transposed sides)
+  int left_now = 0, left_next = 0, left_load = 0;  // elements of this step, the next, the one loaded
+
+  auto aim = [&] {
+    const int l = opaque(lane);
+    const int c = (l & 7) ^ ((wave & 1) * 4 + (l >> 4));
+    if (S::kTransA) {
+      const int r = wave * kRowsA + l / (S::kN / 8);
+      at_a = work.chunk_a((l % (S::kN / 8)) ^ flip<S::kN>(r));
+#pragma unroll
+      for (int i = 0; i < kLoadsA; ++i) off[i] = at_a + (i * kWaves * kRowsA + r) * work.pitch_a;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoadsA; ++i)
+        off[i] = static_cast<uint32_t>(work.row_a((i * kWaves + wave) * 8 + (l >> 3))) * work.pitch + c * 16;
+    }
+    if (S::kTransB) {
+      const int r = wave * kRowsB + l / (S::kM / 8);
+      at_b = work.chunk_b((l % (S::kM / 8)) ^ flip<S::kM>(r));
+#pragma unroll
+      for (int i = kLoadsA; i < kLoads; ++i)
+        off[i] = at_b + ((i - kLoadsA) * kWaves * kRowsB + r) * work.pitch_b;
+    } else {
+#pragma unroll
+      for (int i = kLoadsA; i < kLoads; ++i)
+        off[i] = static_cast<uint32_t>(work.row_b(((i - kLoadsA) * kWaves + wave) * 8 + (l >> 3))) * work.pitch + c * 16;
+    }
+  };
+  // Load i of a step into buffer `slot`.  What lies past the step's elements is loaded
+  // from its first ones and not used.
+  auto issue = [&](int slot, int i) {
+    const bool a = i < kLoadsA;
+    uint32_t o;
+    if (a ? S::kTransA : S::kTransB) {
+      const int r = a ? i * kWaves * kRowsA + first_a : (i - kLoadsA) * kWaves * kRowsB + first_b;
+      o = r < left_load ? off[i] : a ? at_a : at_b;
+    } else {
+      o = off[i] - (chunk * (S::kStep / 8) >= left_load ? chunk * 16 : 0);
+    }
+    const int8_t *base = !a ? work.pb : work.second(i * kWaves + wave) ? work.pa2 : work.pa;
+    load_to_lds(uniform(base), o,
+                __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + (i * kWaves + wave) * 1024));
+  };
+  // (8-bit) the words that hold 4 steps' scales of every channel and row
+  auto issue_scales = [&](int group) {
+    constexpr int kAll = S::kN + S::kM;
+#pragma unroll
+    for (int i = 0; i < kAll; i += kWaves * kWave) {
+      const int j = i + wave * kWave;  // the same side for all lanes
+      if (j >= kAll) break;
+      load_word_to_lds(uniform(j < S::kN ? work.sa : work.sb), work.scale_at(j, lane) + group * 4,
+                       __builtin_amdgcn_readfirstlane(lds0 + S::kScaleAt + ((group & 1) * kAll + j) * 4));
+    }
+  };
+
+  int loaded = 0;  // steps of the item loaded at its beginning, up to 2
+  auto begin = [&] {
+    if (!work.next_item()) return false;
+    aim();
+    loaded = 0;
+    if (S::kFp8) issue_scales(0);
+    if (work.more()) {
+      work.advance();
+      left_now = left_load = work.left;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) issue(0, i);
+      loaded = 1;
+    }
+    if (work.more()) {
+      work.advance();
+      left_next = left_load = work.left;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) issue(1, i);
+      loaded = 2;
+    }
+    return true;
+  };
+  auto arrived = [&] {  // the first step's bytes are there
+    if (loaded == 2)
+      asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  };
+
+  // what this lane reads of a part: 16 (two times 16) bytes of the common index of one
+  // channel or row, from a transposed side by two reads that each hand 4 elements of 16
+  // channels, as they lie for 4 values of the index, to 16 lanes, one channel each
+  const int tr_row = (lane >> 2 & 3) + hi * 8;
+  const int tr_chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+  auto read = [&](auto trans, auto width, int side, int part, int slot, int kk) {
+    const int8_t *b = s_lds + slot * kBuf + side;
+    if constexpr (decltype(trans)::value) {
+      constexpr int kW = decltype(width)::value;
+      const int8_t *p = b + (kk * 16 + tr_row) * (kW * 2) +
+                        ((part * 4 + tr_chunk) ^ flip<kW>(lane >> 2)) * 16 + (lane & 1) * 8;
+      typedef __attribute__((address_space(3))) v4s *Lds;
+      const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p)));
+      const v2u up = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * kW * 2)));
+      return v4i{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(up.x), static_cast<int>(up.y)};
+    } else if constexpr (S::kFp8) {
+      const int8_t *p = b + (part * 32 + lr) * kBk;
+      const v4i lo = *reinterpret_cast<const v4i *>(p + ((kk * 4 + hi * 2) ^ (lr >> 1 & 7)) * 16);
+      const v4i up = *reinterpret_cast<const v4i *>(p + ((kk * 4 + hi * 2 + 1) ^ (lr >> 1 & 7)) * 16);
+      return __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const v4i *>(b + (part * 32 + lr) * kBk + ((kk * 2 + hi) ^ (lr >> 1 & 7)) * 16);
+    }
+  };
+
+  if (!begin()) return;
+  arrived();
+  while (true) {
+    asm volatile("s_barrier" : : : "memory");
+    v16f acc[kFn][kFm] = {};
+    Part fa[2][kFn], fb[2][kFm];
+    int scale[kFn + kFm], scale_next[kFn + kFm];
+    auto fetch = [&](int slot, int kk, int f) {
+      if (f < kFn)
+        fa[kk & 1][f] = read(std::bool_constant<S::kTransA>(), std::integral_constant<int, S::kN>(), 0,
+                             wn * kFn + f, slot, kk);
+      else
+        fb[kk & 1][f - kFn] = read(std::bool_constant<S::kTransB>(), std::integral_constant<int, S::kM>(),
+                                   S::kN * kBk, wm * kFm + f - kFn, slot, kk);
+    };
+    auto fetch_scales = [&](int group, int *to) {
+      const int8_t *b = s_lds + S::kScaleAt + (group & 1) * (S::kN + S::kM) * 4;
+#pragma unroll
+      for (int f = 0; f < kFn; ++f) to[f] = *reinterpret_cast<const int *>(b + ((wn * kFn + f) * 32 + lr) * 4);
+#pragma unroll
+      for (int f = 0; f < kFm; ++f)
+        to[kFn + f] = *reinterpret_cast<const int *>(b + (S::kN + (wm * kFm + f) * 32 + lr) * 4);
+    };
+    // the elements of a part past the step's `left` become 0 on both sides (0 times what
+    // lies there could be a NaN)
+    auto clear = [&](int kk, int left) {
+      const int mine = left - (S::kFp8 ? kk * 64 + hi * 32 : kk * 16 + hi * 8);
+      if constexpr (S::kFp8) {  // (whole chunks of 16)
+#pragma unroll
+        for (int f = 0; f < kFn + kFm; ++f) {
+          Part &p = f < kFn ? fa[kk & 1][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
+#pragma unroll
+          for (int d = 0; d < 8; ++d)
+            if (mine <= d / 4 * 16) p[d] = 0;
+        }
+      } else {
+        int keep[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) keep[d] = mine >= 2 * d + 2 ? -1 : mine == 2 * d + 1 ? 0xFFFF : 0;
+#pragma unroll
+        for (int f = 0; f < kFn + kFm; ++f) {
+          Part &p = f < kFn ? fa[kk & 1][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
+#pragma unroll
+          for (int d = 0; d < 4; ++d) p[d] &= keep[d];
+        }
+      }
+    };
+    // One step, its first parts already in registers.  Reads of the next parts, and at the
+    // step's end the loads of the step after the next, lie between the products.  kMore:
+    // how many steps follow, up to 2.
+    auto step = [&](int s, auto ahead) {
+      constexpr int kMore = decltype(ahead)::value;
+      const int slot = s & 1;
+#pragma unroll
+      for (int kk = 0; kk < kDepths; ++kk) {
+        if (kk == kDepths - 1) {  // the next step's bytes are there, and nobody reads this step's any more
+          if (kMore == 2) {
+            work.advance();
+            left_load = work.left;
+          }
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+          if (S::kFp8 && kMore > 0 && (s & 3) == 3) fetch_scales((s + 1) >> 2, scale_next);
+          if (S::kFp8 && kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
+        }
+        if (Work::kRagged) {
+          if (left_now < S::kStep) clear(kk, left_now);
+        } else if (kMore == 0) {
+          if (work.tail < (kk + 1) * (S::kStep / kDepths)) clear(kk, work.tail);
+        }
+        constexpr int kAll = kFn * kFm, kParts = kFn + kFm;
+#pragma unroll
+        for (int m = 0; m < kAll; ++m) {
+          const int i = m / kFm, j = m % kFm;
+          if constexpr (S::kFp8)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                fa[kk & 1][i], fb[kk & 1][j], acc[i][j], 0, 0, 0, scale[i], 0, scale[kFn + j]);
+          else
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(v8b, fa[kk & 1][i]), __builtin_bit_cast(v8b, fb[kk & 1][j]),
+                acc[i][j], 0, 0, 0);
+          // spread evenly over the products
+          for (int f = m * kParts / kAll; f < (m + 1) * kParts / kAll; ++f) {
+            if (kk < kDepths - 1) fetch(slot, kk + 1, f);
+            else if (kMore > 0) fetch(slot ^ 1, 0, f);
+          }
+          if (kk == kDepths - 1 && kMore == 2)
+            for (int f = m * kLoads / kAll; f < (m + 1) * kLoads / kAll; ++f) issue(slot, f);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      left_now = left_next;
+      left_next = left_load;
+      if (S::kFp8 && kMore > 0) {
+        if ((s & 3) == 3) {
+#pragma unroll
+          for (int f = 0; f < kFn + kFm; ++f) scale[f] = scale_next[f];
+        } else {
+#pragma unroll
+          for (int f = 0; f < kFn + kFm; ++f) scale[f] = static_cast<int>(static_cast<uint32_t>(scale[f]) >> 8);
+        }
+      }
+    };
+
+    if (loaded > 0) {
+#pragma unroll
+      for (int f = 0; f < kFn + kFm; ++f) fetch(0, 0, f);
+      if (S::kFp8) fetch_scales(0, scale);
+      int s = 0;
+      for (; work.more(); ++s) step(s, std::integral_constant<int, 2>());
+      if (loaded == 2) step(s++, std::integral_constant<int, 1>());
+      step(s, std::integral_constant<int, 0>());
+    }
+
+    const auto out = work.out();
+    typename Work::Early early;
+    work.early(out, early, wn, wm);
+    const bool more = S::kAhead && begin();
+    work.results(out, early, acc, s_lds + (S::kAhead ? 2 * kBuf : 0) + wave * 4096, wn, wm);
+    if (S::kAhead) {
+      if (!more) return;
+    } else {
+      __syncthreads();
+      if (!begin()) return;
+      arrived();
+    }
+  }
+}
+
+// Results of 32 rows x 64 channels (32 in fp32) leave through 4 KiB of LDS a wave, so that
+// a row's channels go out in whole lines.  A row's 16-byte slots are exchanged by the row.
+//   put: 4 neighbouring channels (q * 8 + eh * 4 on) of row er of the part at `half`
+//   get: the 16 bytes that lane el stores of row p * 8 + el / 8
+struct Stage {
+  int8_t *at;
+  int er, eh, el;
+  __device__ explicit Stage(int8_t *s) : at(s) {
+    el = opaque(lane_id());
+    er = el & 31;
+    eh = el >> 5;
+  }
+  __device__ void put(int half, int q, const float *v, std::true_type) const {
+    const int slot = (half * 4 + q) ^ (er & 7);
+    *reinterpret_cast<v2u *>(at + er * 128 + slot * 16 + eh * 8) = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  }
+  __device__ void put(int, int q, const float *v, std::false_type) const {
+    const int slot = (q * 2 + eh) ^ (er & 7);
+    *reinterpret_cast<v4f *>(at + er * 128 + slot * 16) = v4f{v[0], v[1], v[2], v[3]};
+  }
+  __device__ int row(int p) const { return p * 8 + el / 8; }
+  template <class V>
+  __device__ V get(int p) const {
+    const int r = row(p);
+    return *reinterpret_cast<const V *>(at + r * 128 + ((el & 7) ^ (r & 7)) * 16);
+  }
+};
+
+// ---------------------------------------------------------------- the products
+
+struct ProductArgs {
+  const int8_t *x, *w;    // elements
+  const int8_t *xs, *ws;  // (8-bit) scales
+  const int64_t *block_off;
+  const int32_t *block_w;
+  uint16_t *pre;
+  void *y;
+  int32_t *status;
+  int64_t M, w_stride;  // (w_stride in elements)
+  int32_t n_w, N, K, n_block;
+  int32_t n_out;  // channels of v that items are cut from: N, or with SwiGLU N / 2
+};
+
+// gradients of silu(a) * b with respect to a and b, from v, that of its value; s and 1 - s
+// as e^-a / (1 + e^-a), without cancellation or overflow
+__device__ __forceinline__ void swiglu_grad(float v, float a, float b, float &da, float &db) {
+  const float e = fast_exp(-a), s = fast_rcp(1.f + e), rest = e > 0x1p100f ? 1.f : e * s;
+  da = v * b * s * (1.f + a * rest);
+  db = v * a * s;
+}
+
+// Items item, item + stride, .. below n_item, item 0 being that numbered `first`.  An item
+// is a tile that `tiles` numbers, or (kPart = 2) a quarter of one, 2 x 2.  With SwiGLU a
+// wave's parts of 32 channels alternate between gates and their partners, so that a gate's
+// sum meets its partner's in the same lane.
+template <class S, int kPart, int kAct, bool kBf16>
+struct ProductWork {
+  static constexpr bool kRagged = false, kGlu = kAct == ULTRAEP_SWIGLU;
+  static constexpr int kOut = kGlu ? S::kN / 2 : S::kN;  // channels of an item
+  static constexpr int kOutW = kOut / S::kWn;            // of a wave
+  static constexpr int kEsize = S::kFp8 ? 1 : 2;
+  static_assert(!kGlu || S::kFn % 2 == 0, "a wave has gates with their partners");
+
+  const ProductArgs &a;
+  RowTiles<S::kM * kPart> &tiles;
+  const int n_col, first, stride, n_item;
+  int item;
+  RowTile tile;
+  int n0, half, tail, left, to_load;
+  const int8_t *pa, *pa2, *pb, *sa, *sb;
+  uint32_t pitch, pitch_a;
+  static constexpr uint32_t pitch_b = 0;
+
+  __device__ ProductWork(const ProductArgs &args, RowTiles<S::kM * kPart> &t, int col, int f, int i, int st, int n)
+      : a(args), tiles(t), n_col(col), first(f), stride(st), n_item(n), item(i) {
+    half = a.N / 2;
+    pitch = a.K * kEsize;
+    pitch_a = a.N * 2;
+    tail = a.K - (a.K - 1) / S::kStep * S::kStep;
+  }
+  // false for a quarter that has no rows or no channels
+  __device__ bool aim(int id) {
+    const int it = first + id / (kPart * kPart), part = id % (kPart * kPart);
+    constexpr int kGroup = 8;  // 8 row tiles by all columns at a time
+    const int group = it / (kGroup * n_col), rest = it - group * kGroup * n_col;
+    const int high = min(kGroup, tiles.total - group * kGroup);
+    tile = tiles.find(a, group * kGroup + rest % high);
+    n0 = (rest / high * kPart + part / kPart) * kOut;
+    if (kPart > 1) {
+      tile.row += part % kPart * S::kM;
+      tile.rows = min(tile.rows - part % kPart * S::kM, S::kM);
+      return tile.rows > 0 && n0 < a.n_out;
+    }
+    return true;
+  }
+  __device__ bool next_item() {
+    while (true) {
+      if (item >= n_item) return false;
+      const int id = item;
+      item += stride;
+      if (aim(id)) break;
+    }
+    const int64_t at = tile.w * a.w_stride;
+    pa = uniform(a.w + (S::kTransA ? at + n0 : at + static_cast<int64_t>(n0) * a.K) * kEsize);
+    pa2 = pa + static_cast<int64_t>(half) * a.K * kEsize;  // (contiguous) the gates' partners
+    pb = uniform(a.x + tile.row * a.K * kEsize);
+    if (S::kFp8) {
+      const int p = scale_pitch(a.K);
+      sa = uniform(a.ws + (static_cast<int64_t>(tile.w) * a.N + n0) * p);
+      sb = uniform(a.xs + tile.row * p);
+    }
+    to_load = (a.K + S::kStep - 1) / S::kStep;
+    started = false;
+    return true;
+  }
+  bool started;
+  __device__ bool more() const { return to_load > 0; }
+  __device__ void advance() {
+    if (started) {
+      const int64_t d = S::kTransA ? static_cast<int64_t>(S::kStep) * a.N * 2 : kBk;
+      pa = uniform(pa + d);
+      if (kGlu) pa2 = uniform(pa2 + d);
+      pb = uniform(pb + kBk);
+    }
+    started = true;
+    left = --to_load == 0 ? tail : S::kStep;
+  }
+  // memory rows and chunks of the tile's, in range for any j and c
+  __device__ int row_a(int j) const {
+    return kGlu ? min(j / 64 * 32 + j % 32, half - 1 - n0) : min(j, a.N - 1 - n0);
+  }
+  __device__ int row_b(int j) const { return min(j, tile.rows - 1); }
+  __device__ bool second(int unit) const { return kGlu && !S::kTransA && unit * 8 < S::kN && unit * 8 % 64 >= 32; }
+  __device__ uint32_t chunk_a(int c) const {
+    const int j = c * 8;
+    return 2 * (kGlu ? min(j / 64 * 32 + j % 32, half - 8 - n0) + (j % 64 >= 32 ? half : 0) : min(j, a.N - 8 - n0));
+  }
+  __device__ uint32_t chunk_b(int) const { return 0; }
+  __device__ uint32_t scale_at(int j, int lane) const {
+    const int r = j >= S::kN ? row_b(j - S::kN + lane) : row_a(j + lane) + (kGlu && lane >= 32 ? half : 0);
+    return static_cast<uint32_t>(r) * scale_pitch(a.K);
+  }
+
+  struct Out {
+    int64_t row;
+    int rows, n0;
+  };
+  __device__ Out out() const { return {tile.row, tile.rows, n0}; }
+
+  // (the gradient of SwiGLU) the gates and partners of a part, of the next one while one
+  // is worked on
+  struct Kept {
+    v2u g[2][4], u[2][4];
+  };
+  struct Nothing {};
+  using Early = std::conditional_t<kAct == ULTRAEP_SWIGLU_GRAD, Kept, Nothing>;
+  __device__ void keep(const Out &o, Early &k, int n, int wn, int wm) const {
+    if constexpr (kAct == ULTRAEP_SWIGLU_GRAD) {
+      const int el = opaque(lane_id());
+      const int c = o.n0 + wn * kOutW + n % S::kFn * 32 + (el & 7) * 4;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int r = (wm * S::kFm + n / S::kFn) * 32 + p * 8 + el / 8;
+        k.g[n & 1][p] = k.u[n & 1][p] = v2u{0, 0};
+        if (r < o.rows && c < a.N) {
+          const uint16_t *at = a.pre + (o.row + r) * 2 * a.N + c;
+          k.g[n & 1][p] = *reinterpret_cast<const v2u *>(at);
+          k.u[n & 1][p] = *reinterpret_cast<const v2u *>(at + a.N);
+        }
+      }
+    }
+  }
+  __device__ void early(const Out &o, Early &k, int wn, int wm) const { keep(o, k, 0, wn, wm); }
+
+  template <class Acc>
+  __device__ void results(const Out &o, Early &kept, Acc &acc, int8_t *lds, int wn, int wm) const {
+    const Stage st(lds);
+    constexpr int kFn = S::kFn, kFm = S::kFm, kSize = kBf16 ? 2 : 4;
+    constexpr int kParts = kOutW / 32, kGroup = kBf16 ? 2 : 1;  // parts that the stage takes
+    const int nw = o.n0 + wn * kOutW, limit = min(a.n_out, nw + kOutW);
+    char *const y = static_cast<char *>(a.y);
+#pragma unroll
+    for (int j = 0; j < kFm; ++j) {
+      const int r0 = (wm * kFm + j) * 32;
+      // the sums stay in the accumulation registers until here
+#pragma unroll
+      for (int i = 0; i < kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
+      // before the last stores: all loads, and the earlier stores, are done
+      if (S::kAhead && j == kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      else asm volatile("" : : : "memory");
+      // the stage's channels to rows of ld elements, from channel c0 on, below `end`
+      auto leave = [&](char *dst, int64_t ld, int size, int c0, int end) {
+        const int c = c0 + (st.el & 7) * (16 / size);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int r = r0 + st.row(p);
+          const v4u v = st.get<v4u>(p);
+          if (r < o.rows && c < end)
+            __builtin_nontemporal_store(v, reinterpret_cast<v4u *>(dst + ((o.row + r) * ld + c) * size));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto put = [&](auto bf16, int h, int q, auto value) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = value(q * 4 + e);
+        st.put(h, q, v, bf16);
+      };
+      if constexpr (kAct == ULTRAEP_SWIGLU_GRAD) {
+#pragma unroll
+        for (int i = 0; i < kFn; ++i) {
+          const int n = j * kFn + i, c = nw + i * 32 + (st.el & 7) * 4;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            put(std::false_type(), 0, q, [&](int e) { return acc[i][j][e]; });
+          if (n + 1 < kFn * kFm) keep(o, kept, n + 1, wn, wm);
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const int r = r0 + st.row(p);
+            const v4f v = st.get<v4f>(p);
+            const v2u g = kept.g[n & 1][p], u = kept.u[n & 1][p];
+            float da[4], db[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              swiglu_grad(v[e], e % 2 ? bf16_at_high(g[e / 2]) : bf16_at_low(g[e / 2]),
+                          e % 2 ? bf16_at_high(u[e / 2]) : bf16_at_low(u[e / 2]), da[e], db[e]);
+            if (r < o.rows && c < limit) {
+              char *at = y + ((o.row + r) * 2 * a.N + c) * kSize, *at2 = at + static_cast<int64_t>(a.N) * kSize;
+              if (kBf16) {
+                __builtin_nontemporal_store(v2u{pack_bf16(da[0], da[1]), pack_bf16(da[2], da[3])}, reinterpret_cast<v2u *>(at));
+                __builtin_nontemporal_store(v2u{pack_bf16(db[0], db[1]), pack_bf16(db[2], db[3])}, reinterpret_cast<v2u *>(at2));
+              } else {
+                __builtin_nontemporal_store(v4f{da[0], da[1], da[2], da[3]}, reinterpret_cast<v4f *>(at));
+                __builtin_nontemporal_store(v4f{db[0], db[1], db[2], db[3]}, reinterpret_cast<v4f *>(at2));
+              }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        continue;
+      }
+      if constexpr (kGlu && !S::kFp8) {
+        if (a.pre) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s)  // gates, partners
+#pragma unroll
+            for (int i = 0; i < kParts; i += 2) {
+#pragma unroll
+              for (int h = 0; h < 2 && i + h < kParts; ++h)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                  put(std::true_type(), h, q, [&](int e) { return acc[2 * (i + h) + s][j][e]; });
+              leave(reinterpret_cast<char *>(a.pre), a.N, 2, s * half + nw + i * 32, s * half + limit);
+            }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kParts; i += kGroup) {
+#pragma unroll
+        for (int h = 0; h < kGroup && i + h < kParts; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int f = kGlu ? 2 * (i + h) : i + h;
+            put(std::bool_constant<kBf16>(), h, q, [&](int e) {
+              return kGlu ? silu(acc[f][j][e]) * acc[kGlu ? f + 1 : f][j][e] : acc[f][j][e];
+            });
+          }
+        leave(y, a.n_out, kSize, nw + i * 32, limit);
+      }
+    }
+  }
+};
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kFp8, bool kTrans, int kAct, bool kBf16>
+__global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32_t n_col) {
+  using S = Tile<kN, kM, kWn, kWm, kAhead, kFp8, kTrans, false>;
+  __shared__ __align__(1024) int8_t s_lds[S::kLds];
+  __shared__ int s_run[32];
+  RowTiles<kM> tiles;
+  tiles.count(a, s_run, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), S::kWaves);
+  const int n_item = tiles.total * n_col;  // (fewer than 2^31: M * N < 2^38)
+  // the workgroups of one XCD (those of equal number modulo 8) take neighbouring items
+  constexpr int kXcd = 8;
+  const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
+  const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
+  int last = 0;  // tiles of the last round that are taken by quarters
+  if (kAhead && n_item % grid * 4 <= grid) last = n_item % grid;
+  {
+    ProductWork<S, 1, kAct, kBf16> work(a, tiles, n_col, 0, slot, grid, n_item - last);
+    tile_items<S>(work, s_lds);
+  }
+  if constexpr (kAhead) {
+    __syncthreads();
+    using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, kFp8, kTrans, false>;
+    ProductWork<Q, 2, kAct, kBf16> work(a, tiles, n_col, n_item - last, slot, grid, last * 4);
+    tile_items<Q>(work, s_lds);
+  }
+}
+
+}  // namespace uep

@@ -1,0 +1,247 @@
+// The floating-point products of few rows a block.  Internal header.
+#pragma once
+
+#include "products.hpp"
+
+namespace uep {
+
+// Few rows a block: the weight's bytes bound the call.  A workgroup takes kRows weight
+// rows (with SwiGLU half of them gates, then their partners) and up to kTok rows; its waves
+// share K in steps of 128 bytes in turn, each through an LDS ring of its own that kDeep
+// steps fill, so no wave waits for another until they add their sums.
+template <int kTok, int kRows, int kWaves, int kDeep, bool kFp8, int kAct, bool kBf16>
+__global__ void __launch_bounds__(64 * kWaves) k_product_thin(ProductArgs a, int32_t n_col) {
+  constexpr bool kGlu = kAct == ULTRAEP_SWIGLU;
+  constexpr int kThreads = 64 * kWaves, kFm = kTok / 16, kFn = kRows / 16, kEsize = kFp8 ? 1 : 2;
+  constexpr int kOut = kGlu ? kRows / 2 : kRows;
+  constexpr int kPitch = kRows + 4;          // words of a row's sums
+  constexpr int kScales = kFp8 ? 2 : 0;      // loads of a step's scales
+  constexpr int kScaleAt = (kRows + kTok) * kBk;
+  constexpr int kStep = kScaleAt + kScales * 256;
+  constexpr int kLoadsN = kRows / 8, kLoads = (kRows + kTok) / 8;
+  constexpr int kRing = kDeep * kStep;
+  static_assert(kTok * kPitch * 4 <= kRing, "a wave's sums take the place of its ring");
+  static_assert(kRows <= 64 && kTok <= 64, "one load takes a side's scales");
+  __shared__ __align__(1024) int8_t s_ring[kWaves][kRing];
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lr = lane & 15, lc = lane >> 4;
+  const int half = a.N / 2;
+  RowTiles<kTok> tiles;
+  tiles.count(a, reinterpret_cast<int *>(s_ring[0]), wave, kWaves);
+  const int n_item = tiles.total * n_col;
+  const int n_chunk = a.K * kEsize / 16, steps = (a.K * kEsize + kBk - 1) / kBk;
+  const int scale_row = scale_pitch(a.K);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(&s_ring[wave][0]));
+
+  for (int item = blockIdx.x; item < n_item; item += gridDim.x) {
+    const RowTile tile = tiles.find(a, item / n_col);
+    const int n0 = item % n_col * kOut;
+    const int8_t *w = uniform(a.w + (tile.w * a.w_stride + static_cast<int64_t>(n0) * a.K) * kEsize);
+    const int8_t *w2 = w + static_cast<int64_t>(half) * a.K * kEsize;  // the gates' partners
+    const int8_t *x = uniform(a.x + tile.row * a.K * kEsize);
+    // the weight row, after n0 (of gates or partners), and the row of a row of the tile
+    auto weight_row = [&](int j) { return kGlu ? min(j % kOut, half - 1 - n0) : min(j, a.N - 1 - n0); };
+    auto row = [&](int j) { return min(j, tile.rows - 1); };
+    // byte offsets of this lane's rows: 8 rows of 8 chunks an instruction, chunk c of
+    // row r at c ^ (r / 2 % 8)
+    uint32_t off[kLoads], off_ws = 0, off_xs = 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int j = (i < kLoadsN ? i : i - kLoadsN) * 8 + (lane >> 3);
+      off[i] = static_cast<uint32_t>(i >= kLoadsN ? row(j) : weight_row(j)) * (a.K * kEsize);
+    }
+    const int8_t *ws = nullptr, *xs = nullptr;
+    if (kFp8) {
+      ws = uniform(a.ws + (static_cast<int64_t>(tile.w) * a.N + n0) * scale_row);
+      xs = uniform(a.xs + tile.row * scale_row);
+      const int j = min(lane, kRows - 1);
+      off_ws = static_cast<uint32_t>(weight_row(j) + (kGlu && j >= kOut ? half : 0)) * scale_row;
+      off_xs = static_cast<uint32_t>(row(min(lane, kTok - 1))) * scale_row;
+    }
+    // step s of the wave into part `slot` of the ring; what lies past K is loaded from its
+    // last chunk and not used
+    const int chunk = (lane & 7) ^ (lane >> 4);
+    auto issue = [&](int s, int slot) {
+      const uint32_t at[2] = {min(s * 8 + chunk, n_chunk - 1) * 16u, min(s * 8 + (chunk ^ 4), n_chunk - 1) * 16u};
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        load_to_lds(i >= kLoadsN ? x : kGlu && i >= kLoadsN / 2 ? w2 : w, off[i] + at[i & 1],
+                    __builtin_amdgcn_readfirstlane(lds0 + slot * kStep + i * 1024));
+      if (kFp8) {  // the words that hold the step's scales
+        const uint32_t word = min(s >> 2, scale_row / 4 - 1) * 4u;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + slot * kStep + kScaleAt);
+        load_word_to_lds(ws, off_ws + word, to);
+        load_word_to_lds(xs, off_xs + word, to + 256);
+      }
+    };
+
+    v4f acc[kFn][kFm] = {};
+#pragma unroll
+    for (int b = 0; b < kDeep; ++b) issue(wave + b * kWaves, b);
+    for (int s0 = wave; s0 < steps; s0 += kDeep * kWaves) {
+#pragma unroll
+      for (int b = 0; b < kDeep; ++b) {
+        const int s = s0 + b * kWaves;
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kDeep - 1) * (kLoads + kScales)) : "memory");
+        const int8_t *part = s_ring[wave] + b * kStep;
+        v4i fw[2][kFn], fx[2][kFm];
+        int sw[kFn], sx[kFm];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = lr * kBk + ((h * 4 + lc) ^ (lr >> 1)) * 16;
+#pragma unroll
+          for (int i = 0; i < kFn; ++i) fw[h][i] = *reinterpret_cast<const v4i *>(part + i * 16 * kBk + at);
+#pragma unroll
+          for (int j = 0; j < kFm; ++j) fx[h][j] = *reinterpret_cast<const v4i *>(part + (kRows + j * 16) * kBk + at);
+        }
+        if (kFp8) {
+#pragma unroll
+          for (int i = 0; i < kFn; ++i)
+            sw[i] = *reinterpret_cast<const uint8_t *>(part + kScaleAt + (i * 16 + lr) * 4 + (s & 3));
+#pragma unroll
+          for (int j = 0; j < kFm; ++j)
+            sx[j] = *reinterpret_cast<const uint8_t *>(part + kScaleAt + 256 + (j * 16 + lr) * 4 + (s & 3));
+        }
+        if (s * 8 + 8 > n_chunk) {
+          // past K (or a step past the last) both sides are 0: 0 times what was loaded
+          // could be a NaN
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (s * 8 + h * 4 + lc >= n_chunk) {
+#pragma unroll
+              for (int i = 0; i < kFn; ++i) fw[h][i] = v4i{0, 0, 0, 0};
+#pragma unroll
+              for (int j = 0; j < kFm; ++j) fx[h][j] = v4i{0, 0, 0, 0};
+            }
+          if (kFp8 && s >= steps) {  // (nor may a scale be a NaN)
+#pragma unroll
+            for (int i = 0; i < kFn; ++i) sw[i] = 127;
+#pragma unroll
+            for (int j = 0; j < kFm; ++j) sx[j] = 127;
+          }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the part is free
+        issue(s + kDeep * kWaves, b);
+        if constexpr (kFp8) {
+#pragma unroll
+          for (int j = 0; j < kFm; ++j)
+#pragma unroll
+            for (int i = 0; i < kFn; ++i)
+              acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                  __builtin_shufflevector(fw[0][i], fw[1][i], 0, 1, 2, 3, 4, 5, 6, 7),
+                  __builtin_shufflevector(fx[0][j], fx[1][j], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], 0, 0, 0,
+                  sw[i], 0, sx[j]);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < kFm; ++j)
+#pragma unroll
+              for (int i = 0; i < kFn; ++i)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(v8b, fw[h][i]), __builtin_bit_cast(v8b, fx[h][j]), acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+
+    // lane: row lr of a 16 x 16 part, weight rows 4 lc ..
+    float *sums = reinterpret_cast<float *>(s_ring[wave]);
+#pragma unroll
+    for (int i = 0; i < kFn; ++i)
+#pragma unroll
+      for (int j = 0; j < kFm; ++j)
+        *reinterpret_cast<v4f *>(sums + (j * 16 + lr) * kPitch + i * 16 + lc * 4) = acc[i][j];
+    __syncthreads();
+    for (int o = tid; o < kTok * kOut / 4; o += kThreads) {  // four channels of a row
+      const int r = o / (kOut / 4), c = o % (kOut / 4) * 4, n = n0 + c;
+      if (r >= tile.rows || n >= a.n_out) continue;
+      auto total = [&](int at) {  // of four of the row's channels, the waves in order
+        v4f sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < kWaves; ++u)
+          sum += *reinterpret_cast<const v4f *>(reinterpret_cast<float *>(s_ring[u]) + r * kPitch + at);
+        return sum;
+      };
+      auto packed = [](v4f v) { return v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; };
+      v4f v = total(c);
+      const int64_t m = tile.row + r;
+      if (kGlu) {
+        const v4f up = total(c + kOut);
+        if (!kFp8 && a.pre) {
+          *reinterpret_cast<v2u *>(a.pre + m * a.N + n) = packed(v);
+          *reinterpret_cast<v2u *>(a.pre + m * a.N + half + n) = packed(up);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * up[e];
+      }
+      char *out = static_cast<char *>(a.y) + (m * a.n_out + n) * (kBf16 ? 2 : 4);
+      if (kBf16) *reinterpret_cast<v2u *>(out) = packed(v);
+      else *reinterpret_cast<v4f *>(out) = v;
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------- launching
+
+// most row tiles that M rows in n_block blocks make: every block that has rows may
+// end in a part of a tile
+inline int64_t most_tiles(const ProductArgs &a, int tile_rows) {
+  return a.M / tile_rows + (a.M < a.n_block ? a.M : a.n_block);
+}
+
+template <int kTok, int kRows, int kWaves, int kDeep, bool kFp8, int kAct, bool kBf16>
+void start_thin(const ProductArgs &a, hipStream_t stream) {
+  const int out = kAct == ULTRAEP_SWIGLU ? kRows / 2 : kRows;
+  const int32_t n_col = (a.n_out + out - 1) / out;
+  const int64_t items = most_tiles(a, kTok) * n_col;
+  const dim3 grid(static_cast<unsigned>(items < 1 << 16 ? items : 1 << 16)), block(64 * kWaves);
+  hipLaunchKernelGGL((k_product_thin<kTok, kRows, kWaves, kDeep, kFp8, kAct, kBf16>), grid, block, 0, stream, a, n_col);
+}
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kFp8, bool kTrans, int kAct, bool kBf16>
+void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
+  const int out = kAct == ULTRAEP_SWIGLU ? kN / 2 : kN;
+  const int32_t n_col = (a.n_out + out - 1) / out;
+  const int64_t items = most_tiles(a, kM) * n_col;
+  const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
+  hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kFp8, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
+}
+
+template <bool kFp8, bool kTrans, int kAct, bool kBf16>
+void choose_product(const ProductArgs &a, hipStream_t stream) {
+  const int64_t blocks = a.M < a.n_block ? a.M : a.n_block, rows = (a.M + blocks - 1) / blocks;
+  auto items = [&](int64_t tile_rows, int64_t channels) {
+    return (blocks > 1 ? a.M / tile_rows + (blocks + 1) / 2 : (a.M + tile_rows - 1) / tile_rows) *
+           ((a.N + channels - 1) / channels);
+  };
+  const int64_t big = items(256, 256), full = big / 256, last = big % 256;
+  const int64_t big_time = full * 10 + (last == 0 ? 0 : full && last <= 64 ? 4 : 10);
+  const int64_t mid_time = (items(128, 128) + 511) / 512 * 6;
+  constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
+  if (rows > 64 && big_time < mid_time)
+    return start_product<256, 256, 2, 2, true, kFp8, kTrans, kAct, kBf16>(a, 256, stream);
+  if (rows > 56 && items(128, 128) >= 256)
+    return start_product<128, 128, 2, 2, false, kFp8, kTrans, kAct, kBf16>(a, 512, stream);
+  if (!kThin || (rows > 32 && items(64, 128) >= 320))
+    return start_product<128, 64, 2, 1, false, kFp8, kTrans, kAct, kBf16>(a, 768, stream);
+  if constexpr (kThin) {
+    const bool deep = static_cast<int64_t>(a.K) * (kFp8 ? 1 : 2) >= 4096;
+    if (rows > 32 && items(64, 64) >= 256 && deep) start_thin<64, 64, 4, 2, kFp8, kAct, kBf16>(a, stream);
+    else if (rows > 32 && items(64, 64) >= 256) start_thin<64, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
+    else if (rows > 12 && items(32, 64) >= 256 && deep) start_thin<32, 64, 4, 2, kFp8, kAct, kBf16>(a, stream);
+    else if (rows > 12 && items(32, 64) >= 256) start_thin<32, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
+    else if (deep) start_thin<16, 32, 4, 2, kFp8, kAct, kBf16>(a, stream);
+    else start_thin<16, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
+  }
+}
+
+template <bool kFp8, bool kTrans, int kAct>
+void choose_type(const ProductArgs &a, int32_t type, hipStream_t stream) {
+  if (type == ULTRAEP_BF16) choose_product<kFp8, kTrans, kAct, true>(a, stream);
+  else choose_product<kFp8, kTrans, kAct, false>(a, stream);
+}
+
+}  // namespace uep

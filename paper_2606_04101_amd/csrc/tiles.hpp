@@ -1,5 +1,5 @@
-// Tiles of rows over the blocks of a dispatch, and loads straight into LDS: what the
-// experts' products share.  Internal header.
+// Tiles of rows over the blocks of a dispatch, loads straight into LDS, and SwiGLU's
+// activation: what the experts' products share.  Internal header.
 #pragma once
 
 #include "operators.hpp"
@@ -127,5 +127,12 @@ template <class T>
 __device__ __forceinline__ uint32_t lds_address(T *p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) T *)p));
 }
+
+// v / (1 + exp(-v)) by the hardware's exp2 and reciprocal: a relative error of
+// (|v| + 5) 2^-24 at most for v >= -87; below, where it is under 2e-36 in magnitude, it
+// becomes 0.  |v| 2^-24 is far below the rounding of 8-bit operands or of a bf16 result;
+// with expf and a division the epilogue's arithmetic costs 65 us of 3350 at
+// 131072 x 4096 x 7168 in 8-bit integers.
+__device__ __forceinline__ float silu(float v) { return v * fast_rcp(1.f + fast_exp(-v)); }
 
 }  // namespace uep
