@@ -25,8 +25,16 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kBk = 128;  // bytes of a step: of a contiguous side's row
 
-template <int N, int M, int Wn, int Wm, bool Ahead, bool Fp8, bool TransA, bool TransB>
+// How the products are made: of bf16; of e4m3 by the matrix unit's own 8-bit products; or of
+// e4m3 taken to bf16.  The unit cuts the products of 8 neighbouring elements 13 bits below
+// the largest's exponent before it adds them, so its sums of 8-bit products are off by about
+// 1.5e-5 of the result: nothing where that is rounded to bf16 (2^-9), but too much for an
+// fp32 result, which kMathWide makes of exact products summed in fp32, at half the rate.
+enum Math { kMath16, kMath8, kMathWide };
+
+template <int N, int M, int Wn, int Wm, bool Ahead, Math Kind, bool TransA, bool TransB>
 struct Tile {
+  static constexpr bool Fp8 = Kind != kMath16, kWide = Kind == kMathWide;
   static constexpr int kN = N, kM = M, kWn = Wn, kWm = Wm;
   static constexpr bool kAhead = Ahead, kFp8 = Fp8, kTransA = TransA, kTransB = TransB;
   static constexpr int kWaves = Wn * Wm, kThreads = kWaves * kWave;
@@ -37,6 +45,7 @@ struct Tile {
   static constexpr int kDepths = Fp8 ? 2 : 4;   // products of a pair of parts in a step
   static constexpr int kScaleAt = 2 * kBuf + (Ahead ? kWaves * 4096 : 0);
   static constexpr int kLds = kScaleAt + (Fp8 ? 2 * (N + M) * 4 : 0);
+  static constexpr Math kKind = Kind;
   using Part = std::conditional_t<Fp8, v8i, v4i>;
   static_assert(kLoadsA * kWaves * 8 == N && kWaves % 2 == 0, "whole loads of each side");
   static_assert(Ahead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
@@ -51,6 +60,38 @@ struct Tile {
 template <int kW>
 __device__ __forceinline__ int flip(int r) {
   return kW >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2;
+}
+
+// (kMathWide) 8 elements of 8 bits with their scale as bf16.  An e4m3 times a power of two
+// is one exactly, from 2^-126 on.
+__device__ __forceinline__ v4i widen8(int lo, int up, float scale) {
+  typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+  auto two = [&](v2b v) { return __builtin_bit_cast(int, v); };
+  return v4i{two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+             two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+             two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(up, scale, false)),
+             two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(up, scale, true))};
+}
+// the scale of a byte: its bits are an fp32's exponent; a NaN's byte gives a NaN
+__device__ __forceinline__ float scale_value(int byte) {
+  byte &= 255;
+  return byte == 255 ? __builtin_nanf("") : __int_as_float(byte << 23);
+}
+// c + a b for 32 x 32 parts over 16 elements of bf16, or 64 of 8 bits with their scales
+template <Math kKind>
+__device__ __forceinline__ v16f multiply(const v4i &a, int, const v4i &b, int, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+}
+template <Math kKind>
+__device__ __forceinline__ v16f multiply(const v8i &a, int scale_a, const v8i &b, int scale_b, v16f c) {
+  if constexpr (kKind == kMath8)
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+  const float sa = scale_value(scale_a), sb = scale_value(scale_b);
+#pragma unroll
+  for (int d = 0; d < 8; d += 2)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, widen8(a[d], a[d + 1], sa)),
+                                                __builtin_bit_cast(v8b, widen8(b[d], b[d + 1], sb)), c, 0, 0, 0);
+  return c;
 }
 
 // Work: the items and their addresses.
@@ -122,7 +163,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       o = off[i] - (chunk * (S::kStep / 8) >= left_load ? chunk * 16 : 0);
     }
     const int8_t *base = !a ? work.pb : work.second(i * kWaves + wave) ? work.pa2 : work.pa;
-    load_to_lds(uniform(base), o,
+    load_to_lds(base, o,
                 __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + (i * kWaves + wave) * 1024));
   };
   // (8-bit) the words that hold 4 steps' scales of every channel and row
@@ -166,28 +207,35 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   };
 
-  // what this lane reads of a part: 16 (two times 16) bytes of the common index of one
-  // channel or row, from a transposed side by two reads that each hand 4 elements of 16
-  // channels, as they lie for 4 values of the index, to 16 lanes, one channel each
+  // What this lane reads of a part: 16 (two times 16) bytes of the common index of one
+  // channel or row; from a transposed side by two reads that each hand 4 elements of 16
+  // channels, as they lie for 4 values of the index, to 16 lanes, one channel each.  Where
+  // of the buffer: of the wave's first part at the first depth; the other parts' and
+  // depths' differ in some bits, or are so much further on.
+  constexpr int kBits = S::kFp8 ? 5 : 4;  // (bytes of a lane's elements of one depth)
   const int tr_row = (lane >> 2 & 3) + hi * 8;
-  const int tr_chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-  auto read = [&](auto trans, auto width, int side, int part, int slot, int kk) {
-    const int8_t *b = s_lds + slot * kBuf + side;
+  auto lane_at = [&](bool trans, int width, int part) {
+    const int across = (lane >> 4 & 1) * 32 + (lane >> 1 & 1) * 16 + (lane & 1) * 8;
+    const int turned = (width >= 128 ? lane >> 2 & 3 : lane >> 3 & 1) * 64;
+    if (trans) return tr_row * width * 2 + (across ^ turned ^ part * 64);
+    return (part * 32 + lr) * kBk + ((hi << kBits) ^ (lr >> 1 & 7) << 4);
+  };
+  int from_a = lane_at(S::kTransA, S::kN, wn * kFn);
+  int from_b = S::kN * kBk + lane_at(S::kTransB, S::kM, wm * kFm);
+  auto read = [&](auto trans, auto width, int from, int f, int slot, int kk) {
+    constexpr int kW = decltype(width)::value;
     if constexpr (decltype(trans)::value) {
-      constexpr int kW = decltype(width)::value;
-      const int8_t *p = b + (kk * 16 + tr_row) * (kW * 2) +
-                        ((part * 4 + tr_chunk) ^ flip<kW>(lane >> 2)) * 16 + (lane & 1) * 8;
+      const int8_t *p = s_lds + ((from ^ f * 64) + slot * kBuf) + kk * 32 * kW;
       typedef __attribute__((address_space(3))) v4s *Lds;
       const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p)));
-      const v2u up = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * kW * 2)));
+      const v2u up = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * kW)));
       return v4i{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(up.x), static_cast<int>(up.y)};
     } else if constexpr (S::kFp8) {
-      const int8_t *p = b + (part * 32 + lr) * kBk;
-      const v4i lo = *reinterpret_cast<const v4i *>(p + ((kk * 4 + hi * 2) ^ (lr >> 1 & 7)) * 16);
-      const v4i up = *reinterpret_cast<const v4i *>(p + ((kk * 4 + hi * 2 + 1) ^ (lr >> 1 & 7)) * 16);
+      const v4i lo = *reinterpret_cast<const v4i *>(s_lds + ((from ^ kk * 64) + slot * kBuf) + f * 32 * kBk);
+      const v4i up = *reinterpret_cast<const v4i *>(s_lds + ((from ^ (kk * 64 + 16)) + slot * kBuf) + f * 32 * kBk);
       return __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const v4i *>(b + (part * 32 + lr) * kBk + ((kk * 2 + hi) ^ (lr >> 1 & 7)) * 16);
+      return *reinterpret_cast<const v4i *>(s_lds + ((from ^ kk * 32) + slot * kBuf) + f * 32 * kBk);
     }
   };
 
@@ -196,15 +244,17 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   while (true) {
     asm volatile("s_barrier" : : : "memory");
     v16f acc[kFn][kFm] = {};
-    Part fa[2][kFn], fb[2][kFm];
+    // (8-bit: parts of A come one row of products ahead instead of one depth)
+    constexpr int kSets = S::kFp8 ? 1 : 2;
+    Part fa[kSets][kFn], fb[2][kFm];
     int scale[kFn + kFm], scale_next[kFn + kFm];
     auto fetch = [&](int slot, int kk, int f) {
       if (f < kFn)
-        fa[kk & 1][f] = read(std::bool_constant<S::kTransA>(), std::integral_constant<int, S::kN>(), 0,
-                             wn * kFn + f, slot, kk);
+        fa[kk % kSets][f] = read(std::bool_constant<S::kTransA>(), std::integral_constant<int, S::kN>(),
+                               from_a, f, slot, kk);
       else
         fb[kk & 1][f - kFn] = read(std::bool_constant<S::kTransB>(), std::integral_constant<int, S::kM>(),
-                                   S::kN * kBk, wm * kFm + f - kFn, slot, kk);
+                                   from_b, f - kFn, slot, kk);
     };
     auto fetch_scales = [&](int group, int *to) {
       const int8_t *b = s_lds + S::kScaleAt + (group & 1) * (S::kN + S::kM) * 4;
@@ -217,60 +267,50 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     // the elements of a part past the step's `left` become 0 on both sides (0 times what
     // lies there could be a NaN)
     auto clear = [&](int kk, int left) {
-      const int mine = left - (S::kFp8 ? kk * 64 + hi * 32 : kk * 16 + hi * 8);
-      if constexpr (S::kFp8) {  // (whole chunks of 16)
+      const int mine = left - (kk * 16 + hi * 8);
+      int keep[4];
 #pragma unroll
-        for (int f = 0; f < kFn + kFm; ++f) {
-          Part &p = f < kFn ? fa[kk & 1][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
+      for (int d = 0; d < 4; ++d) keep[d] = mine >= 2 * d + 2 ? -1 : mine == 2 * d + 1 ? 0xFFFF : 0;
 #pragma unroll
-          for (int d = 0; d < 8; ++d)
-            if (mine <= d / 4 * 16) p[d] = 0;
-        }
-      } else {
-        int keep[4];
+      for (int f = 0; f < kFn + kFm; ++f) {
+        Part &p = f < kFn ? fa[kk % kSets][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) keep[d] = mine >= 2 * d + 2 ? -1 : mine == 2 * d + 1 ? 0xFFFF : 0;
-#pragma unroll
-        for (int f = 0; f < kFn + kFm; ++f) {
-          Part &p = f < kFn ? fa[kk & 1][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
-#pragma unroll
-          for (int d = 0; d < 4; ++d) p[d] &= keep[d];
-        }
+        for (int d = 0; d < 4; ++d) p[d] &= keep[d];
       }
+    };
+    auto clear8 = [&](int kk, int left, auto &p) {  // (whole chunks of 16)
+      const int mine = left - (kk * 64 + hi * 32);
+#pragma unroll
+      for (int d = 0; d < (S::kFp8 ? 8 : 0); ++d)
+        if (mine <= d / 4 * 16) p[d] = 0;
     };
     // One step, its first parts already in registers.  Reads of the next parts, and at the
     // step's end the loads of the step after the next, lie between the products.  kMore:
     // how many steps follow, up to 2.
-    auto step = [&](int s, auto ahead) {
+    auto next_arrives = [&](auto ahead) {
+      // the next step's bytes are there, and nobody reads this step's any more
+      if (decltype(ahead)::value == 2) {
+        work.advance();
+        left_load = work.left;
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    };
+    auto step16 = [&](int s, auto ahead) {
       constexpr int kMore = decltype(ahead)::value;
       const int slot = s & 1;
 #pragma unroll
       for (int kk = 0; kk < kDepths; ++kk) {
-        if (kk == kDepths - 1) {  // the next step's bytes are there, and nobody reads this step's any more
-          if (kMore == 2) {
-            work.advance();
-            left_load = work.left;
-          }
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-          if (S::kFp8 && kMore > 0 && (s & 3) == 3) fetch_scales((s + 1) >> 2, scale_next);
-          if (S::kFp8 && kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
-        }
+        if (kk == kDepths - 1) next_arrives(ahead);
         if (Work::kRagged) {
           if (left_now < S::kStep) clear(kk, left_now);
         } else if (kMore == 0) {
-          if (work.tail < (kk + 1) * (S::kStep / kDepths)) clear(kk, work.tail);
+          if (work.tail < (kk + 1) * 16) clear(kk, work.tail);
         }
         constexpr int kAll = kFn * kFm, kParts = kFn + kFm;
 #pragma unroll
         for (int m = 0; m < kAll; ++m) {
           const int i = m / kFm, j = m % kFm;
-          if constexpr (S::kFp8)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                fa[kk & 1][i], fb[kk & 1][j], acc[i][j], 0, 0, 0, scale[i], 0, scale[kFn + j]);
-          else
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(v8b, fa[kk & 1][i]), __builtin_bit_cast(v8b, fb[kk & 1][j]),
-                acc[i][j], 0, 0, 0);
+          acc[i][j] = multiply<S::kKind>(fa[kk % kSets][i], 0, fb[kk & 1][j], 0, acc[i][j]);
           // spread evenly over the products
           for (int f = m * kParts / kAll; f < (m + 1) * kParts / kAll; ++f) {
             if (kk < kDepths - 1) fetch(slot, kk + 1, f);
@@ -283,7 +323,56 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       }
       left_now = left_next;
       left_next = left_load;
-      if (S::kFp8 && kMore > 0) {
+    };
+    // The same for 8-bit elements, whose parts are twice as large: a part of A is read
+    // kLead rows of products before its own, into the place of one that is done with.
+    constexpr int kLead = kFn / 2;
+    auto step8 = [&](int s, auto ahead) {
+      constexpr int kMore = decltype(ahead)::value, kRows = kDepths * kFn;
+      const int slot = s & 1;
+      if (kMore == 0 && work.tail <= 64) {  // (its first depth's parts of B, first kLead of A)
+#pragma unroll
+        for (int j = 0; j < kFm; ++j) clear8(0, work.tail, fb[0][j]);
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const int kk = r / kFn, i = r % kFn;
+        if (r == kRows - kLead) {
+          next_arrives(ahead);
+          if (kMore > 0 && (s & 3) == 3) fetch_scales((s + 1) >> 2, scale_next);
+          if (kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
+        }
+        if (kMore == 0 && work.tail < S::kStep) {
+          clear8(kk, work.tail, fa[0][i]);
+          if (i == 0 && kk > 0) {
+#pragma unroll
+            for (int j = 0; j < kFm; ++j) clear8(kk, work.tail, fb[kk & 1][j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kFm; ++j) {
+          acc[i][j] = multiply<S::kKind>(fa[0][i], scale[i], fb[kk & 1][j], scale[kFn + j], acc[i][j]);
+          // between the products: A's part kLead rows on, B's parts of the next depth, all of
+          // them in the last rows where that is the next step's
+          if (j == kFm - 1) {
+            const int to = r + kLead;
+            if (to < kRows) fetch(slot, to / kFn, to % kFn);
+            else if (kMore > 0) fetch(slot ^ 1, 0, to - kRows);
+          }
+          if (kk < kDepths - 1) {
+            for (int f = (i * kFm + j) * kFm / (kFn * kFm); f < (i * kFm + j + 1) * kFm / (kFn * kFm); ++f)
+              fetch(slot, kk + 1, kFn + f);
+          } else if (r >= kRows - kLead) {
+            const int at = (r - (kRows - kLead)) * kFm + j, all = kLead * kFm;
+            if (kMore > 0)
+              for (int f = at * kFm / all; f < (at + 1) * kFm / all; ++f) fetch(slot ^ 1, 0, kFn + f);
+            if (kMore == 2)
+              for (int f = at * kLoads / all; f < (at + 1) * kLoads / all; ++f) issue(slot, f);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (kMore > 0) {
         if ((s & 3) == 3) {
 #pragma unroll
           for (int f = 0; f < kFn + kFm; ++f) scale[f] = scale_next[f];
@@ -293,10 +382,18 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
         }
       }
     };
+    auto step = [&](int s, auto ahead) {
+      // (else every part's address would be held throughout)
+      from_a = opaque(from_a);
+      from_b = opaque(from_b);
+      if constexpr (S::kFp8) step8(s, ahead);
+      else step16(s, ahead);
+    };
 
     if (loaded > 0) {
 #pragma unroll
-      for (int f = 0; f < kFn + kFm; ++f) fetch(0, 0, f);
+      for (int f = 0; f < kFn + kFm; ++f)
+        if (!S::kFp8 || f < kLead || f >= kFn) fetch(0, 0, f);
       if (S::kFp8) fetch_scales(0, scale);
       int s = 0;
       for (; work.more(); ++s) step(s, std::integral_constant<int, 2>());
@@ -383,6 +480,7 @@ struct ProductWork {
   static_assert(!kGlu || S::kFn % 2 == 0, "a wave has gates with their partners");
 
   const ProductArgs &a;
+  const int N, K, n_out;  // (held: a reload could look like another value in some lanes)
   RowTiles<S::kM * kPart> &tiles;
   const int n_col, first, stride, n_item;
   int item;
@@ -393,24 +491,28 @@ struct ProductWork {
   static constexpr uint32_t pitch_b = 0;
 
   __device__ ProductWork(const ProductArgs &args, RowTiles<S::kM * kPart> &t, int col, int f, int i, int st, int n)
-      : a(args), tiles(t), n_col(col), first(f), stride(st), n_item(n), item(i) {
-    half = a.N / 2;
-    pitch = a.K * kEsize;
-    pitch_a = a.N * 2;
-    tail = a.K - (a.K - 1) / S::kStep * S::kStep;
+      : a(args), N(__builtin_amdgcn_readfirstlane(args.N)), K(__builtin_amdgcn_readfirstlane(args.K)),
+        n_out(__builtin_amdgcn_readfirstlane(args.n_out)), tiles(t), n_col(col), first(f), stride(st), n_item(n), item(i) {
+    half = N / 2;
+    pitch = K * kEsize;
+    pitch_a = N * 2;
+    tail = K - (K - 1) / S::kStep * S::kStep;
   }
   // false for a quarter that has no rows or no channels
   __device__ bool aim(int id) {
     const int it = first + id / (kPart * kPart), part = id % (kPart * kPart);
     constexpr int kGroup = 8;  // 8 row tiles by all columns at a time
     const int group = it / (kGroup * n_col), rest = it - group * kGroup * n_col;
-    const int high = min(kGroup, tiles.total - group * kGroup);
+    const int high = min(kGroup, __builtin_amdgcn_readfirstlane(tiles.total) - group * kGroup);
     tile = tiles.find(a, group * kGroup + rest % high);
+    tile.row = readlane64(tile.row, 0);  // (the same in all lanes)
+    tile.rows = __builtin_amdgcn_readfirstlane(tile.rows);
+    tile.w = __builtin_amdgcn_readfirstlane(tile.w);
     n0 = (rest / high * kPart + part / kPart) * kOut;
     if (kPart > 1) {
       tile.row += part % kPart * S::kM;
       tile.rows = min(tile.rows - part % kPart * S::kM, S::kM);
-      return tile.rows > 0 && n0 < a.n_out;
+      return tile.rows > 0 && n0 < n_out;
     }
     return true;
   }
@@ -422,15 +524,15 @@ struct ProductWork {
       if (aim(id)) break;
     }
     const int64_t at = tile.w * a.w_stride;
-    pa = uniform(a.w + (S::kTransA ? at + n0 : at + static_cast<int64_t>(n0) * a.K) * kEsize);
-    pa2 = pa + static_cast<int64_t>(half) * a.K * kEsize;  // (contiguous) the gates' partners
-    pb = uniform(a.x + tile.row * a.K * kEsize);
+    pa = uniform(a.w + (S::kTransA ? at + n0 : at + static_cast<int64_t>(n0) * K) * kEsize);
+    pa2 = pa + static_cast<int64_t>(half) * K * kEsize;  // (contiguous) the gates' partners
+    pb = uniform(a.x + tile.row * K * kEsize);
     if (S::kFp8) {
-      const int p = scale_pitch(a.K);
-      sa = uniform(a.ws + (static_cast<int64_t>(tile.w) * a.N + n0) * p);
+      const int p = scale_pitch(K);
+      sa = uniform(a.ws + (static_cast<int64_t>(tile.w) * N + n0) * p);
       sb = uniform(a.xs + tile.row * p);
     }
-    to_load = (a.K + S::kStep - 1) / S::kStep;
+    to_load = (K + S::kStep - 1) / S::kStep;
     started = false;
     return true;
   }
@@ -438,7 +540,7 @@ struct ProductWork {
   __device__ bool more() const { return to_load > 0; }
   __device__ void advance() {
     if (started) {
-      const int64_t d = S::kTransA ? static_cast<int64_t>(S::kStep) * a.N * 2 : kBk;
+      const int64_t d = S::kTransA ? static_cast<int64_t>(S::kStep) * N * 2 : kBk;
       pa = uniform(pa + d);
       if (kGlu) pa2 = uniform(pa2 + d);
       pb = uniform(pb + kBk);
@@ -448,18 +550,18 @@ struct ProductWork {
   }
   // memory rows and chunks of the tile's, in range for any j and c
   __device__ int row_a(int j) const {
-    return kGlu ? min(j / 64 * 32 + j % 32, half - 1 - n0) : min(j, a.N - 1 - n0);
+    return kGlu ? min(j / 64 * 32 + j % 32, half - 1 - n0) : min(j, N - 1 - n0);
   }
   __device__ int row_b(int j) const { return min(j, tile.rows - 1); }
   __device__ bool second(int unit) const { return kGlu && !S::kTransA && unit * 8 < S::kN && unit * 8 % 64 >= 32; }
   __device__ uint32_t chunk_a(int c) const {
     const int j = c * 8;
-    return 2 * (kGlu ? min(j / 64 * 32 + j % 32, half - 8 - n0) + (j % 64 >= 32 ? half : 0) : min(j, a.N - 8 - n0));
+    return 2 * (kGlu ? min(j / 64 * 32 + j % 32, half - 8 - n0) + (j % 64 >= 32 ? half : 0) : min(j, N - 8 - n0));
   }
   __device__ uint32_t chunk_b(int) const { return 0; }
   __device__ uint32_t scale_at(int j, int lane) const {
     const int r = j >= S::kN ? row_b(j - S::kN + lane) : row_a(j + lane) + (kGlu && lane >= 32 ? half : 0);
-    return static_cast<uint32_t>(r) * scale_pitch(a.K);
+    return static_cast<uint32_t>(r) * scale_pitch(K);
   }
 
   struct Out {
@@ -483,10 +585,10 @@ struct ProductWork {
       for (int p = 0; p < 4; ++p) {
         const int r = (wm * S::kFm + n / S::kFn) * 32 + p * 8 + el / 8;
         k.g[n & 1][p] = k.u[n & 1][p] = v2u{0, 0};
-        if (r < o.rows && c < a.N) {
-          const uint16_t *at = a.pre + (o.row + r) * 2 * a.N + c;
+        if (r < o.rows && c < N) {
+          const uint16_t *at = a.pre + (o.row + r) * 2 * N + c;
           k.g[n & 1][p] = *reinterpret_cast<const v2u *>(at);
-          k.u[n & 1][p] = *reinterpret_cast<const v2u *>(at + a.N);
+          k.u[n & 1][p] = *reinterpret_cast<const v2u *>(at + N);
         }
       }
     }
@@ -498,7 +600,7 @@ struct ProductWork {
     const Stage st(lds);
     constexpr int kFn = S::kFn, kFm = S::kFm, kSize = kBf16 ? 2 : 4;
     constexpr int kParts = kOutW / 32, kGroup = kBf16 ? 2 : 1;  // parts that the stage takes
-    const int nw = o.n0 + wn * kOutW, limit = min(a.n_out, nw + kOutW);
+    const int nw = o.n0 + wn * kOutW, limit = min(n_out, nw + kOutW);
     char *const y = static_cast<char *>(a.y);
 #pragma unroll
     for (int j = 0; j < kFm; ++j) {
@@ -546,7 +648,7 @@ struct ProductWork {
               swiglu_grad(v[e], e % 2 ? bf16_at_high(g[e / 2]) : bf16_at_low(g[e / 2]),
                           e % 2 ? bf16_at_high(u[e / 2]) : bf16_at_low(u[e / 2]), da[e], db[e]);
             if (r < o.rows && c < limit) {
-              char *at = y + ((o.row + r) * 2 * a.N + c) * kSize, *at2 = at + static_cast<int64_t>(a.N) * kSize;
+              char *at = y + ((o.row + r) * 2 * N + c) * kSize, *at2 = at + static_cast<int64_t>(N) * kSize;
               if (kBf16) {
                 __builtin_nontemporal_store(v2u{pack_bf16(da[0], da[1]), pack_bf16(da[2], da[3])}, reinterpret_cast<v2u *>(at));
                 __builtin_nontemporal_store(v2u{pack_bf16(db[0], db[1]), pack_bf16(db[2], db[3])}, reinterpret_cast<v2u *>(at2));
@@ -571,7 +673,7 @@ struct ProductWork {
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                   put(std::true_type(), h, q, [&](int e) { return acc[2 * (i + h) + s][j][e]; });
-              leave(reinterpret_cast<char *>(a.pre), a.N, 2, s * half + nw + i * 32, s * half + limit);
+              leave(reinterpret_cast<char *>(a.pre), N, 2, s * half + nw + i * 32, s * half + limit);
             }
         }
       }
@@ -586,20 +688,21 @@ struct ProductWork {
               return kGlu ? silu(acc[f][j][e]) * acc[kGlu ? f + 1 : f][j][e] : acc[f][j][e];
             });
           }
-        leave(y, a.n_out, kSize, nw + i * 32, limit);
+        leave(y, n_out, kSize, nw + i * 32, limit);
       }
     }
   }
 };
 
-template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kFp8, bool kTrans, int kAct, bool kBf16>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, Math kKind, bool kTrans, int kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32_t n_col) {
-  using S = Tile<kN, kM, kWn, kWm, kAhead, kFp8, kTrans, false>;
+  using S = Tile<kN, kM, kWn, kWm, kAhead, kKind, kTrans, false>;
   __shared__ __align__(1024) int8_t s_lds[S::kLds];
   __shared__ int s_run[32];
   RowTiles<kM> tiles;
   tiles.count(a, s_run, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), S::kWaves);
-  const int n_item = tiles.total * n_col;  // (fewer than 2^31: M * N < 2^38)
+  // (fewer than 2^31: M * N < 2^38)
+  const int n_item = __builtin_amdgcn_readfirstlane(tiles.total) * n_col;
   // the workgroups of one XCD (those of equal number modulo 8) take neighbouring items
   constexpr int kXcd = 8;
   const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
@@ -612,7 +715,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32
   }
   if constexpr (kAhead) {
     __syncthreads();
-    using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, kFp8, kTrans, false>;
+    using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, kKind, kTrans, false>;
     ProductWork<Q, 2, kAct, kBf16> work(a, tiles, n_col, n_item - last, slot, grid, last * 4);
     tile_items<Q>(work, s_lds);
   }

@@ -14,9 +14,9 @@ hipError_t launch_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_
                       nullptr, nullptr, block_off, block_w, pre, y, status, M, w_stride, n_w, N, K,
                       n_block, act == ULTRAEP_SWIGLU ? N / 2 : N};
   if (trans) return launch_product_trans(a, act, type, stream);
-  if (act == ULTRAEP_NO_ACT) choose_type<false, false, ULTRAEP_NO_ACT>(a, type, stream);
-  else if (act == ULTRAEP_SWIGLU) choose_type<false, false, ULTRAEP_SWIGLU>(a, type, stream);
-  else choose_type<false, false, ULTRAEP_SWIGLU_GRAD>(a, type, stream);
+  if (act == ULTRAEP_NO_ACT) choose_type<kMath16, false, ULTRAEP_NO_ACT>(a, type, stream);
+  else if (act == ULTRAEP_SWIGLU) choose_type<kMath16, false, ULTRAEP_SWIGLU>(a, type, stream);
+  else choose_type<kMath16, false, ULTRAEP_SWIGLU_GRAD>(a, type, stream);
   return hipGetLastError();
 }
 

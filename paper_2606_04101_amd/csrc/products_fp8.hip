@@ -12,8 +12,8 @@ hipError_t launch_expert_matmul_fp8(const uint8_t *xq, const uint8_t *xs, int64_
   auto bytes = [](const uint8_t *p) { return reinterpret_cast<const int8_t *>(p); };
   const ProductArgs a{bytes(xq), bytes(wq), bytes(xs), bytes(ws), block_off, block_w, nullptr, y,
                       status, M, static_cast<int64_t>(N) * K, n_w, N, K, n_block, act ? N / 2 : N};
-  if (act == ULTRAEP_SWIGLU) choose_type<true, false, ULTRAEP_SWIGLU>(a, type, stream);
-  else choose_type<true, false, ULTRAEP_NO_ACT>(a, type, stream);
+  if (act == ULTRAEP_SWIGLU) choose_type<kMath8, false, ULTRAEP_SWIGLU>(a, type, stream);
+  else choose_type<kMath8, false, ULTRAEP_NO_ACT>(a, type, stream);
   return hipGetLastError();
 }
 

@@ -9,9 +9,9 @@ namespace uep {
 // rows (with SwiGLU half of them gates, then their partners) and up to kTok rows; its waves
 // share K in steps of 128 bytes in turn, each through an LDS ring of its own that kDeep
 // steps fill, so no wave waits for another until they add their sums.
-template <int kTok, int kRows, int kWaves, int kDeep, bool kFp8, int kAct, bool kBf16>
+template <int kTok, int kRows, int kWaves, int kDeep, Math kKind, int kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWaves) k_product_thin(ProductArgs a, int32_t n_col) {
-  constexpr bool kGlu = kAct == ULTRAEP_SWIGLU;
+  constexpr bool kGlu = kAct == ULTRAEP_SWIGLU, kFp8 = kKind != kMath16;
   constexpr int kThreads = 64 * kWaves, kFm = kTok / 16, kFn = kRows / 16, kEsize = kFp8 ? 1 : 2;
   constexpr int kOut = kGlu ? kRows / 2 : kRows;
   constexpr int kPitch = kRows + 4;          // words of a row's sums
@@ -123,7 +123,20 @@ __global__ void __launch_bounds__(64 * kWaves) k_product_thin(ProductArgs a, int
         }
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the part is free
         issue(s + kDeep * kWaves, b);
-        if constexpr (kFp8) {
+        if constexpr (kKind == kMathWide) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int d = 0; d < 4; d += 2)
+#pragma unroll
+              for (int j = 0; j < kFm; ++j)
+#pragma unroll
+                for (int i = 0; i < kFn; ++i)
+                  acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      __builtin_bit_cast(v8b, widen8(fw[h][i][d], fw[h][i][d + 1], scale_value(sw[i]))),
+                      __builtin_bit_cast(v8b, widen8(fx[h][j][d], fx[h][j][d + 1], scale_value(sx[j]))),
+                      acc[i][j], 0, 0, 0);
+        } else if constexpr (kFp8) {
 #pragma unroll
           for (int j = 0; j < kFm; ++j)
 #pragma unroll
@@ -192,25 +205,25 @@ inline int64_t most_tiles(const ProductArgs &a, int tile_rows) {
   return a.M / tile_rows + (a.M < a.n_block ? a.M : a.n_block);
 }
 
-template <int kTok, int kRows, int kWaves, int kDeep, bool kFp8, int kAct, bool kBf16>
+template <int kTok, int kRows, int kWaves, int kDeep, Math kKind, int kAct, bool kBf16>
 void start_thin(const ProductArgs &a, hipStream_t stream) {
   const int out = kAct == ULTRAEP_SWIGLU ? kRows / 2 : kRows;
   const int32_t n_col = (a.n_out + out - 1) / out;
   const int64_t items = most_tiles(a, kTok) * n_col;
   const dim3 grid(static_cast<unsigned>(items < 1 << 16 ? items : 1 << 16)), block(64 * kWaves);
-  hipLaunchKernelGGL((k_product_thin<kTok, kRows, kWaves, kDeep, kFp8, kAct, kBf16>), grid, block, 0, stream, a, n_col);
+  hipLaunchKernelGGL((k_product_thin<kTok, kRows, kWaves, kDeep, kKind, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
-template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kFp8, bool kTrans, int kAct, bool kBf16>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, Math kKind, bool kTrans, int kAct, bool kBf16>
 void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
   const int out = kAct == ULTRAEP_SWIGLU ? kN / 2 : kN;
   const int32_t n_col = (a.n_out + out - 1) / out;
   const int64_t items = most_tiles(a, kM) * n_col;
   const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
-  hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kFp8, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
+  hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kKind, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
-template <bool kFp8, bool kTrans, int kAct, bool kBf16>
+template <Math kKind, bool kTrans, int kAct, bool kBf16>
 void choose_product(const ProductArgs &a, hipStream_t stream) {
   const int64_t blocks = a.M < a.n_block ? a.M : a.n_block, rows = (a.M + blocks - 1) / blocks;
   auto items = [&](int64_t tile_rows, int64_t channels) {
@@ -221,27 +234,29 @@ void choose_product(const ProductArgs &a, hipStream_t stream) {
   const int64_t big_time = full * 10 + (last == 0 ? 0 : full && last <= 64 ? 4 : 10);
   const int64_t mid_time = (items(128, 128) + 511) / 512 * 6;
   constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
-  if (rows > 64 && big_time < mid_time)
-    return start_product<256, 256, 2, 2, true, kFp8, kTrans, kAct, kBf16>(a, 256, stream);
+  if constexpr (kKind != kMathWide) {
+    if (rows > 64 && big_time < mid_time)
+      return start_product<256, 256, 2, 2, true, kKind, kTrans, kAct, kBf16>(a, 256, stream);
+  }
   if (rows > 56 && items(128, 128) >= 256)
-    return start_product<128, 128, 2, 2, false, kFp8, kTrans, kAct, kBf16>(a, 512, stream);
+    return start_product<128, 128, 2, 2, false, kKind, kTrans, kAct, kBf16>(a, 512, stream);
   if (!kThin || (rows > 32 && items(64, 128) >= 320))
-    return start_product<128, 64, 2, 1, false, kFp8, kTrans, kAct, kBf16>(a, 768, stream);
+    return start_product<128, 64, 2, 1, false, kKind, kTrans, kAct, kBf16>(a, 768, stream);
   if constexpr (kThin) {
-    const bool deep = static_cast<int64_t>(a.K) * (kFp8 ? 1 : 2) >= 4096;
-    if (rows > 32 && items(64, 64) >= 256 && deep) start_thin<64, 64, 4, 2, kFp8, kAct, kBf16>(a, stream);
-    else if (rows > 32 && items(64, 64) >= 256) start_thin<64, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
-    else if (rows > 12 && items(32, 64) >= 256 && deep) start_thin<32, 64, 4, 2, kFp8, kAct, kBf16>(a, stream);
-    else if (rows > 12 && items(32, 64) >= 256) start_thin<32, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
-    else if (deep) start_thin<16, 32, 4, 2, kFp8, kAct, kBf16>(a, stream);
-    else start_thin<16, 64, 2, 2, kFp8, kAct, kBf16>(a, stream);
+    const bool deep = static_cast<int64_t>(a.K) * (kKind == kMath16 ? 2 : 1) >= 4096;
+    if (rows > 32 && items(64, 64) >= 256 && deep) start_thin<64, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
+    else if (rows > 32 && items(64, 64) >= 256) start_thin<64, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
+    else if (rows > 12 && items(32, 64) >= 256 && deep) start_thin<32, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
+    else if (rows > 12 && items(32, 64) >= 256) start_thin<32, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
+    else if (deep) start_thin<16, 32, 4, 2, kKind, kAct, kBf16>(a, stream);
+    else start_thin<16, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
   }
 }
 
-template <bool kFp8, bool kTrans, int kAct>
+template <Math kKind, bool kTrans, int kAct>
 void choose_type(const ProductArgs &a, int32_t type, hipStream_t stream) {
-  if (type == ULTRAEP_BF16) choose_product<kFp8, kTrans, kAct, true>(a, stream);
-  else choose_product<kFp8, kTrans, kAct, false>(a, stream);
+  if (type == ULTRAEP_BF16) choose_product<kKind, kTrans, kAct, true>(a, stream);
+  else choose_product<kKind == kMath8 ? kMathWide : kKind, kTrans, kAct, false>(a, stream);
 }
 
 }  // namespace uep

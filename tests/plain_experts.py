@@ -9,6 +9,15 @@ import numpy as np
 
 from plain64 import U16, U32, sigmoid
 
+def matmul(a, b):
+    """a @ b in 64 bits; by torch where the GPU is at hand, since large ones take long."""
+    if a.size * b.shape[1] > 1 << 26:
+        import torch
+        if torch.cuda.is_available():
+            return (torch.from_numpy(np.ascontiguousarray(a)).cuda() @ torch.from_numpy(np.ascontiguousarray(b)).cuda()).cpu().numpy()
+    return a @ b
+
+
 TINY = 1e-34   # below this the fast exponential may give 0
 
 
@@ -54,23 +63,43 @@ def rounded(y, err, f32):
     return err + u * (np.abs(y) + err) + 1e-37
 
 
-def product(x, w, off, of, act, trans=False, pre=None):
+def eights(x):
+    """The largest magnitude of each 8 neighbours of the last axis."""
+    x = np.pad(np.abs(x), [(0, 0)] * (x.ndim - 1) + [(0, -x.shape[-1] % 8)])
+    return x.reshape(*x.shape[:-1], -1, 8).max(axis=-1)
+
+
+def product(x, w, off, of, act, trans=False, pre=None, cut=False, taken_to_bf16=False):
     """y [M], its bound, v and its bound, of rows x [M][K] (fp64) and weights
-    [n_w][N][K] (trans: [n_w][K][N]); rows outside the blocks are NaN."""
+    [n_w][N][K] (trans: [n_w][K][N]); rows outside the blocks are NaN.
+    cut: by the matrix unit's 8-bit products, 8 neighbours of which are cut 13 bits
+    below the exponent of the largest before they are added: each of the 7 others
+    loses less than 2^-13 of it.
+    taken_to_bf16: values below 2^-126 are off by half of bf16's least step, 2^-133."""
     M, K = x.shape
     N = w.shape[2] if trans else w.shape[1]
     width = {"none": N, "swiglu": N // 2, "swiglu_grad": 2 * N}[act]
     y, err = np.full((M, width), np.nan), np.full((M, width), np.nan)
     v, dv = np.full((M, N), np.nan), np.full((M, N), np.nan)
+    sides = {}  # of each weight: itself, its magnitudes, their largest of 8
     for g in range(len(off) - 1):
         lo, hi = off[g], off[g + 1]
         if hi <= lo:
             continue
-        ww = w[of[g] if of is not None else g]
-        ww = ww if trans else ww.T
+        j = of[g] if of is not None else g
+        if j not in sides:
+            ww = w[j] if trans else w[j].T
+            sides[j] = ww, np.abs(ww), eights(ww.T).T if cut else None
+        ww, size, most = sides[j]
         with np.errstate(invalid="ignore"):
-            v[lo:hi] = x[lo:hi] @ ww
-            dv[lo:hi] = 2 * K * U32 * (np.abs(x[lo:hi]) @ np.abs(ww)) + 1e-37
+            v[lo:hi] = matmul(x[lo:hi], ww)
+            dv[lo:hi] = 2 * K * U32 * matmul(np.abs(x[lo:hi]), size) + 1e-37
+            if cut:
+                dv[lo:hi] += 7 * 2.0 ** -13 * matmul(eights(x[lo:hi]), most)
+            if taken_to_bf16:
+                small = (np.abs(x[lo:hi]) < 2.0 ** -126) & (x[lo:hi] != 0), (size < 2.0 ** -126) & (ww != 0)
+                if small[0].any() or small[1].any():
+                    dv[lo:hi] += 2.0 ** -134 * (small[0] @ size + np.abs(x[lo:hi]) @ small[1])
         y[lo:hi], err[lo:hi] = activate(v[lo:hi], dv[lo:hi], act, None if pre is None else pre[lo:hi])
     return y, err, v, dv
 
@@ -84,8 +113,8 @@ def weight_grad(dy, x, off, of, n_w):
         if hi <= lo:
             continue
         w = of[g] if of is not None else g
-        dw[w] += dy[lo:hi].T @ x[lo:hi]
-        mag[w] += np.abs(dy[lo:hi]).T @ np.abs(x[lo:hi])
+        dw[w] += matmul(dy[lo:hi].T, x[lo:hi])
+        mag[w] += matmul(np.abs(dy[lo:hi]).T, np.abs(x[lo:hi]))
         rows[w] += hi - lo
     return dw, 2 * (rows[:, None, None] + 2) * U32 * mag + 1e-37
 

@@ -129,12 +129,17 @@ TILES = [  # every choice of tiles: one to four blocks of a few rows to many, wi
     ([3000], 264, 72), ([33] * 64, 520, 200), ([8] * 40, 1024, 4104), ([24] * 30, 1040, 4104), ([40] * 30, 1040, 4104)]
 
 
+def shared(sizes):
+    """Many blocks over five weights."""
+    return dict(of=[g * 3 % 5 for g in range(len(sizes))], n_w=5) if len(sizes) > 5 else {}
+
+
 @pytest.mark.parametrize("sizes,N,K", TILES)
 @pytest.mark.parametrize("trans,act", [(False, "none"), (True, "none"), (False, "swiglu"), (True, "swiglu_grad")])
 def test_bf16_products_over_the_tile_shapes(sizes, N, K, trans, act):
     if act == "swiglu":
         N = N // 16 * 16
-    check_bf16(sizes, N, K, trans, act, f32=False)
+    check_bf16(sizes, N, K, trans, act, f32=False, **shared(sizes))
 
 
 @pytest.mark.parametrize("trans", [False, True])
@@ -472,11 +477,15 @@ def e4m3_rows(rng, rows, K, spread=2.0):
     return pe.quant_blocks(x.astype(np.float32), K)
 
 
-def fp8_product(sizes, N, K, act, f32, of=None, n_w=None, start=0, tail=0, seed=0, spoil=None):
+def fp8_product(sizes, N, K, act, f32, of=None, n_w=None, start=0, tail=0, seed=0, spoil=None, whole=False):
     rng = np.random.default_rng(seed)
     off, M = layout(sizes, start, tail)
     n_w = n_w or len(sizes)
     (xq, xs), (wq, ws) = e4m3_rows(rng, M, K), e4m3_rows(rng, n_w * N, K)
+    if whole:  # small integers: every product and sum is exact
+        digits = pe.e4m3_bits(np.arange(-3.0, 4.0))
+        xq, wq = rng.choice(digits, xq.shape), rng.choice(digits, wq.shape)
+        xs, ws = np.where(xs > 0, 127, 0).astype(np.uint8), np.where(ws > 0, 126, 0).astype(np.uint8)
     wq, ws = wq.reshape(n_w, N, K), ws.reshape(n_w, N, -1)
     if spoil:
         spoil(xq, xs, wq, ws)
@@ -485,7 +494,9 @@ def fp8_product(sizes, N, K, act, f32, of=None, n_w=None, start=0, tail=0, seed=
     uep.ultraep_expert_matmul_fp8(dev(xq), dev(xs), M, dev(wq), dev(ws), n_w, N, K, dev(off),
                                   None if of is None else dev(np.array(of, np.int32)), len(sizes), ACTS[act], y, st)
     assert int(st.item()) == 0
-    want, err, _, _ = pe.product(pe.dequantised(xq, xs), pe.dequantised(wq, ws), off, of, act)
+    want, err, _, _ = pe.product(pe.dequantised(xq, xs), pe.dequantised(wq, ws), off, of, act, cut=not f32, taken_to_bf16=f32)
+    if whole:
+        err = np.zeros_like(err)
     got = y.double().cpu().numpy()
     inside = np.zeros(M, bool)
     inside[off[0]:off[-1]] = True
@@ -493,13 +504,34 @@ def fp8_product(sizes, N, K, act, f32, of=None, n_w=None, start=0, tail=0, seed=
     return got[inside], want[inside], pe.rounded(want, err, f32)[inside]
 
 
-@pytest.mark.parametrize("sizes,N,K", [
+SHAPES8 = [
     ([1], 16, 16), ([1], 64, 4096), ([0, 3, 0], 48, 48), ([65, 0, 63, 1], 96, 144), ([130, 7], 272, 272),
-    ([5, 64, 128, 200], 144, 528), ([257], 528, 128), ([300, 300], 320, 400), ([16] * 4, 1040, 2064), ([40], 64, 3600)]
-    + [(s, n // 16 * 16, k // 16 * 16) for s, n, k in TILES])
+    ([5, 64, 128, 200], 144, 528), ([257], 528, 128), ([300, 300], 320, 400), ([16] * 4, 1040, 2064), ([40], 64, 3600)
+] + [(s, n // 16 * 16, k // 16 * 16) for s, n, k in TILES]
+
+
+@pytest.mark.parametrize("sizes,N,K", SHAPES8)
 @pytest.mark.parametrize("act", ["none", "swiglu"])
 def test_fp8_products(sizes, N, K, act):
-    got, want, err = fp8_product(sizes, N, K, act, False)
+    got, want, err = fp8_product(sizes, N, K, act, False, **shared(sizes))
+    assert np.isfinite(got).all()
+    same_where_defined(got, want, err)
+
+
+@pytest.mark.parametrize("sizes,N,K", SHAPES8)
+@pytest.mark.parametrize("f32", [False, True])
+def test_fp8_products_of_small_integers_are_exact(sizes, N, K, f32):
+    """Products of at most 9 are summed without a rounding, so every element that a wrong
+    place would bring is seen; a bf16 result is the exact one's rounding."""
+    got, want, _ = fp8_product(sizes, N, K, "none", f32, whole=True, **shared(sizes))
+    if not f32:
+        want = p64.bf16(want.astype(np.float32)).astype(np.float64)
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("sizes,N,K", [(s, n // 16 * 16, k // 16 * 16) for s, n, k in TILES])
+def test_fp8_products_fp32_results_over_the_tile_shapes(sizes, N, K):
+    got, want, err = fp8_product(sizes, N, K, "swiglu", True, **shared(sizes))
     assert np.isfinite(got).all()
     same_where_defined(got, want, err)
 
