@@ -1,87 +1,342 @@
 // The gradient of the experts' weights: for each weight the sum, over its blocks' rows, of
 // the outer products of the two sides' rows.
-#include "operators.hpp"
+#include "products.hpp"
 
 namespace uep {
 
 struct GradArgs {
-  const uint16_t *dy, *x;
+  const int8_t *dy, *x;
   const int64_t *block_off;
   const int32_t *block_w;
   void *dw;
   int32_t *status;
-  int64_t M, dw_stride;
-  int32_t n_w, N, K, n_block, accumulate, bf16;
+  int64_t M, dw_stride;  // (dw_stride in elements)
+  int32_t n_w, N, K, n_block;
+  int32_t parts;  // a weight's rows in so many parts, dw_stride * n_w elements apart
 };
 
-constexpr int kTile = 64, kStepM = 16;
+// Items item, item + stride, .. below n_item: tiles of a weight's gradient, kM of its rows
+// (channels n of dy) by kN of its columns (channels k of x), and of each a part of the rows
+// that are summed over.  Both sides are transposed on their way from LDS.  The steps of an
+// item are its blocks' rows by 64; a block's last may have fewer.  Blocks are looked at in
+// runs of 64, one a lane.
+template <class S, bool kBf16, bool kAdd>
+struct GradWork {
+  static constexpr bool kRagged = true;
+  static constexpr int tail = S::kStep;
+  static constexpr uint32_t pitch = 0;
+  const GradArgs &a;
+  const int N, K, n_block, n_run, tn, tk, stride, n_item;
+  const int64_t *const block_off;
+  const int32_t *const block_w;
+  const int8_t *const dy, *const x;
+  int item;
+  // this lane's block of run `run`: its first row, rows, weight
+  int64_t lo;
+  int rows, w, run;
+  uint64_t mask;  // of the run's blocks of the item's weight that are still to come
+  int weight, part, n0, k0;
+  int64_t row;    // of the next step
+  int remaining;  // rows of its block from there on
+  int budget;     // steps of the item's part that are still to come
+  bool empty;
+  const int8_t *pa, *pa2, *pb, *sa, *sb;
+  int left;
+  uint32_t pitch_a, pitch_b;
 
-// 64 x 64 elements of one weight's gradient, 4 x 4 a thread, on the vector units.
-__global__ void __launch_bounds__(256) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
-  __shared__ float s_y[kStepM][kTile], s_x[kStepM][kTile];
-  const int tid = threadIdx.x;
-  bool sound = true;  // no block is out of order, out of [0, M] or without a weight
-  for (int g = tid; g < a.n_block; g += 256) {
+  __device__ GradWork(const GradArgs &g, int first, int step, int n_tile_n, int n_tile_k, int n)
+      : a(g), N(__builtin_amdgcn_readfirstlane(g.N)), K(__builtin_amdgcn_readfirstlane(g.K)),
+        n_block(__builtin_amdgcn_readfirstlane(g.n_block)), n_run((n_block + kWave - 1) / kWave),
+        tn(n_tile_n), tk(n_tile_k), stride(step), n_item(n), block_off(uniform(g.block_off)),
+        block_w(uniform(g.block_w)), dy(uniform(g.dy)), x(uniform(g.x)), item(first) {
+    pitch_a = K * 2;
+    pitch_b = N * 2;
+    if (n_run == 1) load(0);
+  }
+  __device__ void load(int r) {
+    const int g = r * kWave + lane_id(), at = min(g, n_block - 1);
+    lo = block_off[at];
+    rows = static_cast<int>(block_off[at + 1] - lo);
+    w = block_w ? block_w[at] : at;
+    if (g >= n_block) rows = 0;
+    run = r;
+  }
+  // to the first row of the item's next block; remaining 0 if there is none
+  __device__ void next_block() {
+    remaining = 0;
+    while (!mask) {
+      if (run + 1 >= n_run) return;
+      load(run + 1);
+      mask = ballot(w == weight && rows > 0);
+    }
+    const int l = __builtin_ctzll(mask);
+    mask &= mask - 1;
+    row = readlane64(lo, l);
+    remaining = readlane(rows, l);
+  }
+  __device__ void first_block() {
+    if (n_run == 1) {
+      mask = ballot(w == weight && rows > 0);
+    } else {
+      run = -1;
+      mask = 0;
+    }
+    next_block();
+  }
+  __device__ bool next_item() {
+    if (item >= n_item) return false;
+    int it = item;
+    item += stride;
+    const int of_weight = tn * tk, all = of_weight * a.parts;
+    weight = it / all;
+    it -= weight * all;
+    part = it / of_weight;
+    it -= part * of_weight;
+    constexpr int kGroup = 8;  // 8 row tiles by all columns at a time
+    const int group = it / (kGroup * tk), rest = it - group * kGroup * tk;
+    const int high = min(kGroup, tn - group * kGroup);
+    n0 = (group * kGroup + rest % high) * S::kM;
+    k0 = rest / high * S::kN;
+    first_block();
+    budget = 1 << 30;
+    if (a.parts > 1) {
+      int steps = 0;
+      for (; remaining > 0; next_block()) steps += (remaining + S::kStep - 1) / S::kStep;
+      int skip = static_cast<int>(static_cast<int64_t>(steps) * part / a.parts);
+      budget = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / a.parts) - skip;
+      first_block();
+      while (budget > 0 && skip >= (remaining + S::kStep - 1) / S::kStep) {
+        skip -= (remaining + S::kStep - 1) / S::kStep;
+        next_block();
+      }
+      if (budget > 0) {
+        row += static_cast<int64_t>(skip) * S::kStep;
+        remaining -= skip * S::kStep;
+      }
+    }
+    empty = !more();
+    return true;
+  }
+  __device__ bool more() const { return remaining > 0 && budget > 0; }
+  __device__ void advance() {
+    pa = uniform(x + (row * K + k0) * 2);
+    pb = uniform(dy + (row * N + n0) * 2);
+    left = min(remaining, S::kStep);
+    row += S::kStep;
+    remaining -= left;
+    --budget;
+    if (remaining == 0) next_block();
+  }
+  __device__ int row_a(int) const { return 0; }
+  __device__ int row_b(int) const { return 0; }
+  __device__ bool second(int) const { return false; }
+  __device__ uint32_t scale_at(int, int) const { return 0; }
+  __device__ uint32_t chunk_a(int c) const { return 2 * min(c * 8, K - 8 - k0); }
+  __device__ uint32_t chunk_b(int c) const { return 2 * min(c * 8, N - 8 - n0); }
+
+  struct Out {
+    int weight, part, n0, k0;
+    bool skip;
+  };
+  __device__ Out out() const { return {weight, part, n0, k0, kAdd && empty}; }
+  // Added to what is there the sums leave LDS in fp32, 4 channels a lane; a bf16 gradient
+  // that is not added to leaves as such, 8.
+  static constexpr bool kPacked = kBf16 && !kAdd;
+  static constexpr int kLane = kPacked ? 8 : 4, kParts = S::kFn * 4 / kLane;
+  static constexpr int kSize = kBf16 ? 2 : 4;
+  using Word = std::conditional_t<kBf16 && kAdd, v2u, v4u>;  // what a lane stores
+  // (added to) what is there, of the next part while one is worked on
+  struct Old {
+    Word v[2][4];
+  };
+  struct Nothing {};
+  using Early = std::conditional_t<kAdd, Old, Nothing>;
+  // the address of what lane el stores of row p * 8 + el / 8 of part n; null outside
+  __device__ char *place(const Out &o, int n, int p, int wn, int wm, int el) const {
+    const int r = o.n0 + (wm * S::kFm + n / kParts) * 32 + p * 8 + el / 8;
+    const int c = o.k0 + wn * S::kFn * 32 + (n % kParts * 8 + (el & 7)) * kLane;
+    if (r >= N || c >= K || o.skip) return nullptr;
+    const int64_t at = (static_cast<int64_t>(o.part) * a.n_w + o.weight) * a.dw_stride + static_cast<int64_t>(r) * K + c;
+    return static_cast<char *>(a.dw) + at * kSize;
+  }
+  __device__ void keep(const Out &o, Early &k, int n, int wn, int wm) const {
+    if constexpr (kAdd) {
+      const int el = opaque(lane_id());
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const char *at = place(o, n, p, wn, wm, el);
+        k.v[n & 1][p] = at ? *reinterpret_cast<const Word *>(at) : Word{};
+      }
+    }
+  }
+  __device__ void early(const Out &o, Early &k, int wn, int wm) const { keep(o, k, 0, wn, wm); }
+
+  template <class Acc>
+  __device__ void results(const Out &o, Early &old, Acc &acc, int8_t *lds, int wn, int wm) const {
+    const Stage st(lds);
+#pragma unroll
+    for (int j = 0; j < S::kFm; ++j) {
+#pragma unroll
+      for (int i = 0; i < S::kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
+      // before the last stores: all loads, and the earlier stores, are done
+      if (S::kAhead && j == S::kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      else asm volatile("" : : : "memory");
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        const int n = j * kParts + i;
+#pragma unroll
+        for (int h = 0; h < kLane / 4; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[i * kLane / 4 + h][j][q * 4 + e];
+            st.put(h, q, v, std::bool_constant<kPacked>());
+          }
+        if (n + 1 < S::kFm * kParts) keep(o, old, n + 1, wn, wm);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          char *at = place(o, n, p, wn, wm, st.el);
+          Word word;
+          if constexpr (kAdd) {
+            v4f v = st.get<v4f>(p);
+            const Word w = old.v[n & 1][p];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] += !kBf16 ? __uint_as_float(w[kBf16 ? 0 : e])
+                      : e % 2 ? bf16_at_high(w[e / 2]) : bf16_at_low(w[e / 2]);
+            if constexpr (kBf16) word = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            else word = __builtin_bit_cast(v4u, v);
+          } else {
+            word = st.get<v4u>(p);
+          }
+          if (at) __builtin_nontemporal_store(word, reinterpret_cast<Word *>(at));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+};
+
+// Whether every block lies in rising order within [0, M], with a weight where it has rows;
+// else that is reported.  The whole workgroup has the answer.
+template <int kWaves>
+__device__ __forceinline__ bool sound_blocks(const GradArgs &a, int *s_sound) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  bool sound = true;
+  for (int r = wave * kWave; r < a.n_block; r += kWaves * kWave) {
+    const int g = min(r + lane_id(), a.n_block - 1);
     const int64_t lo = a.block_off[g], hi = a.block_off[g + 1];
     const int w = a.block_w ? a.block_w[g] : g;
     sound &= lo >= 0 && hi >= lo && hi <= a.M && (hi == lo || (w >= 0 && w < a.n_w));
   }
-  if (!__syncthreads_and(sound)) {
-    if (tid == 0) report(a.status, ULTRAEP_EDATA);
-    return;
-  }
-  const int tr = tid / 16, tc = tid % 16;
-  for (int64_t item = blockIdx.x; item < static_cast<int64_t>(a.n_w) * tn * tk; item += gridDim.x) {
-    const int w = static_cast<int>(item / (tn * tk)), n0 = static_cast<int>(item / tk % tn) * kTile;
-    const int k0 = static_cast<int>(item % tk) * kTile;
-    float v[4][4] = {};
-    for (int g = 0; g < a.n_block; ++g) {
-      if ((a.block_w ? a.block_w[g] : g) != w) continue;
-      const int64_t lo = a.block_off[g], hi = a.block_off[g + 1];
-      for (int64_t m0 = lo; m0 < hi; m0 += kStepM) {
-        for (int i = tid; i < kStepM * kTile; i += 256) {
-          const int64_t m = m0 + i / kTile;
-          const int n = n0 + i % kTile, k = k0 + i % kTile;
-          s_y[i / kTile][i % kTile] = m < hi && n < a.N ? bf16_at_low(a.dy[m * a.N + n]) : 0.f;
-          s_x[i / kTile][i % kTile] = m < hi && k < a.K ? bf16_at_low(a.x[m * a.K + k]) : 0.f;
-        }
-        __syncthreads();
-        for (int m = 0; m < kStepM; ++m)
-          for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j)
-              v[i][j] = fmaf(s_y[m][tr + i * 16], s_x[m][tc + j * 16], v[i][j]);
-        __syncthreads();
+  const bool all = !ballot(!sound);
+  if (lane_id() == 0) s_sound[wave] = all;
+  if (!all && lane_id() == 0) report(a.status, ULTRAEP_EDATA);
+  __syncthreads();
+  int every = 1;
+#pragma unroll
+  for (int u = 0; u < kWaves; ++u) every &= s_sound[u];
+  return __builtin_amdgcn_readfirstlane(every);
+}
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
+__global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
+  using S = Tile<kN, kM, kWn, kWm, kAhead, kMath16, true, true>;
+  __shared__ __align__(1024) int8_t s_lds[S::kLds];
+  __shared__ int s_sound[S::kWaves];
+  if (!sound_blocks<S::kWaves>(a, s_sound)) return;
+  constexpr int kXcd = 8;  // the workgroups of one XCD take neighbouring items
+  const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
+  const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
+  GradWork<S, kBf16, kAdd> work(a, slot, grid, tn, tk, a.n_w * a.parts * tn * tk);
+  tile_items<S>(work, s_lds);
+}
+
+// The parts' sums, in order: 4 elements a thread.
+template <bool kBf16>
+__global__ void __launch_bounds__(256)
+k_weight_grad_sum(GradArgs a, const v4f *from, int64_t of_weight, int32_t accumulate) {
+  __shared__ int s_sound[4];
+  if (!sound_blocks<4>(a, s_sound)) return;
+  const int64_t all = of_weight * a.n_w, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
+    v4f v = from[i];
+    for (int p = 1; p < a.parts; ++p) v += from[p * all + i];
+    const int64_t at = i / of_weight * a.dw_stride + i % of_weight * 4;
+    if (kBf16) {
+      v2u *to = reinterpret_cast<v2u *>(static_cast<uint16_t *>(a.dw) + at);
+      if (accumulate) {
+        const v2u w = *to;
+        v += v4f{bf16_at_low(w.x), bf16_at_high(w.x), bf16_at_low(w.y), bf16_at_high(w.y)};
       }
+      *to = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+      v4f *to = reinterpret_cast<v4f *>(static_cast<float *>(a.dw) + at);
+      *to = accumulate ? *to + v : v;
     }
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const int n = n0 + tr + i * 16, k = k0 + tc + j * 16;
-        if (n >= a.N || k >= a.K) continue;
-        const int64_t at = w * a.dw_stride + static_cast<int64_t>(n) * a.K + k;
-        if (a.bf16) {
-          uint16_t *p = static_cast<uint16_t *>(a.dw) + at;
-          *p = round_bf16(a.accumulate ? bf16_at_low(*p) + v[i][j] : v[i][j]);
-        } else {
-          float *p = static_cast<float *>(a.dw) + at;
-          *p = a.accumulate ? *p + v[i][j] : v[i][j];
-        }
-      }
   }
 }
 
-size_t weight_grad_ws_bytes(int64_t, int32_t, int32_t, int32_t) { return 16; }
+// Parts of the rows: where the weights' tiles would not fill the card, so many that they
+// do, of 512 rows of a weight at least.  It does not fall with M.
+static int32_t row_parts(int64_t M, int32_t N, int32_t K, int32_t n_w) {
+  const int64_t tiles = int64_t(n_w) * ((N + 127) / 128) * ((K + 127) / 128);
+  const int64_t fill = 512 / tiles, rows = M / (int64_t(n_w) * 512);
+  const int64_t parts = fill < rows ? fill : rows;
+  return static_cast<int32_t>(parts < 2 ? 1 : parts > 64 ? 64 : parts);
+}
+
+size_t weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w) {
+  const int64_t parts = row_parts(M, N, K, n_w);
+  return parts > 1 ? static_cast<size_t>(parts) * n_w * N * K * 4 : 16;
+}
+
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
+static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
+  const int32_t tn = (a.N + kM - 1) / kM, tk = (a.K + kN - 1) / kN;
+  const int64_t items = int64_t(a.n_w) * a.parts * tn * tk;
+  const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
+  hipLaunchKernelGGL((k_weight_grad<kN, kM, kWn, kWm, kAhead, kBf16, kAdd>), grid, block, 0, stream, a, tn, tk);
+}
+
+template <bool kBf16, bool kAdd>
+static void choose_grad(const GradArgs &a, hipStream_t stream) {
+  auto tiles = [&](int64_t n, int64_t k) {
+    return int64_t(a.n_w) * a.parts * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
+  };
+  const int64_t big = (tiles(256, 256) + 255) / 256 * 10, mid = (tiles(128, 128) + 511) / 512 * 6;
+  if (big < mid) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
+  else start_grad<128, 128, 2, 2, false, kBf16, kAdd>(a, 512, stream);
+}
 
 hipError_t launch_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M, int32_t N,
                                      int32_t K, const int64_t *block_off, const int32_t *block_w,
                                      int32_t n_block, int32_t n_w, int64_t dw_stride,
-                                     int32_t accumulate, void *dw, int32_t type, void *,
+                                     int32_t accumulate, void *dw, int32_t type, void *ws,
                                      int32_t *status, hipStream_t stream) {
-  const GradArgs a{dy, x, block_off, block_w, dw, status, M, dw_stride, n_w, N, K, n_block,
-                   accumulate, type == ULTRAEP_BF16};
-  const int32_t tn = (N + kTile - 1) / kTile, tk = (K + kTile - 1) / kTile;
-  const int64_t items = static_cast<int64_t>(n_w) * tn * tk;
-  const dim3 grid(static_cast<unsigned>(items < 1 << 16 ? items : 1 << 16));
-  hipLaunchKernelGGL(k_weight_grad, grid, dim3(256), 0, stream, a, tn, tk);
+  GradArgs a{reinterpret_cast<const int8_t *>(dy), reinterpret_cast<const int8_t *>(x), block_off, block_w, dw, status,
+             M, dw_stride, n_w, N, K, n_block, 1};
+  const bool bf16 = type == ULTRAEP_BF16;
+  const int32_t parts = ws ? row_parts(M, N, K, n_w) : 1;
+  if (parts > 1) {
+    GradArgs part = a;
+    const int64_t of_weight = int64_t(N) * K;
+    part.dw = ws;
+    part.dw_stride = of_weight;
+    a.parts = part.parts = parts;
+    choose_grad<false, false>(part, stream);
+    const int64_t wg = (of_weight / 4 * n_w + 255) / 256;
+    const dim3 grid(static_cast<unsigned>(wg < 2048 ? wg : 2048));
+    if (bf16) hipLaunchKernelGGL((k_weight_grad_sum<true>), grid, dim3(256), 0, stream, a, static_cast<const v4f *>(ws), of_weight / 4, accumulate);
+    else hipLaunchKernelGGL((k_weight_grad_sum<false>), grid, dim3(256), 0, stream, a, static_cast<const v4f *>(ws), of_weight / 4, accumulate);
+  } else if (accumulate) {
+    if (bf16) choose_grad<true, true>(a, stream);
+    else choose_grad<false, true>(a, stream);
+  } else {
+    if (bf16) choose_grad<true, false>(a, stream);
+    else choose_grad<false, false>(a, stream);
+  }
   return hipGetLastError();
 }
 

@@ -312,6 +312,22 @@ def test_weight_grad(sizes, N, K, f32):
     check_weight_grad(sizes, N, K, f32)
 
 
+@pytest.mark.parametrize("sizes,N,K", [([300, 77], 2056, 2056), ([70, 0, 130, 1, 64, 9], 2056, 2056), ([33], 4104, 4104)])
+@pytest.mark.parametrize("f32", [True, False])
+@pytest.mark.parametrize("accumulate", [True, False])
+def test_weight_grad_of_large_weights(sizes, N, K, f32, accumulate):
+    check_weight_grad(sizes, N, K, f32, accumulate=accumulate, gap=16)
+
+
+def test_weight_grad_of_parts_over_many_blocks():
+    """Few small weights, their rows in parts that begin and end inside blocks."""
+    rng = np.random.default_rng(3)
+    sizes = rng.integers(0, 200, 300)
+    of = rng.integers(0, 3, 300)
+    check_weight_grad(sizes.tolist(), 72, 136, True, of=of.tolist(), n_w=3)
+    check_weight_grad(sizes.tolist(), 72, 136, True, of=of.tolist(), n_w=3, ws=False)
+
+
 @pytest.mark.parametrize("f32", [True, False])
 @pytest.mark.parametrize("ws", [True, False])
 def test_weight_grad_accumulates(f32, ws):
