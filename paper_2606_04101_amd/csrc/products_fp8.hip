@@ -19,51 +19,93 @@ hipError_t launch_expert_matmul_fp8(const uint8_t *xq, const uint8_t *xs, int64_
 
 // ---------------------------------------------------------------- quantisation
 
-// One wave a block of 128 elements, two a lane.
+// A lane's 8 neighbouring elements as they lie in memory.
 template <bool kBf16>
-__global__ void __launch_bounds__(256)
-k_quant_blocks(const char *x, int64_t rows, int32_t K, int64_t ld, uint8_t *q, int64_t ldq,
-               uint8_t *scale) {
-  const int lane = lane_id(), pitch = scale_pitch(K);
-  const int n = static_cast<int>((ldq + kScaleBlock - 1) / kScaleBlock);
-  const int64_t nw = static_cast<int64_t>(gridDim.x) * 4;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; i < rows * n; i += nw) {
-    const int64_t r = i / n;
-    const int b = static_cast<int>(i % n), k = b * kScaleBlock + lane * 2;
-    float f[2] = {0.f, 0.f};
-    for (int j = 0; j < 2; ++j)
-      if (k + j < K)
-        f[j] = kBf16 ? bf16_at_low(reinterpret_cast<const uint16_t *>(x)[r * ld + k + j])
-                     : reinterpret_cast<const float *>(x)[r * ld + k + j];
-    const int most = wave_max(max(__float_as_int(f[0]) & 0x7FFFFFFF, __float_as_int(f[1]) & 0x7FFFFFFF));
-    uint8_t byte = 255, o[2] = {0x7F, 0x7F};
-    if (most < 0x7F800000) {
-      // 448 = 1.75 * 2^8: e = exponent - 8, one more where the mantissa is above 1.75
-      const int e = max((most >> 23) - 127 - 8 + ((most & 0x7FFFFF) > 0x600000), -127);
-      byte = static_cast<uint8_t>(e + 127);
-      const int two = __builtin_amdgcn_cvt_pk_fp8_f32(ldexpf(f[0], -e), ldexpf(f[1], -e), 0, false);
-      o[0] = static_cast<uint8_t>(two);
-      o[1] = static_cast<uint8_t>(two >> 8);
-    }
-    for (int j = 0; j < 2; ++j)
-      if (k + j < ldq) q[r * ldq + k + j] = k + j < K ? o[j] : 0;
-    const int n_scale = (K + kScaleBlock - 1) / kScaleBlock;
-    if (lane == 0 && b < n_scale) scale[r * pitch + b] = byte;
-    if (b == 0 && lane >= n_scale % 4 && lane < 4 && n_scale % 4) scale[r * pitch + n_scale / 4 * 4 + lane] = 0;
+struct Eight {
+  v4u v[kBf16 ? 1 : 2] = {};
+  __device__ void load(const char *p) {
+#pragma unroll
+    for (int i = 0; i < (kBf16 ? 1 : 2); ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p) + i);
   }
+  __device__ float at(int i) const {
+    if (!kBf16) return __uint_as_float(v[kBf16 ? 0 : i / 4][i % 4]);
+    return i % 2 ? bf16_at_high(v[0][i / 2]) : bf16_at_low(v[0][i / 2]);
+  }
+  // largest magnitude, as the bits of an fp32 (an infinity or a NaN is the largest)
+  __device__ int largest() const {
+    int m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_int(at(i)) & 0x7FFFFFFF);
+    return m;
+  }
+};
+
+// A wave takes kWords times 512 elements of a row at a time, 8 a lane: 16 lanes hold a block
+// of 128, and the four blocks' scales make one word.  Every element is read once.
+//   The scale is a power of two, so x * 2^-e is exact and the converter's rounding to
+// nearest-even is the only one.
+template <bool kBf16, int kWords>
+__global__ void __launch_bounds__(256)
+k_quant_blocks(const char *__restrict__ x, int64_t rows, int32_t K, int64_t ld, uint8_t *__restrict__ q,
+               int64_t ldq, uint32_t *__restrict__ scale) {
+  const int lane = lane_id(), words = scale_pitch(K) / 4;
+  const int first = blockIdx.y * kWords;
+  constexpr int kSize = kBf16 ? 2 : 4;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; r < rows;
+       r += static_cast<int64_t>(gridDim.x) * 4) {
+    Eight<kBf16> f[kWords];
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+      const int k = (first + u) * 512 + lane * 8;
+      if (k < K) f[u].load(x + (r * ld + k) * kSize);
+    }
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+      const int k = (first + u) * 512 + lane * 8;
+      const int most = row_max(f[u].largest());
+      // 448 = 1.75 * 2^8: e is the exponent - 8, one more where the mantissa is above 1.75
+      const int e = max((most >> 23) - 127 - 8 + ((most & 0x7FFFFF) > 0x600000), -127);
+      const bool fine = most < 0x7F800000;
+      const int byte = fine ? e + 127 : 255;
+      const float by = __int_as_float((127 - e) << 23);  // 2^-e
+      v2u o;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int two = __builtin_amdgcn_cvt_pk_fp8_f32(f[u].at(4 * i) * by, f[u].at(4 * i + 1) * by, 0, false);
+        two = __builtin_amdgcn_cvt_pk_fp8_f32(f[u].at(4 * i + 2) * by, f[u].at(4 * i + 3) * by, two, true);
+        o[i] = k >= K ? 0u : fine ? static_cast<uint32_t>(two) : 0x7F7F7F7Fu;
+      }
+      if (k < ldq) __builtin_nontemporal_store(o, reinterpret_cast<v2u *>(q + r * ldq + k));
+      uint32_t word = 0;  // (a block past K has none)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if ((first + u) * 512 + b * kScaleBlock < K) word |= static_cast<uint32_t>(readlane(byte, b * 16)) << (8 * b);
+      if (lane == 0 && first + u < words) scale[r * words + first + u] = word;
+    }
+  }
+}
+
+template <bool kBf16, int kWords>
+static void start_quant(const char *x, int64_t rows, int64_t K, int64_t ld, uint8_t *q, int64_t ldq,
+                        uint8_t *scale, hipStream_t stream) {
+  const int64_t wg = (rows + 3) / 4;
+  const dim3 grid(static_cast<unsigned>(wg < 1 << 20 ? wg : 1 << 20),
+                  static_cast<unsigned>((ldq + 512 * kWords - 1) / (512 * kWords)));
+  hipLaunchKernelGGL((k_quant_blocks<kBf16, kWords>), grid, dim3(256), 0, stream, x, rows,
+                     static_cast<int32_t>(K), ld, q, ldq, reinterpret_cast<uint32_t *>(scale));
 }
 
 hipError_t launch_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,
                                uint8_t *q, int64_t ldq, uint8_t *scale, hipStream_t stream) {
-  const int64_t wg = (rows * ((ldq + kScaleBlock - 1) / kScaleBlock) + 3) / 4;
-  const dim3 grid(static_cast<unsigned>(wg < 1 << 20 ? wg : 1 << 20));
   const char *xs = static_cast<const char *>(x);
-  if (type == ULTRAEP_BF16)
-    hipLaunchKernelGGL((k_quant_blocks<true>), grid, dim3(256), 0, stream, xs, rows,
-                       static_cast<int32_t>(K), ld, q, ldq, scale);
-  else
-    hipLaunchKernelGGL((k_quant_blocks<false>), grid, dim3(256), 0, stream, xs, rows,
-                       static_cast<int32_t>(K), ld, q, ldq, scale);
+  const bool many = rows * ((ldq + 511) / 512) >= 1 << 15 && ldq > 512;
+  if (type == ULTRAEP_BF16) {
+    if (many) start_quant<true, 4>(xs, rows, K, ld, q, ldq, scale, stream);
+    else start_quant<true, 1>(xs, rows, K, ld, q, ldq, scale, stream);
+  } else {
+    if (many) start_quant<false, 4>(xs, rows, K, ld, q, ldq, scale, stream);
+    else start_quant<false, 1>(xs, rows, K, ld, q, ldq, scale, stream);
+  }
   return hipGetLastError();
 }
 
