@@ -423,7 +423,8 @@ def test_weight_grad_offsets_past_32_bits():
 
 @pytest.mark.parametrize("rows,K,ld,ldq", [
     (1, 8, 8, 16), (1, 16, 16, 16), (3, 24, 40, 32), (65, 520, 520, 528), (257, 2888, 2896, 2896), (5, 128, 128, 128),
-    (7, 136, 136, 400), (40, 7168, 7168, 7168), (9, 12288, 12296, 12304), (3, 65536, 65536, 65536), (1000, 64, 72, 128)])
+    (7, 136, 136, 400), (40, 7168, 7168, 7168), (9, 12288, 12296, 12304), (3, 65536, 65536, 65536), (1000, 64, 72, 128),
+    (17000, 520, 528, 528), (11000, 1160, 1160, 1168), (6600, 2312, 2312, 2560)])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_quant_blocks(rows, K, ld, ldq, bf16):
     rng = np.random.default_rng(rows * K)
