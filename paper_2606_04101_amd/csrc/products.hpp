@@ -38,11 +38,11 @@ struct Tile {
   static constexpr int kN = N, kM = M, kWn = Wn, kWm = Wm;
   static constexpr bool kAhead = Ahead, kFp8 = Fp8, kTransA = TransA, kTransB = TransB;
   static constexpr int kWaves = Wn * Wm, kThreads = kWaves * kWave;
-  static constexpr int kFn = N / Wn / 32, kFm = M / Wm / 32;  // 32 x 32 parts of a wave
+  static constexpr int kFn = N / Wn / 16, kFm = M / Wm / 16;  // 16 x 16 parts of a wave
   static constexpr int kBuf = (N + M) * kBk;
   static constexpr int kLoads = kBuf / 1024 / kWaves, kLoadsA = N / 8 / kWaves;  // of a wave in a step
   static constexpr int kStep = Fp8 ? 128 : 64;  // elements of the common index in a step
-  static constexpr int kDepths = Fp8 ? 2 : 4;   // products of a pair of parts in a step
+  static constexpr int kDepths = Fp8 ? 1 : 2;   // products of a pair of parts in a step
   static constexpr int kScaleAt = 2 * kBuf + (Ahead ? kWaves * 4096 : 0);
   static constexpr int kLds = kScaleAt + (Fp8 ? 2 * (N + M) * 4 : 0);
   static constexpr Math kKind = Kind;
@@ -50,16 +50,17 @@ struct Tile {
   static_assert(kLoadsA * kWaves * 8 == N && kWaves % 2 == 0, "whole loads of each side");
   static_assert(Ahead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
   static_assert(!Fp8 || !(TransA || TransB), "the transposing read is one of 16-bit elements");
-  // a transposed side's loads cover whole groups of 4 of the common index
-  static_assert(!(TransA || TransB) || kWaves * 512 / (N > M ? N : M) % 4 == 0, "");
+  // from one of a wave's loads of a transposed side to the next are whole groups of 8 of
+  // the common index
+  static_assert(!(TransA || TransB) || kWaves * 512 / (N > M ? N : M) % 8 == 0, "");
 };
 
 // A transposed side of kW channels lies in LDS as the rows of its memory, kW * 2 bytes
-// each, chunk c (of 16 bytes) of row r at c ^ flip: the reads of 4 rows by 64 bytes that
-// half a wave makes meet all banks.
+// each, chunk c (of 16 bytes) of row r at c ^ flip(r): the reads that half a wave makes, of
+// 32 bytes of the 8 rows r, r + 1, r + 2, r + 3, r + 8 .. r + 11, meet all banks.
 template <int kW>
 __device__ __forceinline__ int flip(int r) {
-  return kW >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2;
+  return kW >= 128 ? ((r & 3) | (r >> 3 & 1) << 2) << 1 : ((r >> 1 & 1) | (r >> 3 & 1) << 1) << 1;
 }
 
 // (kMathWide) 8 elements of 8 bits with their scale as bf16.  An e4m3 times a power of two
@@ -77,19 +78,19 @@ __device__ __forceinline__ float scale_value(int byte) {
   byte &= 255;
   return byte == 255 ? __builtin_nanf("") : __int_as_float(byte << 23);
 }
-// c + a b for 32 x 32 parts over 16 elements of bf16, or 64 of 8 bits with their scales
+// c + a b for 16 x 16 parts over 32 elements of bf16, or 128 of 8 bits with their scales
 template <Math kKind>
-__device__ __forceinline__ v16f multiply(const v4i &a, int, const v4i &b, int, v16f c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+__device__ __forceinline__ v4f multiply(const v4i &a, int, const v4i &b, int, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
 }
 template <Math kKind>
-__device__ __forceinline__ v16f multiply(const v8i &a, int scale_a, const v8i &b, int scale_b, v16f c) {
+__device__ __forceinline__ v4f multiply(const v8i &a, int scale_a, const v8i &b, int scale_b, v4f c) {
   if constexpr (kKind == kMath8)
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
   const float sa = scale_value(scale_a), sb = scale_value(scale_b);
 #pragma unroll
   for (int d = 0; d < 8; d += 2)
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, widen8(a[d], a[d + 1], sa)),
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, widen8(a[d], a[d + 1], sa)),
                                                 __builtin_bit_cast(v8b, widen8(b[d], b[d + 1], sb)), c, 0, 0, 0);
   return c;
 }
@@ -102,17 +103,16 @@ __device__ __forceinline__ v16f multiply(const v8i &a, int scale_a, const v8i &b
 //   row_a(j), row_b(j), pitch  of contiguous sides: memory row of tile row j, bytes a row
 //   chunk_a(c), chunk_b(c), pitch_a, pitch_b  of transposed sides: byte offset of tile
 //                    chunk c, bytes a row
-//   tail             elements of the last step;  kRagged: any step may have fewer
 //   out(), early(), results()  what the finished tile needs
 template <class S, class Work>
 __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   using Part = typename S::Part;
   constexpr int kFn = S::kFn, kFm = S::kFm, kLoads = S::kLoads, kLoadsA = S::kLoadsA;
-  constexpr int kWaves = S::kWaves, kBuf = S::kBuf, kDepths = S::kDepths;
+  constexpr int kWaves = S::kWaves, kBuf = S::kBuf;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wn = wave % S::kWn, wm = wave / S::kWn;
-  const int lr = lane & 31, hi = lane >> 5;
+  const int lr = lane & 15, lc = lane >> 4;
   const uint32_t lds0 = lds_address(s_lds);
 
   // A wave's load of 1 KiB: of a contiguous side 8 rows of 8 chunks, chunk c of row r at
@@ -123,17 +123,17 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   const int first_a = wave * kRowsA + lane / (S::kN / 8);
   const int first_b = wave * kRowsB + lane / (S::kM / 8);
   uint32_t off[kLoads];
-  uint32_t at_a = 0, at_b = 0;  // of the lane's chunk in row 0 (transposed sides)
-  int left_now = 0, left_next = 0, left_load = 0;  // elements of this step, the next, the one loaded
 
   auto aim = [&] {
     const int l = opaque(lane);
     const int c = (l & 7) ^ ((wave & 1) * 4 + (l >> 4));
     if (S::kTransA) {
       const int r = wave * kRowsA + l / (S::kN / 8);
-      at_a = work.chunk_a((l % (S::kN / 8)) ^ flip<S::kN>(r));
+      uint32_t at_a[2];  // of the lane's chunk in row 0, by load % 2
 #pragma unroll
-      for (int i = 0; i < kLoadsA; ++i) off[i] = at_a + (i * kWaves * kRowsA + r) * work.pitch_a;
+      for (int i = 0; i < 2; ++i) at_a[i] = work.chunk_a((l % (S::kN / 8)) ^ flip<S::kN>(r + i * kWaves * kRowsA));
+#pragma unroll
+      for (int i = 0; i < kLoadsA; ++i) off[i] = at_a[i & 1] + (i * kWaves * kRowsA + r) * work.pitch_a;
     } else {
 #pragma unroll
       for (int i = 0; i < kLoadsA; ++i)
@@ -141,30 +141,32 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     }
     if (S::kTransB) {
       const int r = wave * kRowsB + l / (S::kM / 8);
-      at_b = work.chunk_b((l % (S::kM / 8)) ^ flip<S::kM>(r));
+      uint32_t at_b[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) at_b[i] = work.chunk_b((l % (S::kM / 8)) ^ flip<S::kM>(r + i * kWaves * kRowsB));
 #pragma unroll
       for (int i = kLoadsA; i < kLoads; ++i)
-        off[i] = at_b + ((i - kLoadsA) * kWaves * kRowsB + r) * work.pitch_b;
+        off[i] = at_b[(i - kLoadsA) & 1] + ((i - kLoadsA) * kWaves * kRowsB + r) * work.pitch_b;
     } else {
 #pragma unroll
       for (int i = kLoadsA; i < kLoads; ++i)
         off[i] = static_cast<uint32_t>(work.row_b(((i - kLoadsA) * kWaves + wave) * 8 + (l >> 3))) * work.pitch + c * 16;
     }
   };
-  // Load i of a step into buffer `slot`.  What lies past the step's elements is loaded
-  // from its first ones and not used.
+  // Load i of a step into buffer `slot`.  What lies past the step's elements becomes 0, on
+  // both sides (0 times what lies there could be a NaN): its offset is out of the buffer's
+  // range.
   auto issue = [&](int slot, int i) {
     const bool a = i < kLoadsA;
-    uint32_t o;
-    if (a ? S::kTransA : S::kTransB) {
-      const int r = a ? i * kWaves * kRowsA + first_a : (i - kLoadsA) * kWaves * kRowsB + first_b;
-      o = r < left_load ? off[i] : a ? at_a : at_b;
-    } else {
-      o = off[i] - (chunk * (S::kStep / 8) >= left_load ? chunk * 16 : 0);
-    }
+    const int n = a ? i : i - kLoadsA;
+    bool in;
+    if (a ? S::kTransA : S::kTransB)
+      in = (a ? n * kWaves * kRowsA + first_a : n * kWaves * kRowsB + first_b) < work.left;
+    else
+      in = chunk * (S::kStep / 8) < work.left;
     const int8_t *base = !a ? work.pb : work.second(i * kWaves + wave) ? work.pa2 : work.pa;
-    load_to_lds(base, o,
-                __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + (i * kWaves + wave) * 1024));
+    buffer_to_lds(base, in ? +off[i] : kBufferBytes,
+                  __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + (i * kWaves + wave) * 1024));
   };
   // (8-bit) the words that hold 4 steps' scales of every channel and row
   auto issue_scales = [&](int group) {
@@ -186,14 +188,12 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     if (S::kFp8) issue_scales(0);
     if (work.more()) {
       work.advance();
-      left_now = left_load = work.left;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) issue(0, i);
       loaded = 1;
     }
     if (work.more()) {
       work.advance();
-      left_next = left_load = work.left;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) issue(1, i);
       loaded = 2;
@@ -207,35 +207,36 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   };
 
-  // What this lane reads of a part: 16 (two times 16) bytes of the common index of one
-  // channel or row; from a transposed side by two reads that each hand 4 elements of 16
-  // channels, as they lie for 4 values of the index, to 16 lanes, one channel each.  Where
-  // of the buffer: of the wave's first part at the first depth; the other parts' and
-  // depths' differ in some bits, or are so much further on.
-  constexpr int kBits = S::kFp8 ? 5 : 4;  // (bytes of a lane's elements of one depth)
-  const int tr_row = (lane >> 2 & 3) + hi * 8;
-  auto lane_at = [&](bool trans, int width, int part) {
-    const int across = (lane >> 4 & 1) * 32 + (lane >> 1 & 1) * 16 + (lane & 1) * 8;
-    const int turned = (width >= 128 ? lane >> 2 & 3 : lane >> 3 & 1) * 64;
-    if (trans) return tr_row * width * 2 + (across ^ turned ^ part * 64);
-    return (part * 32 + lr) * kBk + ((hi << kBits) ^ (lr >> 1 & 7) << 4);
+  // What this lane reads of a part: 16 bytes of the common index of one channel or row (8
+  // bits: two times 16, 64 apart); from a transposed side by two reads that each hand 4
+  // elements of 16 channels, as they lie for 4 values of the index, to 16 lanes, one channel
+  // each.  Where of the buffer: of the wave's first part at the first depth; the other
+  // parts' and depths' differ in some bits, or are so much further on.
+  const int tr_row = (lane >> 2 & 3) + lc * 8;
+  auto lane_at = [&](auto width, bool trans, int part) {
+    constexpr int kW = decltype(width)::value;
+    if (trans)
+      return tr_row * kW * 2 + (((lane >> 1 & 1) * 16 + (lane & 1) * 8) ^ flip<kW>(tr_row) * 16 ^ part * 32);
+    return (part * 16 + lr) * kBk + (lc ^ (lr >> 1 & 7)) * 16;
   };
-  int from_a = lane_at(S::kTransA, S::kN, wn * kFn);
-  int from_b = S::kN * kBk + lane_at(S::kTransB, S::kM, wm * kFm);
+  using WidthA = std::integral_constant<int, S::kN>;
+  using WidthB = std::integral_constant<int, S::kM>;
+  int from_a = lane_at(WidthA(), S::kTransA, wn * kFn);
+  int from_b = S::kN * kBk + lane_at(WidthB(), S::kTransB, wm * kFm);
   auto read = [&](auto trans, auto width, int from, int f, int slot, int kk) {
     constexpr int kW = decltype(width)::value;
     if constexpr (decltype(trans)::value) {
-      const int8_t *p = s_lds + ((from ^ f * 64) + slot * kBuf) + kk * 32 * kW;
+      const int8_t *p = s_lds + ((from ^ f * 32) + slot * kBuf) + kk * 64 * kW;
       typedef __attribute__((address_space(3))) v4s *Lds;
       const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p)));
       const v2u up = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * kW)));
       return v4i{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(up.x), static_cast<int>(up.y)};
     } else if constexpr (S::kFp8) {
-      const v4i lo = *reinterpret_cast<const v4i *>(s_lds + ((from ^ kk * 64) + slot * kBuf) + f * 32 * kBk);
-      const v4i up = *reinterpret_cast<const v4i *>(s_lds + ((from ^ (kk * 64 + 16)) + slot * kBuf) + f * 32 * kBk);
+      const v4i lo = *reinterpret_cast<const v4i *>(s_lds + (from + slot * kBuf) + f * 16 * kBk);
+      const v4i up = *reinterpret_cast<const v4i *>(s_lds + ((from ^ 64) + slot * kBuf) + f * 16 * kBk);
       return __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const v4i *>(s_lds + ((from ^ kk * 32) + slot * kBuf) + f * 32 * kBk);
+      return *reinterpret_cast<const v4i *>(s_lds + ((from ^ kk * 64) + slot * kBuf) + f * 16 * kBk);
     }
   };
 
@@ -243,160 +244,86 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   arrived();
   while (true) {
     asm volatile("s_barrier" : : : "memory");
-    v16f acc[kFn][kFm] = {};
-    // (8-bit: parts of A come one row of products ahead instead of one depth)
-    constexpr int kSets = S::kFp8 ? 1 : 2;
-    Part fa[kSets][kFn], fb[2][kFm];
-    int scale[kFn + kFm], scale_next[kFn + kFm];
-    auto fetch = [&](int slot, int kk, int f) {
-      if (f < kFn)
-        fa[kk % kSets][f] = read(std::bool_constant<S::kTransA>(), std::integral_constant<int, S::kN>(),
-                               from_a, f, slot, kk);
-      else
-        fb[kk & 1][f - kFn] = read(std::bool_constant<S::kTransB>(), std::integral_constant<int, S::kM>(),
-                                   from_b, f - kFn, slot, kk);
+    // A depth's products are made in two halves of A's parts, each with one part of B after
+    // the other.  While one half is worked on the parts of the next are read; in a depth's
+    // second half each part of B makes room for the next depth's as soon as it is done with.
+    constexpr int kHalf = kFn / 2, kHalves = S::kDepths * 2, kAll = kHalf * kFm;
+    v4f acc[kFn][kFm] = {};
+    Part fa[2][kHalf], fb[kFm];
+    int scale[kFn + kFm];
+    auto fetch_a = [&](int slot, int h, int i) {
+      fa[h & 1][i] = read(std::bool_constant<S::kTransA>(), WidthA(), from_a, (h & 1) * kHalf + i, slot, h / 2);
     };
-    auto fetch_scales = [&](int group, int *to) {
+    auto fetch_b = [&](int slot, int kk, int j) {
+      fb[j] = read(std::bool_constant<S::kTransB>(), WidthB(), from_b, j, slot, kk);
+    };
+    auto fetch_scales = [&](int group) {
       const int8_t *b = s_lds + S::kScaleAt + (group & 1) * (S::kN + S::kM) * 4;
 #pragma unroll
-      for (int f = 0; f < kFn; ++f) to[f] = *reinterpret_cast<const int *>(b + ((wn * kFn + f) * 32 + lr) * 4);
+      for (int f = 0; f < kFn; ++f) scale[f] = *reinterpret_cast<const int *>(b + ((wn * kFn + f) * 16 + lr) * 4);
 #pragma unroll
       for (int f = 0; f < kFm; ++f)
-        to[kFn + f] = *reinterpret_cast<const int *>(b + (S::kN + (wm * kFm + f) * 32 + lr) * 4);
+        scale[kFn + f] = *reinterpret_cast<const int *>(b + (S::kN + (wm * kFm + f) * 16 + lr) * 4);
     };
-    // the elements of a part past the step's `left` become 0 on both sides (0 times what
-    // lies there could be a NaN)
-    auto clear = [&](int kk, int left) {
-      const int mine = left - (kk * 16 + hi * 8);
-      int keep[4];
+    // the products up to here are made here, not where their sums are next used
+    auto made = [&] {
 #pragma unroll
-      for (int d = 0; d < 4; ++d) keep[d] = mine >= 2 * d + 2 ? -1 : mine == 2 * d + 1 ? 0xFFFF : 0;
+      for (int i = 0; i < kFn; ++i)
 #pragma unroll
-      for (int f = 0; f < kFn + kFm; ++f) {
-        Part &p = f < kFn ? fa[kk % kSets][f] : fb[kk & 1][f < kFn ? 0 : f - kFn];
-#pragma unroll
-        for (int d = 0; d < 4; ++d) p[d] &= keep[d];
-      }
+        for (int j = 0; j < kFm; ++j) asm volatile("" : "+a"(acc[i][j]));
     };
-    auto clear8 = [&](int kk, int left, auto &p) {  // (whole chunks of 16)
-      const int mine = left - (kk * 64 + hi * 32);
-#pragma unroll
-      for (int d = 0; d < (S::kFp8 ? 8 : 0); ++d)
-        if (mine <= d / 4 * 16) p[d] = 0;
-    };
-    // One step, its first parts already in registers.  Reads of the next parts, and at the
-    // step's end the loads of the step after the next, lie between the products.  kMore:
-    // how many steps follow, up to 2.
-    auto next_arrives = [&](auto ahead) {
-      // the next step's bytes are there, and nobody reads this step's any more
-      if (decltype(ahead)::value == 2) {
-        work.advance();
-        left_load = work.left;
-      }
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    };
-    auto step16 = [&](int s, auto ahead) {
+    // One step, its first parts already in registers; its other reads and the loads of the
+    // steps that follow lie between the products.  kMore: how many follow, up to 2.
+    auto step = [&](int s, auto ahead) {
       constexpr int kMore = decltype(ahead)::value;
       const int slot = s & 1;
-#pragma unroll
-      for (int kk = 0; kk < kDepths; ++kk) {
-        if (kk == kDepths - 1) next_arrives(ahead);
-        if (Work::kRagged) {
-          if (left_now < S::kStep) clear(kk, left_now);
-        } else if (kMore == 0) {
-          if (work.tail < (kk + 1) * 16) clear(kk, work.tail);
-        }
-        constexpr int kAll = kFn * kFm, kParts = kFn + kFm;
-#pragma unroll
-        for (int m = 0; m < kAll; ++m) {
-          const int i = m / kFm, j = m % kFm;
-          acc[i][j] = multiply<S::kKind>(fa[kk % kSets][i], 0, fb[kk & 1][j], 0, acc[i][j]);
-          // spread evenly over the products
-          for (int f = m * kParts / kAll; f < (m + 1) * kParts / kAll; ++f) {
-            if (kk < kDepths - 1) fetch(slot, kk + 1, f);
-            else if (kMore > 0) fetch(slot ^ 1, 0, f);
-          }
-          if (kk == kDepths - 1 && kMore == 2)
-            for (int f = m * kLoads / kAll; f < (m + 1) * kLoads / kAll; ++f) issue(slot, f);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      left_now = left_next;
-      left_next = left_load;
-    };
-    // The same for 8-bit elements, whose parts are twice as large: a part of A is read
-    // kLead rows of products before its own, into the place of one that is done with.
-    constexpr int kLead = kFn / 2;
-    auto step8 = [&](int s, auto ahead) {
-      constexpr int kMore = decltype(ahead)::value, kRows = kDepths * kFn;
-      const int slot = s & 1;
-      if (kMore == 0 && work.tail <= 64) {  // (its first depth's parts of B, first kLead of A)
-#pragma unroll
-        for (int j = 0; j < kFm; ++j) clear8(0, work.tail, fb[0][j]);
-      }
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        const int kk = r / kFn, i = r % kFn;
-        if (r == kRows - kLead) {
-          next_arrives(ahead);
-          if (kMore > 0 && (s & 3) == 3) fetch_scales((s + 1) >> 2, scale_next);
-          if (kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
-        }
-        if (kMore == 0 && work.tail < S::kStep) {
-          clear8(kk, work.tail, fa[0][i]);
-          if (i == 0 && kk > 0) {
-#pragma unroll
-            for (int j = 0; j < kFm; ++j) clear8(kk, work.tail, fb[kk & 1][j]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < kFm; ++j) {
-          acc[i][j] = multiply<S::kKind>(fa[0][i], scale[i], fb[kk & 1][j], scale[kFn + j], acc[i][j]);
-          // between the products: A's part kLead rows on, B's parts of the next depth, all of
-          // them in the last rows where that is the next step's
-          if (j == kFm - 1) {
-            const int to = r + kLead;
-            if (to < kRows) fetch(slot, to / kFn, to % kFn);
-            else if (kMore > 0) fetch(slot ^ 1, 0, to - kRows);
-          }
-          if (kk < kDepths - 1) {
-            for (int f = (i * kFm + j) * kFm / (kFn * kFm); f < (i * kFm + j + 1) * kFm / (kFn * kFm); ++f)
-              fetch(slot, kk + 1, kFn + f);
-          } else if (r >= kRows - kLead) {
-            const int at = (r - (kRows - kLead)) * kFm + j, all = kLead * kFm;
-            if (kMore > 0)
-              for (int f = at * kFm / all; f < (at + 1) * kFm / all; ++f) fetch(slot ^ 1, 0, kFn + f);
-            if (kMore == 2)
-              for (int f = at * kLoads / all; f < (at + 1) * kLoads / all; ++f) issue(slot, f);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      if (kMore > 0) {
-        if ((s & 3) == 3) {
-#pragma unroll
-          for (int f = 0; f < kFn + kFm; ++f) scale[f] = scale_next[f];
-        } else {
-#pragma unroll
-          for (int f = 0; f < kFn + kFm; ++f) scale[f] = static_cast<int>(static_cast<uint32_t>(scale[f]) >> 8);
-        }
-      }
-    };
-    auto step = [&](int s, auto ahead) {
       // (else every part's address would be held throughout)
       from_a = opaque(from_a);
       from_b = opaque(from_b);
-      if constexpr (S::kFp8) step8(s, ahead);
-      else step16(s, ahead);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const int kk = h / 2;
+        const bool last = h == kHalves - 1;
+        if (last) {  // the next step's bytes are there, and nobody reads this step's any more
+          if (S::kFp8) made();
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+          if (S::kFp8 && kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
+        }
+#pragma unroll
+        for (int m = 0; m < kAll; ++m) {
+          const int j = m / kHalf, i = m % kHalf, f = h % 2 * kHalf + i;
+          acc[f][j] = multiply<S::kKind>(fa[h & 1][i], scale[f], fb[j], scale[kFn + j], acc[f][j]);
+          if (!last || kMore > 0) {
+#pragma unroll
+            for (int n = m * kHalf / kAll; n < (m + 1) * kHalf / kAll; ++n)
+              fetch_a(last ? slot ^ 1 : slot, last ? 0 : h + 1, n);
+            if (h % 2 == 1 && i == kHalf - 1) fetch_b(last ? slot ^ 1 : slot, last ? 0 : kk + 1, j);
+          }
+          if (last && kMore == 2)
+#pragma unroll
+            for (int n = m * kLoads / kAll; n < (m + 1) * kLoads / kAll; ++n) issue(slot, n);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (S::kFp8) made();
+      if (S::kFp8 && kMore > 0) {
+#pragma unroll
+        for (int f = 0; f < kFn + kFm; ++f) scale[f] = static_cast<int>(static_cast<uint32_t>(scale[f]) >> 8);
+        if ((s & 3) == 3) fetch_scales((s + 1) >> 2);
+      }
     };
 
     if (loaded > 0) {
 #pragma unroll
-      for (int f = 0; f < kFn + kFm; ++f)
-        if (!S::kFp8 || f < kLead || f >= kFn) fetch(0, 0, f);
-      if (S::kFp8) fetch_scales(0, scale);
+      for (int i = 0; i < kHalf; ++i) fetch_a(0, 0, i);
+#pragma unroll
+      for (int j = 0; j < kFm; ++j) fetch_b(0, 0, j);
+      if (S::kFp8) fetch_scales(0);
       int s = 0;
-      for (; work.more(); ++s) step(s, std::integral_constant<int, 2>());
+      for (; work.more(); ++s) {
+        work.advance();
+        step(s, std::integral_constant<int, 2>());
+      }
       if (loaded == 2) step(s++, std::integral_constant<int, 1>());
       step(s, std::integral_constant<int, 0>());
     }
@@ -418,23 +345,24 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
 
 // Results of 32 rows x 64 channels (32 in fp32) leave through 4 KiB of LDS a wave, so that
 // a row's channels go out in whole lines.  A row's 16-byte slots are exchanged by the row.
-//   put: 4 neighbouring channels (q * 8 + eh * 4 on) of row er of the part at `half`
+//   put: what a lane has of a part, 4 neighbouring channels of a row: part h of the rows'
+//        and jj of the channels' 16s
 //   get: the 16 bytes that lane el stores of row p * 8 + el / 8
 struct Stage {
   int8_t *at;
-  int er, eh, el;
+  int lr, lc, el;
   __device__ explicit Stage(int8_t *s) : at(s) {
     el = opaque(lane_id());
-    er = el & 31;
-    eh = el >> 5;
+    lr = el & 15;
+    lc = el >> 4;
   }
-  __device__ void put(int half, int q, const float *v, std::true_type) const {
-    const int slot = (half * 4 + q) ^ (er & 7);
-    *reinterpret_cast<v2u *>(at + er * 128 + slot * 16 + eh * 8) = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  __device__ void put(int h, int jj, v4f v, std::true_type) const {
+    const int r = jj * 16 + lr, slot = (h * 2 + lc / 2) ^ (r & 7);
+    *reinterpret_cast<v2u *>(at + r * 128 + slot * 16 + lc % 2 * 8) = v2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
-  __device__ void put(int, int q, const float *v, std::false_type) const {
-    const int slot = (q * 2 + eh) ^ (er & 7);
-    *reinterpret_cast<v4f *>(at + er * 128 + slot * 16) = v4f{v[0], v[1], v[2], v[3]};
+  __device__ void put(int h, int jj, v4f v, std::false_type) const {
+    const int r = jj * 16 + lr, slot = (h * 4 + lc) ^ (r & 7);
+    *reinterpret_cast<v4f *>(at + r * 128 + slot * 16) = v;
   }
   __device__ int row(int p) const { return p * 8 + el / 8; }
   template <class V>
@@ -469,15 +397,15 @@ __device__ __forceinline__ void swiglu_grad(float v, float a, float b, float &da
 
 // Items item, item + stride, .. below n_item, item 0 being that numbered `first`.  An item
 // is a tile that `tiles` numbers, or (kPart = 2) a quarter of one, 2 x 2.  With SwiGLU a
-// wave's parts of 32 channels alternate between gates and their partners, so that a gate's
+// wave's groups of 32 channels alternate between gates and their partners, so that a gate's
 // sum meets its partner's in the same lane.
 template <class S, int kPart, int kAct, bool kBf16>
 struct ProductWork {
-  static constexpr bool kRagged = false, kGlu = kAct == ULTRAEP_SWIGLU;
+  static constexpr bool kGlu = kAct == ULTRAEP_SWIGLU;
   static constexpr int kOut = kGlu ? S::kN / 2 : S::kN;  // channels of an item
   static constexpr int kOutW = kOut / S::kWn;            // of a wave
   static constexpr int kEsize = S::kFp8 ? 1 : 2;
-  static_assert(!kGlu || S::kFn % 2 == 0, "a wave has gates with their partners");
+  static_assert(!kGlu || S::kFn % 4 == 0, "a wave has gates with their partners");
 
   const ProductArgs &a;
   const int N, K, n_out;  // (held: a reload could look like another value in some lanes)
@@ -570,8 +498,9 @@ struct ProductWork {
   };
   __device__ Out out() const { return {tile.row, tile.rows, n0}; }
 
-  // (the gradient of SwiGLU) the gates and partners of a part, of the next one while one
-  // is worked on
+  // Results leave by 32 rows and 32 or 64 channels.  (The gradient of SwiGLU) the gates and
+  // partners of 32 x 32, of the next ones while some are worked on:
+  static constexpr int kBands = S::kFm / 2, kCols = kOutW / 32;
   struct Kept {
     v2u g[2][4], u[2][4];
   };
@@ -580,10 +509,10 @@ struct ProductWork {
   __device__ void keep(const Out &o, Early &k, int n, int wn, int wm) const {
     if constexpr (kAct == ULTRAEP_SWIGLU_GRAD) {
       const int el = opaque(lane_id());
-      const int c = o.n0 + wn * kOutW + n % S::kFn * 32 + (el & 7) * 4;
+      const int c = o.n0 + wn * kOutW + n % kCols * 32 + (el & 7) * 4;
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
-        const int r = (wm * S::kFm + n / S::kFn) * 32 + p * 8 + el / 8;
+        const int r = (wm * kBands + n / kCols) * 32 + p * 8 + el / 8;
         k.g[n & 1][p] = k.u[n & 1][p] = v2u{0, 0};
         if (r < o.rows && c < N) {
           const uint16_t *at = a.pre + (o.row + r) * 2 * N + c;
@@ -598,18 +527,20 @@ struct ProductWork {
   template <class Acc>
   __device__ void results(const Out &o, Early &kept, Acc &acc, int8_t *lds, int wn, int wm) const {
     const Stage st(lds);
-    constexpr int kFn = S::kFn, kFm = S::kFm, kSize = kBf16 ? 2 : 4;
-    constexpr int kParts = kOutW / 32, kGroup = kBf16 ? 2 : 1;  // parts that the stage takes
+    constexpr int kSize = kBf16 ? 2 : 4;
     const int nw = o.n0 + wn * kOutW, limit = min(n_out, nw + kOutW);
     char *const y = static_cast<char *>(a.y);
 #pragma unroll
-    for (int j = 0; j < kFm; ++j) {
-      const int r0 = (wm * kFm + j) * 32;
+    for (int b = 0; b < kBands; ++b) {
+      const int r0 = (wm * kBands + b) * 32;
       // the sums stay in the accumulation registers until here
 #pragma unroll
-      for (int i = 0; i < kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
+      for (int i = 0; i < S::kFn; ++i) {
+        asm volatile("" : "+a"(acc[i][2 * b]));
+        asm volatile("" : "+a"(acc[i][2 * b + 1]));
+      }
       // before the last stores: all loads, and the earlier stores, are done
-      if (S::kAhead && j == kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      if (S::kAhead && b == kBands - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       else asm volatile("" : : : "memory");
       // the stage's channels to rows of ld elements, from channel c0 on, below `end`
       auto leave = [&](char *dst, int64_t ld, int size, int c0, int end) {
@@ -623,20 +554,21 @@ struct ProductWork {
         }
         __builtin_amdgcn_sched_barrier(0);
       };
-      auto put = [&](auto bf16, int h, int q, auto value) {
-        float v[4];
+      // the channels' 16s from `from` on, as many as the stage takes and there are
+      auto put = [&](auto bf16, int from, auto value) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = value(q * 4 + e);
-        st.put(h, q, v, bf16);
+        for (int h = 0; h < (decltype(bf16)::value ? 4 : 2) && from + h < 2 * kCols; ++h)
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) st.put(h, jj, value(from + h, 2 * b + jj), bf16);
       };
+      // (SwiGLU) the part of A with the gates of the 16 channels i; their partners' is 2 on
+      auto gate = [](int i) { return i / 2 * 4 + i % 2; };
       if constexpr (kAct == ULTRAEP_SWIGLU_GRAD) {
 #pragma unroll
-        for (int i = 0; i < kFn; ++i) {
-          const int n = j * kFn + i, c = nw + i * 32 + (st.el & 7) * 4;
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            put(std::false_type(), 0, q, [&](int e) { return acc[i][j][e]; });
-          if (n + 1 < kFn * kFm) keep(o, kept, n + 1, wn, wm);
+        for (int i = 0; i < kCols; ++i) {
+          const int n = b * kCols + i, c = nw + i * 32 + (st.el & 7) * 4;
+          put(std::false_type(), 2 * i, [&](int f, int j) { return acc[f][j]; });
+          if (n + 1 < kBands * kCols) keep(o, kept, n + 1, wn, wm);
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
             const int r = r0 + st.row(p);
@@ -667,27 +599,22 @@ struct ProductWork {
 #pragma unroll
           for (int s = 0; s < 2; ++s)  // gates, partners
 #pragma unroll
-            for (int i = 0; i < kParts; i += 2) {
-#pragma unroll
-              for (int h = 0; h < 2 && i + h < kParts; ++h)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                  put(std::true_type(), h, q, [&](int e) { return acc[2 * (i + h) + s][j][e]; });
+            for (int i = 0; i < kCols; i += 2) {
+              put(std::true_type(), 2 * i, [&](int f, int j) { return acc[gate(f) + 2 * s][j]; });
               leave(reinterpret_cast<char *>(a.pre), N, 2, s * half + nw + i * 32, s * half + limit);
             }
         }
       }
 #pragma unroll
-      for (int i = 0; i < kParts; i += kGroup) {
-#pragma unroll
-        for (int h = 0; h < kGroup && i + h < kParts; ++h)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int f = kGlu ? 2 * (i + h) : i + h;
-            put(std::bool_constant<kBf16>(), h, q, [&](int e) {
-              return kGlu ? silu(acc[f][j][e]) * acc[kGlu ? f + 1 : f][j][e] : acc[f][j][e];
-            });
+      for (int i = 0; i < kCols; i += kBf16 ? 2 : 1) {
+        put(std::bool_constant<kBf16>(), 2 * i, [&](int f, int j) {
+          if constexpr (kGlu) {
+            const v4f g = acc[gate(f)][j], u = acc[gate(f) + 2][j];
+            return v4f{silu(g[0]) * u[0], silu(g[1]) * u[1], silu(g[2]) * u[2], silu(g[3]) * u[3]};
+          } else {
+            return acc[f][j];
           }
+        });
         leave(y, n_out, kSize, nw + i * 32, limit);
       }
     }

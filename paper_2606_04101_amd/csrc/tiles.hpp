@@ -116,7 +116,21 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint
                : "memory", "m0");
 }
 
-// the same for 4 bytes a lane
+// the same where an offset of kBufferBytes or more stands for zeros: 16 bytes a lane from a
+// buffer of that many bytes at `base`
+constexpr uint32_t kBufferBytes = 1u << 31;
+__device__ __forceinline__ void buffer_to_lds(const void *base, uint32_t off, uint32_t lds) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(base);
+  // (address, no stride; bytes; raw 32-bit data)
+  const v4i buffer = {static_cast<int>(at), static_cast<int>(at >> 32 & 0xFFFF), static_cast<int>(kBufferBytes),
+                      0x00020000};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(off), "s"(buffer)
+               : "memory", "m0");
+}
+
+// 4 bytes a lane, as the first
 __device__ __forceinline__ void load_word_to_lds(const void *base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                :

@@ -22,8 +22,6 @@ struct GradArgs {
 // runs of 64, one a lane.
 template <class S, bool kBf16, bool kAdd>
 struct GradWork {
-  static constexpr bool kRagged = true;
-  static constexpr int tail = S::kStep;
   static constexpr uint32_t pitch = 0;
   const GradArgs &a;
   const int N, K, n_block, n_run, tn, tk, stride, n_item;
@@ -142,8 +140,8 @@ struct GradWork {
   // Added to what is there the sums leave LDS in fp32, 4 channels a lane; a bf16 gradient
   // that is not added to leaves as such, 8.
   static constexpr bool kPacked = kBf16 && !kAdd;
-  static constexpr int kLane = kPacked ? 8 : 4, kParts = S::kFn * 4 / kLane;
-  static constexpr int kSize = kBf16 ? 2 : 4;
+  static constexpr int kLane = kPacked ? 8 : 4, kParts = S::kFn * 2 / kLane;
+  static constexpr int kSize = kBf16 ? 2 : 4, kBands = S::kFm / 2;  // (of 32 rows)
   using Word = std::conditional_t<kBf16 && kAdd, v2u, v4u>;  // what a lane stores
   // (added to) what is there, of the next part while one is worked on
   struct Old {
@@ -153,8 +151,8 @@ struct GradWork {
   using Early = std::conditional_t<kAdd, Old, Nothing>;
   // the address of what lane el stores of row p * 8 + el / 8 of part n; null outside
   __device__ char *place(const Out &o, int n, int p, int wn, int wm, int el) const {
-    const int r = o.n0 + (wm * S::kFm + n / kParts) * 32 + p * 8 + el / 8;
-    const int c = o.k0 + wn * S::kFn * 32 + (n % kParts * 8 + (el & 7)) * kLane;
+    const int r = o.n0 + (wm * kBands + n / kParts) * 32 + p * 8 + el / 8;
+    const int c = o.k0 + wn * S::kFn * 16 + (n % kParts * 8 + (el & 7)) * kLane;
     if (r >= N || c >= K || o.skip) return nullptr;
     const int64_t at = (static_cast<int64_t>(o.part) * a.n_w + o.weight) * a.dw_stride + static_cast<int64_t>(r) * K + c;
     return static_cast<char *>(a.dw) + at * kSize;
@@ -175,25 +173,24 @@ struct GradWork {
   __device__ void results(const Out &o, Early &old, Acc &acc, int8_t *lds, int wn, int wm) const {
     const Stage st(lds);
 #pragma unroll
-    for (int j = 0; j < S::kFm; ++j) {
+    for (int b = 0; b < kBands; ++b) {
 #pragma unroll
-      for (int i = 0; i < S::kFn; ++i) asm volatile("" : "+a"(acc[i][j]));
+      for (int i = 0; i < S::kFn; ++i) {
+        asm volatile("" : "+a"(acc[i][2 * b]));
+        asm volatile("" : "+a"(acc[i][2 * b + 1]));
+      }
       // before the last stores: all loads, and the earlier stores, are done
-      if (S::kAhead && j == S::kFm - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      if (S::kAhead && b == kBands - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       else asm volatile("" : : : "memory");
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
-        const int n = j * kParts + i;
+        const int n = b * kParts + i;
 #pragma unroll
-        for (int h = 0; h < kLane / 4; ++h)
+        for (int h = 0; h < kLane / 2; ++h)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = acc[i * kLane / 4 + h][j][q * 4 + e];
-            st.put(h, q, v, std::bool_constant<kPacked>());
-          }
-        if (n + 1 < S::kFm * kParts) keep(o, old, n + 1, wn, wm);
+          for (int jj = 0; jj < 2; ++jj)
+            st.put(h, jj, acc[i * kLane / 2 + h][2 * b + jj], std::bool_constant<kPacked>());
+        if (n + 1 < kBands * kParts) keep(o, old, n + 1, wn, wm);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           char *at = place(o, n, p, wn, wm, st.el);
