@@ -78,21 +78,33 @@ __device__ __forceinline__ float scale_value(int byte) {
   byte &= 255;
   return byte == 255 ? __builtin_nanf("") : __int_as_float(byte << 23);
 }
-// c + a b for 16 x 16 parts over 32 elements of bf16, or 128 of 8 bits with their scales
-template <Math kKind>
-__device__ __forceinline__ v4f multiply(const v4i &a, int, const v4i &b, int, v4f c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+// c += a b for 16 x 16 parts over 32 elements of bf16, or 128 of 8 bits with their scales.
+// kTied: the wave's sums take all 256 accumulation registers, where the compiler, left to
+// choose another register for a product's result than for its addend, copies sums about.
+// It does not know these instructions' latencies: `settle` stands between what writes their
+// operands with the vector ALU and them, and between them and the reading of the sums.
+template <Math kKind, bool kTied>
+__device__ __forceinline__ void multiply(const v4i &a, int, const v4i &b, int, v4f &c) {
+  if constexpr (kTied)
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
 }
-template <Math kKind>
-__device__ __forceinline__ v4f multiply(const v8i &a, int scale_a, const v8i &b, int scale_b, v4f c) {
-  if constexpr (kKind == kMath8)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
-  const float sa = scale_value(scale_a), sb = scale_value(scale_b);
+template <Math kKind, bool kTied>
+__device__ __forceinline__ void multiply(const v8i &a, int scale_a, const v8i &b, int scale_b, v4f &c) {
+  if constexpr (kKind == kMath8 && kTied) {
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                 : "+a"(c)
+                 : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
+  } else if constexpr (kKind == kMath8) {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+  } else {
+    const float sa = scale_value(scale_a), sb = scale_value(scale_b);
 #pragma unroll
-  for (int d = 0; d < 8; d += 2)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, widen8(a[d], a[d + 1], sa)),
-                                                __builtin_bit_cast(v8b, widen8(b[d], b[d + 1], sb)), c, 0, 0, 0);
-  return c;
+    for (int d = 0; d < 8; d += 2)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, widen8(a[d], a[d + 1], sa)),
+                                                  __builtin_bit_cast(v8b, widen8(b[d], b[d + 1], sb)), c, 0, 0, 0);
+  }
 }
 
 // Work: the items and their addresses.
@@ -265,13 +277,24 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       for (int f = 0; f < kFm; ++f)
         scale[kFn + f] = *reinterpret_cast<const int *>(b + (S::kN + (wm * kFm + f) * 16 + lr) * 4);
     };
-    // the products up to here are made here, not where their sums are next used
-    auto made = [&] {
+    constexpr bool kTied = kFn * kFm * 4 == 256 && !S::kWide;
+    // the sums are written and may be read, by products (of 8 passes) or by others
+    auto settle = [&] {
+      if (!kTied) return;
+      asm volatile("s_nop 15\n\ts_nop 15" : : : "memory");
 #pragma unroll
       for (int i = 0; i < kFn; ++i)
 #pragma unroll
         for (int j = 0; j < kFm; ++j) asm volatile("" : "+a"(acc[i][j]));
+      asm volatile("s_nop 1" : : : "memory");
     };
+    // the scales are (a shift or two ago at the least)
+    auto settle_scales = [&] {
+#pragma unroll
+      for (int f = 0; f < kFn + kFm; ++f) asm volatile("" : "+v"(scale[f]));
+      asm volatile("s_nop 1" : : : "memory");
+    };
+    settle();
     // One step, its first parts already in registers; its other reads and the loads of the
     // steps that follow lie between the products.  kMore: how many follow, up to 2.
     auto step = [&](int s, auto ahead) {
@@ -285,14 +308,13 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
         const int kk = h / 2;
         const bool last = h == kHalves - 1;
         if (last) {  // the next step's bytes are there, and nobody reads this step's any more
-          if (S::kFp8) made();
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
           if (S::kFp8 && kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
         }
 #pragma unroll
         for (int m = 0; m < kAll; ++m) {
           const int j = m / kHalf, i = m % kHalf, f = h % 2 * kHalf + i;
-          acc[f][j] = multiply<S::kKind>(fa[h & 1][i], scale[f], fb[j], scale[kFn + j], acc[f][j]);
+          multiply<S::kKind, kTied>(fa[h & 1][i], scale[f], fb[j], scale[kFn + j], acc[f][j]);
           if (!last || kMore > 0) {
 #pragma unroll
             for (int n = m * kHalf / kAll; n < (m + 1) * kHalf / kAll; ++n)
@@ -305,11 +327,11 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      if (S::kFp8) made();
       if (S::kFp8 && kMore > 0) {
 #pragma unroll
         for (int f = 0; f < kFn + kFm; ++f) scale[f] = static_cast<int>(static_cast<uint32_t>(scale[f]) >> 8);
         if ((s & 3) == 3) fetch_scales((s + 1) >> 2);
+        if (kTied) settle_scales();
       }
     };
 
@@ -326,6 +348,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       }
       if (loaded == 2) step(s++, std::integral_constant<int, 1>());
       step(s, std::integral_constant<int, 0>());
+      settle();
     }
 
     const auto out = work.out();
