@@ -128,12 +128,9 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   const uint32_t lds0 = lds_address(s_lds);
 
   // A wave's load of 1 KiB: of a contiguous side 8 rows of 8 chunks, chunk c of row r at
-  // c ^ (r / 2 % 8); of a transposed side whole rows.  This lane's chunk and, of a
-  // transposed side, row in the first load:
+  // c ^ (r / 2 % 8); of a transposed side whole rows.
   const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
   constexpr int kRowsA = 512 / S::kN, kRowsB = 512 / S::kM;  // of a load
-  const int first_a = wave * kRowsA + lane / (S::kN / 8);
-  const int first_b = wave * kRowsB + lane / (S::kM / 8);
   uint32_t off[kLoads];
 
   auto aim = [&] {
@@ -166,19 +163,17 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     }
   };
   // Load i of a step into buffer `slot`.  What lies past the step's elements becomes 0, on
-  // both sides (0 times what lies there could be a NaN): its offset is out of the buffer's
-  // range.
+  // both sides (0 times what lies there could be a NaN), by offsets out of the buffer's
+  // range: of a transposed side, whose rows lie in order, by the range, else by `past`.
+  uint32_t past = 0;
+  auto aim_step = [&] { past = chunk * (S::kStep / 8) < work.left ? 0 : kBufferBytes; };
   auto issue = [&](int slot, int i) {
-    const bool a = i < kLoadsA;
-    const int n = a ? i : i - kLoadsA;
-    bool in;
-    if (a ? S::kTransA : S::kTransB)
-      in = (a ? n * kWaves * kRowsA + first_a : n * kWaves * kRowsB + first_b) < work.left;
-    else
-      in = chunk * (S::kStep / 8) < work.left;
+    const bool a = i < kLoadsA, trans = a ? S::kTransA : S::kTransB;
     const int8_t *base = !a ? work.pb : work.second(i * kWaves + wave) ? work.pa2 : work.pa;
-    buffer_to_lds(base, in ? +off[i] : kBufferBytes,
-                  __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + (i * kWaves + wave) * 1024));
+    const uint32_t range = !trans || work.left == S::kStep ? kBufferBytes : work.left * (a ? work.pitch_a : work.pitch_b);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + slot * kBuf + wave * 1024);
+    if (trans) buffer_to_lds(base, range, off[i], lds, i * kWaves * 1024);
+    else buffer_to_lds(base, range, off[i], past, lds, i * kWaves * 1024);
   };
   // (8-bit) the words that hold 4 steps' scales of every channel and row
   auto issue_scales = [&](int group) {
@@ -200,12 +195,14 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     if (S::kFp8) issue_scales(0);
     if (work.more()) {
       work.advance();
+      aim_step();
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) issue(0, i);
       loaded = 1;
     }
     if (work.more()) {
       work.advance();
+      aim_step();
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) issue(1, i);
       loaded = 2;
@@ -300,9 +297,10 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     auto step = [&](int s, auto ahead) {
       constexpr int kMore = decltype(ahead)::value;
       const int slot = s & 1;
-      // (else every part's address would be held throughout)
-      from_a = opaque(from_a);
-      from_b = opaque(from_b);
+      if (S::kFp8) {  // (else every part's address would be held throughout)
+        from_a = opaque(from_a);
+        from_b = opaque(from_b);
+      }
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
         const int kk = h / 2;
@@ -344,6 +342,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       int s = 0;
       for (; work.more(); ++s) {
         work.advance();
+        aim_step();
         step(s, std::integral_constant<int, 2>());
       }
       if (loaded == 2) step(s++, std::integral_constant<int, 1>());

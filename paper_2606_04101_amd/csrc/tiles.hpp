@@ -116,18 +116,28 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint
                : "memory", "m0");
 }
 
-// the same where an offset of kBufferBytes or more stands for zeros: 16 bytes a lane from a
-// buffer of that many bytes at `base`
+// The same from a buffer of `range` bytes at `base`, to lds + at; where the offset is out of
+// range, as kBufferBytes always is, zeros are written.  `past` is added to an offset bit by
+// bit.
 constexpr uint32_t kBufferBytes = 1u << 31;
-__device__ __forceinline__ void buffer_to_lds(const void *base, uint32_t off, uint32_t lds) {
+__device__ __forceinline__ v4i buffer_of(const void *base, uint32_t range) {
   const uint64_t at = reinterpret_cast<uintptr_t>(base);
   // (address, no stride; bytes; raw 32-bit data)
-  const v4i buffer = {static_cast<int>(at), static_cast<int>(at >> 32 & 0xFFFF), static_cast<int>(kBufferBytes),
-                      0x00020000};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  return v4i{static_cast<int>(at), static_cast<int>(at >> 32 & 0xFFFF), static_cast<int>(range), 0x00020000};
+}
+__device__ __forceinline__ void buffer_to_lds(const void *base, uint32_t range, uint32_t off, uint32_t lds, int at) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(lds), "v"(off), "s"(buffer)
-               : "memory", "m0");
+               : "s"(lds), "v"(off), "s"(buffer_of(base, range)), "n"(at)
+               : "memory", "m0", "scc");
+}
+__device__ __forceinline__ void buffer_to_lds(const void *base, uint32_t range, uint32_t off, uint32_t past,
+                                              uint32_t lds, int at) {
+  uint32_t from;
+  asm volatile("s_add_u32 m0, %1, %5\n\tv_or_b32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds"
+               : "=&v"(from)
+               : "s"(lds), "v"(off), "v"(past), "s"(buffer_of(base, range)), "n"(at)
+               : "memory", "m0", "scc");
 }
 
 // 4 bytes a lane, as the first

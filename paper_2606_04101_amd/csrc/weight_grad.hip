@@ -70,7 +70,7 @@ struct GradWork {
     const int l = __builtin_ctzll(mask);
     mask &= mask - 1;
     row = readlane64(lo, l);
-    remaining = readlane(rows, l);
+    remaining = __builtin_amdgcn_readfirstlane(readlane(rows, l));
   }
   __device__ void first_block() {
     if (n_run == 1) {
@@ -119,7 +119,7 @@ struct GradWork {
   __device__ void advance() {
     pa = uniform(x + (row * K + k0) * 2);
     pb = uniform(dy + (row * N + n0) * 2);
-    left = min(remaining, S::kStep);
+    left = __builtin_amdgcn_readfirstlane(min(remaining, S::kStep));
     row += S::kStep;
     remaining -= left;
     --budget;
