@@ -6,7 +6,7 @@
 // channels of one row.  Either side may lie with the common index contiguous, or (kTrans)
 // with its channels or rows contiguous; such a side is transposed on its way from LDS.
 //   The loop is the one of the 8-bit integer products: steps of 128 bytes of the common
-// index through two LDS buffers, loads straight to LDS two steps ahead, one barrier a
+// index through LDS buffers, loads straight to LDS kRing steps ahead, one barrier a
 // step, kWn x kWm waves that stay and take tile after tile, and (kAhead) the next tile's
 // first loads in flight while the results leave.
 #pragma once
@@ -32,10 +32,11 @@ constexpr int kBk = 128;  // bytes of a step: of a contiguous side's row
 // fp32 result, which kMathWide makes of exact products summed in fp32, at half the rate.
 enum Math { kMath16, kMath8, kMathWide };
 
-template <int N, int M, int Wn, int Wm, bool Ahead, Math Kind, bool TransA, bool TransB>
+template <int N, int M, int Wn, int Wm, bool Ahead, int Ring, Math Kind, bool TransA, bool TransB>
 struct Tile {
   static constexpr bool Fp8 = Kind != kMath16, kWide = Kind == kMathWide;
   static constexpr int kN = N, kM = M, kWn = Wn, kWm = Wm;
+  static constexpr int kRing = Ring;  // LDS buffers, of a step each
   static constexpr bool kAhead = Ahead, kFp8 = Fp8, kTransA = TransA, kTransB = TransB;
   static constexpr int kWaves = Wn * Wm, kThreads = kWaves * kWave;
   static constexpr int kFn = N / Wn / 16, kFm = M / Wm / 16;  // 16 x 16 parts of a wave
@@ -43,12 +44,13 @@ struct Tile {
   static constexpr int kLoads = kBuf / 1024 / kWaves, kLoadsA = N / 8 / kWaves;  // of a wave in a step
   static constexpr int kStep = Fp8 ? 128 : 64;  // elements of the common index in a step
   static constexpr int kDepths = Fp8 ? 1 : 2;   // products of a pair of parts in a step
-  static constexpr int kScaleAt = 2 * kBuf + (Ahead ? kWaves * 4096 : 0);
+  static constexpr int kScaleAt = Ring * kBuf + (Ahead ? kWaves * 4096 : 0);
   static constexpr int kLds = kScaleAt + (Fp8 ? 2 * (N + M) * 4 : 0);
   static constexpr Math kKind = Kind;
   using Part = std::conditional_t<Fp8, v8i, v4i>;
   static_assert(kLoadsA * kWaves * 8 == N && kWaves % 2 == 0, "whole loads of each side");
-  static_assert(Ahead || kWaves * 4096 <= 2 * kBuf, "results take the place of the operands");
+  static_assert(Ahead || kWaves * 4096 <= Ring * kBuf, "results take the place of the operands");
+  static_assert(Ring == 2 || Ring == 4, "");
   static_assert(!Fp8 || !(TransA || TransB), "the transposing read is one of 16-bit elements");
   // from one of a wave's loads of a transposed side to the next are whole groups of 8 of
   // the common index
@@ -187,33 +189,33 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     }
   };
 
-  int loaded = 0;  // steps of the item loaded at its beginning, up to 2
+  constexpr int kRing = S::kRing;
+  int loaded = 0;  // steps of the item loaded at its beginning, up to kRing
   auto begin = [&] {
     if (!work.next_item()) return false;
     aim();
     loaded = 0;
     if (S::kFp8) issue_scales(0);
-    if (work.more()) {
+#pragma unroll
+    for (int r = 0; r < kRing; ++r) {
+      if (!work.more()) break;
       work.advance();
       aim_step();
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) issue(0, i);
-      loaded = 1;
-    }
-    if (work.more()) {
-      work.advance();
-      aim_step();
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) issue(1, i);
-      loaded = 2;
+      for (int i = 0; i < kLoads; ++i) issue(r, i);
+      loaded = r + 1;
     }
     return true;
   };
-  auto arrived = [&] {  // the first step's bytes are there
-    if (loaded == 2)
-      asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  // all but the latest n steps' loads are there
+  auto arrived = [&](auto n) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(decltype(n)::value * kLoads) : "memory");
+  };
+  auto first_arrived = [&] {
+    if (kRing == 4 && loaded == 4) arrived(std::integral_constant<int, 3>());
+    else if (kRing == 4 && loaded == 3) arrived(std::integral_constant<int, 2>());
+    else if (loaded == 2) arrived(std::integral_constant<int, 1>());
+    else arrived(std::integral_constant<int, 0>());
   };
 
   // What this lane reads of a part: 16 bytes of the common index of one channel or row (8
@@ -250,7 +252,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   };
 
   if (!begin()) return;
-  arrived();
+  first_arrived();
   while (true) {
     asm volatile("s_barrier" : : : "memory");
     // A depth's products are made in two halves of A's parts, each with one part of B after
@@ -293,10 +295,10 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     };
     settle();
     // One step, its first parts already in registers; its other reads and the loads of the
-    // steps that follow lie between the products.  kMore: how many follow, up to 2.
+    // step kRing on lie between the products.  kMore: how many steps follow, up to kRing.
     auto step = [&](int s, auto ahead) {
       constexpr int kMore = decltype(ahead)::value;
-      const int slot = s & 1;
+      const int slot = s & (kRing - 1), next = (s + 1) & (kRing - 1);
       if (S::kFp8) {  // (else every part's address would be held throughout)
         from_a = opaque(from_a);
         from_b = opaque(from_b);
@@ -306,8 +308,9 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
         const int kk = h / 2;
         const bool last = h == kHalves - 1;
         if (last) {  // the next step's bytes are there, and nobody reads this step's any more
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-          if (S::kFp8 && kMore == 2 && (s & 3) == 2) issue_scales((s + 2) >> 2);
+          arrived(std::integral_constant<int, (kMore < 2 ? 0 : kMore == kRing ? kRing - 2 : kMore - 1)>());
+          asm volatile("s_barrier" : : : "memory");
+          if (S::kFp8 && kMore == kRing && (s + kRing & 3) == 0) issue_scales((s + kRing) >> 2);
         }
 #pragma unroll
         for (int m = 0; m < kAll; ++m) {
@@ -316,10 +319,10 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
           if (!last || kMore > 0) {
 #pragma unroll
             for (int n = m * kHalf / kAll; n < (m + 1) * kHalf / kAll; ++n)
-              fetch_a(last ? slot ^ 1 : slot, last ? 0 : h + 1, n);
-            if (h % 2 == 1 && i == kHalf - 1) fetch_b(last ? slot ^ 1 : slot, last ? 0 : kk + 1, j);
+              fetch_a(last ? next : slot, last ? 0 : h + 1, n);
+            if (h % 2 == 1 && i == kHalf - 1) fetch_b(last ? next : slot, last ? 0 : kk + 1, j);
           }
-          if (last && kMore == 2)
+          if (last && kMore == kRing)
 #pragma unroll
             for (int n = m * kLoads / kAll; n < (m + 1) * kLoads / kAll; ++n) issue(slot, n);
           __builtin_amdgcn_sched_barrier(0);
@@ -343,9 +346,16 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       for (; work.more(); ++s) {
         work.advance();
         aim_step();
-        step(s, std::integral_constant<int, 2>());
+        step(s, std::integral_constant<int, kRing>());
       }
-      if (loaded == 2) step(s++, std::integral_constant<int, 1>());
+      // (as another value: paths of their own for each number of steps leave the compiler
+      // short of registers)
+      asm volatile("" : "+s"(loaded));
+      if constexpr (kRing == 4) {
+        if (loaded == 4) step(s++, std::integral_constant<int, 3>());
+        if (loaded >= 3) step(s++, std::integral_constant<int, 2>());
+      }
+      if (loaded >= 2) step(s++, std::integral_constant<int, 1>());
       step(s, std::integral_constant<int, 0>());
       settle();
     }
@@ -354,13 +364,13 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
     typename Work::Early early;
     work.early(out, early, wn, wm);
     const bool more = S::kAhead && begin();
-    work.results(out, early, acc, s_lds + (S::kAhead ? 2 * kBuf : 0) + wave * 4096, wn, wm);
+    work.results(out, early, acc, s_lds + (S::kAhead ? kRing * kBuf : 0) + wave * 4096, wn, wm);
     if (S::kAhead) {
       if (!more) return;
     } else {
       __syncthreads();
       if (!begin()) return;
-      arrived();
+      first_arrived();
     }
   }
 }
@@ -643,9 +653,9 @@ struct ProductWork {
   }
 };
 
-template <int kN, int kM, int kWn, int kWm, bool kAhead, Math kKind, bool kTrans, int kAct, bool kBf16>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, int kRing, Math kKind, bool kTrans, int kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32_t n_col) {
-  using S = Tile<kN, kM, kWn, kWm, kAhead, kKind, kTrans, false>;
+  using S = Tile<kN, kM, kWn, kWm, kAhead, kRing, kKind, kTrans, false>;
   __shared__ __align__(1024) int8_t s_lds[S::kLds];
   __shared__ int s_run[32];
   RowTiles<kM> tiles;
@@ -664,7 +674,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32
   }
   if constexpr (kAhead) {
     __syncthreads();
-    using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, kKind, kTrans, false>;
+    using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, 4, kKind, kTrans, false>;
     ProductWork<Q, 2, kAct, kBf16> work(a, tiles, n_col, n_item - last, slot, grid, last * 4);
     tile_items<Q>(work, s_lds);
   }

@@ -214,13 +214,13 @@ void start_thin(const ProductArgs &a, hipStream_t stream) {
   hipLaunchKernelGGL((k_product_thin<kTok, kRows, kWaves, kDeep, kKind, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
-template <int kN, int kM, int kWn, int kWm, bool kAhead, Math kKind, bool kTrans, int kAct, bool kBf16>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, int kRing, Math kKind, bool kTrans, int kAct, bool kBf16>
 void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
   const int out = kAct == ULTRAEP_SWIGLU ? kN / 2 : kN;
   const int32_t n_col = (a.n_out + out - 1) / out;
   const int64_t items = most_tiles(a, kM) * n_col;
   const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
-  hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kKind, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
+  hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kRing, kKind, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
 template <Math kKind, bool kTrans, int kAct, bool kBf16>
@@ -236,12 +236,12 @@ void choose_product(const ProductArgs &a, hipStream_t stream) {
   constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
   if constexpr (kKind != kMathWide) {
     if (rows > 64 && big_time < mid_time)
-      return start_product<256, 256, 2, 2, true, kKind, kTrans, kAct, kBf16>(a, 256, stream);
+      return start_product<256, 256, 2, 2, true, 2, kKind, kTrans, kAct, kBf16>(a, 256, stream);
   }
   if (rows > 56 && items(128, 128) >= 256)
-    return start_product<128, 128, 2, 2, false, kKind, kTrans, kAct, kBf16>(a, 512, stream);
+    return start_product<128, 128, 2, 2, false, 2, kKind, kTrans, kAct, kBf16>(a, 512, stream);
   if (!kThin || (rows > 32 && items(64, 128) >= 320))
-    return start_product<128, 64, 2, 1, false, kKind, kTrans, kAct, kBf16>(a, 768, stream);
+    return start_product<128, 64, 2, 1, false, 2, kKind, kTrans, kAct, kBf16>(a, 768, stream);
   if constexpr (kThin) {
     const bool deep = static_cast<int64_t>(a.K) * (kKind == kMath16 ? 2 : 1) >= 4096;
     if (rows > 32 && items(64, 64) >= 256 && deep) start_thin<64, 64, 4, 2, kKind, kAct, kBf16>(a, stream);

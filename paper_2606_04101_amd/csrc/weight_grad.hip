@@ -239,7 +239,7 @@ __device__ __forceinline__ bool sound_blocks(const GradArgs &a, int *s_sound) {
 
 template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
-  using S = Tile<kN, kM, kWn, kWm, kAhead, kMath16, true, true>;
+  using S = Tile<kN, kM, kWn, kWm, kAhead, 2, kMath16, true, true>;
   __shared__ __align__(1024) int8_t s_lds[S::kLds];
   __shared__ int s_sound[S::kWaves];
   if (!sound_blocks<S::kWaves>(a, s_sound)) return;
