@@ -668,15 +668,15 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32
   const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
   int last = 0;  // tiles of the last round that are taken by quarters
   if (kAhead && n_item % grid * 4 <= grid) last = n_item % grid;
-  {
-    ProductWork<S, 1, kAct, kBf16> work(a, tiles, n_col, 0, slot, grid, n_item - last);
-    tile_items<S>(work, s_lds);
-  }
   if constexpr (kAhead) {
-    __syncthreads();
     using Q = Tile<kN / 2, kM / 2, kWn, kWm, false, 4, kKind, kTrans, false>;
     ProductWork<Q, 2, kAct, kBf16> work(a, tiles, n_col, n_item - last, slot, grid, last * 4);
     tile_items<Q>(work, s_lds);
+    __syncthreads();
+  }
+  {
+    ProductWork<S, 1, kAct, kBf16> work(a, tiles, n_col, 0, slot, grid, n_item - last);
+    tile_items<S>(work, s_lds);
   }
 }
 
