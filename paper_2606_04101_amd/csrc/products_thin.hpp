@@ -223,33 +223,70 @@ void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
   hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kRing, kKind, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
+// The tiles by the rounds that they would take: a round is 256 of them, one a compute unit (of
+// 128 x 128 two a compute unit, 512), and its time is in hundredths of a round of 256 x 256,
+// bf16 / 8 bits.  `rows`: M over the blocks, of which the host cannot know how many are empty
+// (a list that is mostly empty, or an M above the rows that the blocks hold, is taken for
+// small or large blocks: the result is the same but for the order of the sums of K, the
+// time is not); items: estimated tiles, half a tile of padding a block where there are several.
+//   Measured, us (256 x 256 / 128 x 128, two buffers / four / 128 x 64, four / thin 64 / 32 /
+//   16; x: not run):
+//   bf16, 1 block, N = 4096, K = 7168: M = 10240 485 / 519 / 618 / 827, 8192 324 / 411 / 496 / 646,
+//   6144 320 / 290 / 333 / 428, 5120 218 / 288 / 274 / 344, 4096 163 / 194 / 222 / 281, 2560 143 /
+//   194 / 158 / 182, 2048 144 / 99 / 113 / 142, 1024 140 / 81 / 59 / 78 / 91 / 134, 512 139 / 72 / 54 /
+//   41 / 48 / 70 / x, 384 142 / 71 / 53 / 36 / 45 / 52 / 104, 256 140 / 70 / 52 / 35 / 24 / 35 / 70, 128
+//   140 / 70 / 51 / 35 / 23 / 19 / 37, 64 x / x / x / 35 / 23 / 18 / 19, 16 138 / 65 / 50 / 34 / 19 / 16 / 12
+//   10 blocks, the same with SwiGLU: M = 20480 998 / 1255 / 1336 / 1761, 7680 401 / 509 / 547 / 692,
+//   5120 275 / 413 / 362 / 509, 2560 213 / 287 / 228 / 269, 1024 196 / 156 / 158 / 162 / 169 / 229, 640
+//   x / x / x / 138 / 132 / 148 / 240, 320 x / x / x / 129 / 117 / 114 / 152, 160 x / x / x / 125 / 114 /
+//   110 / 105
+//   8 bits, 4 blocks, the same with SwiGLU: M = 16384 355 / 693 / 630 / 893, 4096 88 / 166 / 158 /
+//   221, 2048 83 / 90 / 86 / 116, 1024 79 / 87 / 47 / 63, 512 80 / 50 / 46 / 34; 1 block: M = 512 x / x / x /
+//   32 / 32 / 45 / 70, 256 x / x / x / 31 / 17 / 24 / 37, 128 x / x / x / 30 / 16 / 13 / 20, 16 x / x / x / 30 /
+//   14 / 11 / 7
+//   weights [K][N], 4 blocks, N = 2048, K = 4096: M = 16384 198 / 238 / 273 / 362, 4096 88 / 59 / 67 /
+//   90, 2048 85 / 49 / 34 / 47, 1024 85 / 41 / 32 / 24
+//   (Where the weights' bytes bound the call the choice misses the best by up to an eighth: 10
+//   blocks of 6 rows, weights [K][N], take 130 us of 128 x 64 where two tiles of 128 x 128 a
+//   compute unit take 114.)
 template <Math kKind, bool kTrans, int kAct, bool kBf16>
 void choose_product(const ProductArgs &a, hipStream_t stream) {
-  const int64_t blocks = a.M < a.n_block ? a.M : a.n_block, rows = (a.M + blocks - 1) / blocks;
+  const int64_t blocks = a.M < a.n_block ? a.M : a.n_block;
   auto items = [&](int64_t tile_rows, int64_t channels) {
     return (blocks > 1 ? a.M / tile_rows + (blocks + 1) / 2 : (a.M + tile_rows - 1) / tile_rows) *
            ((a.N + channels - 1) / channels);
   };
-  const int64_t big = items(256, 256), full = big / 256, last = big % 256;
-  const int64_t big_time = full * 10 + (last == 0 ? 0 : full && last <= 64 ? 4 : 10);
-  const int64_t mid_time = (items(128, 128) + 511) / 512 * 6;
+  auto rounds = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+  constexpr bool k8 = kKind == kMath8, kBig = kKind != kMathWide;
   constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
-  if constexpr (kKind != kMathWide) {
-    if (rows > 64 && big_time < mid_time)
-      return start_product<256, 256, 2, 2, true, 2, kKind, kTrans, kAct, kBf16>(a, 256, stream);
+  const bool deep = static_cast<int64_t>(a.K) * (kKind == kMath16 ? 2 : 1) >= 4096;  // four waves' worth of steps
+  const int64_t big = items(256, 256), full = big / 256, last = big % 256;
+  constexpr int64_t kNever = int64_t(1) << 60;
+  const int64_t time[] = {
+      kBig ? full * 1000 + (last == 0 ? 0 : full && last <= 64 ? 350 : 1000) : kNever,
+      rounds(items(128, 128), 512) * (k8 ? 1050 : 600),
+      rounds(items(128, 128), 256) * (k8 ? 550 : 360),
+      rounds(items(64, 128), 256) * (k8 ? 370 : 250),
+      kThin ? rounds(items(64, 64), 256) * (k8 ? 190 : 155) : kNever,
+      kThin ? rounds(items(32, 64), 256) * (k8 ? 135 : 115) : kNever,
+      kThin ? rounds(items(16, deep ? 32 : 64), 256) * (deep ? 70 : 80) : kNever,
+  };
+  int best = 0;
+  for (int i = 1; i < 7; ++i)
+    if (time[i] < time[best]) best = i;
+  if constexpr (kBig) {
+    if (best == 0) start_product<256, 256, 2, 2, true, 2, kKind, kTrans, kAct, kBf16>(a, 256, stream);
   }
-  if (rows > 56 && items(128, 128) >= 256)
-    return start_product<128, 128, 2, 2, false, 2, kKind, kTrans, kAct, kBf16>(a, 512, stream);
-  if (!kThin || (rows > 32 && items(64, 128) >= 320))
-    return start_product<128, 64, 2, 1, false, 2, kKind, kTrans, kAct, kBf16>(a, 768, stream);
+  if (best == 1) start_product<128, 128, 2, 2, false, 2, kKind, kTrans, kAct, kBf16>(a, 512, stream);
+  if (best == 2) start_product<128, 128, 2, 2, false, 4, kKind, kTrans, kAct, kBf16>(a, 256, stream);
+  if (best == 3) start_product<128, 64, 2, 2, false, 4, kKind, kTrans, kAct, kBf16>(a, 256, stream);
   if constexpr (kThin) {
-    const bool deep = static_cast<int64_t>(a.K) * (kKind == kMath16 ? 2 : 1) >= 4096;
-    if (rows > 32 && items(64, 64) >= 256 && deep) start_thin<64, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
-    else if (rows > 32 && items(64, 64) >= 256) start_thin<64, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
-    else if (rows > 12 && items(32, 64) >= 256 && deep) start_thin<32, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
-    else if (rows > 12 && items(32, 64) >= 256) start_thin<32, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
-    else if (deep) start_thin<16, 32, 4, 2, kKind, kAct, kBf16>(a, stream);
-    else start_thin<16, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 4 && deep) start_thin<64, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 4 && !deep) start_thin<64, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 5 && deep) start_thin<32, 64, 4, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 5 && !deep) start_thin<32, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 6 && deep) start_thin<16, 32, 4, 2, kKind, kAct, kBf16>(a, stream);
+    if (best == 6 && !deep) start_thin<16, 64, 2, 2, kKind, kAct, kBf16>(a, stream);
   }
 }
 
