@@ -237,6 +237,11 @@ __device__ __forceinline__ bool sound_blocks(const GradArgs &a, int *s_sound) {
   return __builtin_amdgcn_readfirstlane(every);
 }
 
+// dw = dy^T x, a weight's tiles of kM rows x kN columns.  As the products bound by the matrix
+// units' power, with two transposing reads more a part: 780 us at 8192^3 (1.41 PFLOP/s), 32768
+// rows of 5 weights of 4096 x 7168 to fp32 in 1583 to 1644 us (1.17 to 1.21): 2240 tiles are 8.75
+// rounds of 256 and the fp32 results 587 MB.  Few rows a weight are bound by the results' bytes
+// (2991 rows over 16 weights of 2880 x 1440, bf16: 53 us, of which the bytes take 30).
 template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
   using S = Tile<kN, kM, kWn, kWm, kAhead, 2, kMath16, true, true>;
@@ -305,13 +310,15 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 //   weights, K = 2048, M = 8192: N = 2048 94 / 64, 1024 67 / 49, 512 43 / 32; 8 weights, K = 1024,
 //   M = 8192: N = 2048 37 / 37, 1024 31 / 21; 64 weights, N = 1024, K = 2048: M = 4096 91 / 104; 16
 //   weights, N = 2880, K = 1440: M = 2000 69 / 56 (bf16 results 48 / 40)
+//   Out of a cache that holds no results yet: 16 weights, N = 2880, K = 1440: M = 8192 113 / 104, 2991
+//   to bf16 76 / 57; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
 template <bool kBf16, bool kAdd>
 static void choose_grad(const GradArgs &a, hipStream_t stream) {
   auto tiles = [&](int64_t n, int64_t k) {
     return int64_t(a.n_w) * a.parts * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
   };
   const int64_t big = (tiles(256, 256) + 255) / 256 * 20, mid = (tiles(128, 128) + 511) / 512 * 13;
-  const bool few = a.M < int64_t(256) * a.n_w && tiles(128, 128) < 4 * tiles(256, 256);
+  const bool few = a.M < int64_t(768) * a.n_w && tiles(128, 128) < 4 * tiles(256, 256);
   if (big < mid && !few) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
   else start_grad<128, 128, 2, 2, false, kBf16, kAdd>(a, 512, stream);
 }
