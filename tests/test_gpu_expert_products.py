@@ -142,6 +142,23 @@ def test_bf16_products_over_the_tile_shapes(sizes, N, K, trans, act):
     check_bf16(sizes, N, K, trans, act, f32=False, **shared(sizes))
 
 
+MANY = [  # enough tiles for the largest, whole rounds of them and not, and many blocks of middling rows
+    ([4096], 4088, 72), ([2000, 2230], 4088, 72), ([2040], 4096, 72), ([2040], 2040, 136), ([60] * 60, 264, 2056),
+    ([40] * 40, 264, 4104), ([50] * 50, 128, 136), ([50] * 50, 128, 4112)]
+
+
+@pytest.mark.parametrize("sizes,N,K", MANY)
+@pytest.mark.parametrize("trans,act", [(False, "none"), (True, "none"), (False, "swiglu"), (True, "swiglu"), (False, "swiglu_grad"), (True, "swiglu_grad")])
+def test_bf16_products_of_many_tiles(sizes, N, K, trans, act):
+    check_bf16(sizes, N // 16 * 16 if act == "swiglu" else N, K, trans, act, f32=False, **shared(sizes))
+
+
+@pytest.mark.parametrize("sizes,N,K", MANY[1:3] + MANY[4:6])
+@pytest.mark.parametrize("trans,act", [(True, "none"), (False, "swiglu")])
+def test_bf16_products_of_many_tiles_fp32_results(sizes, N, K, trans, act):
+    check_bf16(sizes, N // 16 * 16, K, trans, act, f32=True, **shared(sizes))
+
+
 @pytest.mark.parametrize("trans", [False, True])
 def test_bf16_products_of_other_numbers(trans):
     """Infinities and NaN stay in their row, channel and block."""
@@ -312,7 +329,8 @@ def test_weight_grad(sizes, N, K, f32):
     check_weight_grad(sizes, N, K, f32)
 
 
-@pytest.mark.parametrize("sizes,N,K", [([300, 77], 2056, 2056), ([70, 0, 130, 1, 64, 9], 2056, 2056), ([33], 4104, 4104)])
+@pytest.mark.parametrize("sizes,N,K", [([300, 77], 2056, 2056), ([70, 0, 130, 1, 64, 9], 2056, 2056), ([33], 4104, 4104),
+                                           ([300, 0, 513, 77], 2040, 2032), ([1, 65, 129, 64, 63], 2048, 2048)])
 @pytest.mark.parametrize("f32", [True, False])
 @pytest.mark.parametrize("accumulate", [True, False])
 def test_weight_grad_of_large_weights(sizes, N, K, f32, accumulate):
@@ -523,7 +541,8 @@ def fp8_product(sizes, N, K, act, f32, of=None, n_w=None, start=0, tail=0, seed=
 
 SHAPES8 = [
     ([1], 16, 16), ([1], 64, 4096), ([0, 3, 0], 48, 48), ([65, 0, 63, 1], 96, 144), ([130, 7], 272, 272),
-    ([5, 64, 128, 200], 144, 528), ([257], 528, 128), ([300, 300], 320, 400), ([16] * 4, 1040, 2064), ([40], 64, 3600)
+    ([5, 64, 128, 200], 144, 528), ([257], 528, 128), ([300, 300], 320, 400), ([16] * 4, 1040, 2064), ([40], 64, 3600),
+    ([200], 2064, 144)
 ] + [(s, n // 16 * 16, k // 16 * 16) for s, n, k in TILES]
 
 
@@ -549,6 +568,14 @@ def test_fp8_products_of_small_integers_are_exact(sizes, N, K, f32):
 @pytest.mark.parametrize("sizes,N,K", [(s, n // 16 * 16, k // 16 * 16) for s, n, k in TILES])
 def test_fp8_products_fp32_results_over_the_tile_shapes(sizes, N, K):
     got, want, err = fp8_product(sizes, N, K, "swiglu", True, **shared(sizes))
+    assert np.isfinite(got).all()
+    same_where_defined(got, want, err)
+
+
+@pytest.mark.parametrize("sizes,N,K", [(s, n // 16 * 16, k // 16 * 16) for s, n, k in MANY])
+@pytest.mark.parametrize("act,f32", [("none", False), ("swiglu", False), ("none", True)])
+def test_fp8_products_of_many_tiles(sizes, N, K, act, f32):
+    got, want, err = fp8_product(sizes, N, K, act, f32, **shared(sizes))
     assert np.isfinite(got).all()
     same_where_defined(got, want, err)
 
