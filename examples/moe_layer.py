@@ -5,9 +5,10 @@ and in serving.
   python examples/moe_layer.py
 
 Training: the router's ids, gates and balance loss, the load count's row taken
-from the router's counts, the plan, the dispatch, the experts (bf16, torch), the
-combine, and every backward pass; a few steps of SGD bring the balance loss down.
-Serving: the same layer with its experts in 8-bit integers.
+from the router's counts, the plan, the dispatch, the experts (bf16), the combine,
+and every backward pass; a few steps of SGD bring the balance loss down.
+Serving: the same layer with its experts in 8-bit integers and in 8-bit floating
+point.
 
 The other ranks' tokens are random, and all experts' weights are in this process:
 the blocks that a real program would send to other ranks are multiplied here.
@@ -135,17 +136,41 @@ class Combine(torch.autograd.Function):
         return dy, dgate, None
 
 
+class Experts(torch.autograd.Function):
+    """Each block of rows through its expert: silu(x G) * (x U), then the down product; rows
+    behind the last block (masked slots) are neither read nor written, here or by the combine."""
+
+    @staticmethod
+    def forward(ctx, x, w1, w2, layer):
+        m, M, (E, H, F) = layer, x.shape[0], w2.shape
+        of = m.block_experts()
+        pre, h, y = (torch.empty(M, n, dtype=BF16, device=DEV) for n in (2 * F, F, H))
+        blocks = m.off, of, of.numel()
+        uep.ultraep_expert_matmul_bf16(x, M, w1, E, 2 * F * H, 2 * F, H, False, *blocks, uep.ULTRAEP_SWIGLU, pre, h,
+                                       m.status)
+        uep.ultraep_expert_matmul_bf16(h, M, w2, E, F * H, H, F, False, *blocks, uep.ULTRAEP_NO_ACT, None, y, m.status)
+        ctx.save_for_backward(x, w1, w2, pre, h, m.off, of)
+        ctx.layer = m
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        (x, w1, w2, pre, h, off, of), m = ctx.saved_tensors, ctx.layer
+        M, (E, H, F), dy = x.shape[0], w2.shape, dy.contiguous()
+        dpre, dx, dw1, dw2 = torch.empty_like(pre), torch.empty_like(x), torch.empty_like(w1), torch.empty_like(w2)
+        ws = m.empty(torch.uint8, max(uep.ultraep_expert_weight_grad_ws_bytes(M, *s, E) for s in ((H, F), (2 * F, H))))
+        blocks = off, of, of.numel()
+        uep.ultraep_expert_weight_grad(dy, h, M, H, F, *blocks, E, H * F, False, dw2, ws, m.status)
+        uep.ultraep_expert_matmul_bf16(dy, M, w2, E, F * H, F, H, True, *blocks, uep.ULTRAEP_SWIGLU_GRAD, pre, dpre,
+                                       m.status)
+        uep.ultraep_expert_weight_grad(dpre, x, M, 2 * F, H, *blocks, E, 2 * F * H, False, dw1, ws, m.status)
+        uep.ultraep_expert_matmul_bf16(dpre, M, w1, E, 2 * F * H, H, 2 * F, True, *blocks, uep.ULTRAEP_NO_ACT, None, dx,
+                                       m.status)
+        return dx, dw1, dw2, None
+
+
 def experts_bf16(send, layer, w1, w2):
-    """Each block of rows through its expert: silu(x G) * (x U), then the down product."""
-    off, of = layer.off.tolist(), layer.block_experts().tolist()
-    parts = []
-    for b, e in enumerate(of):
-        x = send[off[b]:off[b + 1]]
-        if x.shape[0]:
-            a, u = (x @ w1[e].t()).float().chunk(2, 1)
-            parts.append((torch.nn.functional.silu(a) * u).to(BF16) @ w2[e].t())
-    parts.append(send[off[-1]:] * 0)  # the rows of masked slots
-    return torch.cat(parts)
+    return Experts.apply(send, w1, w2, layer)
 
 
 def train_step(layer, x, wg, w1, w2, target, alpha):
@@ -181,6 +206,31 @@ class Int8Experts:
         return y
 
 
+class Fp8Experts:
+    """The experts' weights in 8-bit floating point with a scale for each 128 elements."""
+
+    def __init__(self, w1, w2):
+        self.w = []
+        for w in (w1, w2):
+            n, N, K = w.shape
+            self.w.append((*self.quantised(w.detach().contiguous(), n * N, K), n, N, K))
+
+    def quantised(self, x, rows, K):
+        q = torch.empty(rows, K, dtype=torch.float8_e4m3fn, device=DEV)
+        s = torch.empty(rows, uep.scale_pitch(K), dtype=torch.uint8, device=DEV)
+        uep.ultraep_quant_blocks(x, rows, K, K, q, K, s)
+        return q, s
+
+    def product(self, i, x, layer, of, act):
+        q, s, n, N, K = self.w[i]
+        M = x.shape[0]
+        xq, xs = self.quantised(x, M, K)
+        y = torch.zeros(M, N // 2 if act else N, dtype=BF16, device=DEV)
+        uep.ultraep_expert_matmul_fp8(xq, xs, M, q, s, n, N, K, layer.off, of, of.numel(),
+                                      uep.ULTRAEP_SWIGLU if act else uep.ULTRAEP_NO_ACT, y, layer.status)
+        return y
+
+
 def serve(layer, x, wg, experts):
     m = layer
     m.route((x.float() @ wg.t()).contiguous())
@@ -209,8 +259,8 @@ def plain_layer(x, wg, w1, w2, k, ids):
 
 
 def main(T=512, H=256, F=512, steps=30, verbose=True):
-    """Returns (relative error of the training output, of the 8-bit output, balance
-    losses, relative errors of the gradients by name)."""
+    """Returns (relative error of the training output, of the output with 8-bit integers,
+    balance losses, relative errors of the gradients by name)."""
     R, E, n_slot, k = 4, 16, 2, 2
     layer = Layer(R, E, n_slot, k, T, H, F)
     gen = layer.gen
@@ -245,7 +295,7 @@ def main(T=512, H=256, F=512, steps=30, verbose=True):
         send = Dispatch.apply(x.detach(), layer)
         bf16 = torch.empty(T, H, dtype=BF16, device=DEV)
         uep.ultraep_combine(experts_bf16(send, layer, w1, w2), T * k, layer.gate, layer.rows, T, k, H, bf16, layer.status)
-        int8 = serve(layer, x.detach(), wg.detach(), Int8Experts(w1, w2))
+        int8, fp8 = (serve(layer, x.detach(), wg.detach(), kind(w1, w2)) for kind in (Int8Experts, Fp8Experts))
     layer.check()
     x.requires_grad_(False)
 
@@ -258,7 +308,8 @@ def main(T=512, H=256, F=512, steps=30, verbose=True):
     layer.check()
     errors = rel(bf16, out), rel(int8, out)
     if verbose:
-        print(f"output against torch in fp32: bf16 experts {errors[0]:.2e}, 8-bit experts {errors[1]:.2e}")
+        print(f"output against torch in fp32: bf16 experts {errors[0]:.2e}, 8-bit integers {errors[1]:.2e}, "
+              f"8-bit floating point {rel(fp8, out):.2e}")
         print("gradients against torch: " + ", ".join(f"{n} {v:.2e}" for n, v in grads.items()))
         print(f"balance loss over {steps} steps: {losses[0]:.3f} -> {losses[-1]:.3f} (1 is even)")
     return errors[0], errors[1], losses, grads
