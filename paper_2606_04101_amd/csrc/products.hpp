@@ -461,7 +461,10 @@ struct ProductWork {
   // false for a quarter that has no rows or no channels
   __device__ bool aim(int id) {
     const int it = first + id / (kPart * kPart), part = id % (kPart * kPart);
-    constexpr int kGroup = 8;  // 8 row tiles by all columns at a time
+    // 4 row tiles by all columns at a time: 32 neighbouring items, an XCD's, share 4 of one side
+    // and 8 of the other (8 row tiles: 32768 rows of 5 experts, N = 2048, K = 7168, SwiGLU's
+    // gradient 860 us, 4: 838; 16381 rows of 6, N = 4096, K = 2816: 337, 327)
+    constexpr int kGroup = 4;
     const int group = it / (kGroup * n_col), rest = it - group * kGroup * n_col;
     const int high = min(kGroup, __builtin_amdgcn_readfirstlane(tiles.total) - group * kGroup);
     tile = tiles.find(a, group * kGroup + rest % high);

@@ -90,7 +90,9 @@ struct GradWork {
     it -= weight * all;
     part = it / of_weight;
     it -= part * of_weight;
-    constexpr int kGroup = 8;  // 8 row tiles by all columns at a time
+    // 4 row tiles by all columns at a time (32768 rows of 5, 4096 x 7168: 2 1675 us, 4 1682, 6
+    // 1683, 8 1730, 16 1785; 4096 x 8192: 1775, 1740, 1780, 1890, 1925)
+    constexpr int kGroup = 4;
     const int group = it / (kGroup * tk), rest = it - group * kGroup * tk;
     const int high = min(kGroup, tn - group * kGroup);
     n0 = (group * kGroup + rest % high) * S::kM;
