@@ -658,8 +658,8 @@ struct ProductWork {
 
 // y = act(x w^T) by tiles of kN channels x kM rows.  Of 256 x 256 (4 waves of 128 x 128, 64
 // parts of 16 x 16 each) a step of 64 KiB feeds 16.8 MFLOP, so the matrix units bound it, and
-// before their issue rate their power: 8192^3 takes 830 us (1.32 PFLOP/s) where registers
-// alone, fed with the same random data, reach 1.95, and fewer stalls no longer shorten it;
+// before their issue rate their power: 8192^3 takes 785 us (1.40 PFLOP/s) where registers
+// alone, fed with random data, reach 1.95, and fewer stalls no longer shorten it;
 // products of 32 x 32 reach 1.57 in registers and were slower here by a tenth.  Results leave
 // in a burst, all compute units in step, of 9 to 13 us a round of tiles; the next tile's loads
 // are under way meanwhile.  Where K is long that is little (32768 rows of 5 experts, N = 4096,
@@ -667,8 +667,8 @@ struct ProductWork {
 // at K = 1408 it is a fourth (8 bits, 32761 rows of 6, N = 4096: 175 us).
 //   A last round that would occupy at most a quarter of the workgroups goes by quarters of its
 // tiles, through four buffers: 8704 x 2048 x 7168 in 223 us (two buffers 250, whole 290);
-// and first, so that the compute units are out of step from then on: 847 us with SwiGLU's
-// gradient for 32768 rows of 5 (last 870).
+// and first, so that the compute units are out of step from then on: 847 us (last 870) with
+// SwiGLU's gradient for 32768 rows of 5 of 2048 x 7168, 836 by the order of items above.
 template <int kN, int kM, int kWn, int kWm, bool kAhead, int kRing, Math kKind, bool kTrans, int kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_product(ProductArgs a, int32_t n_col) {
   using S = Tile<kN, kM, kWn, kWm, kAhead, kRing, kKind, kTrans, false>;

@@ -241,7 +241,7 @@ __device__ __forceinline__ bool sound_blocks(const GradArgs &a, int *s_sound) {
 
 // dw = dy^T x, a weight's tiles of kM rows x kN columns.  As the products bound by the matrix
 // units' power, with two transposing reads more a part: 780 us at 8192^3 (1.41 PFLOP/s), 32768
-// rows of 5 weights of 4096 x 7168 to fp32 in 1583 to 1644 us (1.17 to 1.21): 2240 tiles are 8.75
+// rows of 5 weights of 4096 x 7168 to fp32 in 1622 to 1722 us by the card (1.12 to 1.19): 2240 tiles are 8.75
 // rounds of 256 and the fp32 results 587 MB.  Few rows a weight are bound by the results' bytes
 // (2991 rows over 16 weights of 2880 x 1440, bf16: 53 us, of which the bytes take 30).
 template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>

@@ -615,6 +615,30 @@ def test_fp8_products_of_other_numbers(K):
     same_where_defined(got, want, err)
 
 
+@pytest.mark.parametrize("M", [5, 300])
+@pytest.mark.parametrize("bytes_", [(0, 254), (254, 0), (1, 253), (254, 127), (127, 0)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_fp8_products_of_the_least_and_largest_scales(M, bytes_, f32):
+    """0, 1 and -1 (2 and -2 under scale 2^-127, so that bf16 holds them too): sums of 144 are exact."""
+    rng = np.random.default_rng(6)
+    N, K = 80, 144
+    def side(rows, byte):
+        digits = pe.e4m3_bits(np.array([-1.0, 0.0, 1.0]) * (2 if byte == 0 else 1))
+        s = np.zeros((rows, uep.scale_pitch(K)), np.uint8)
+        s[:, :2] = byte
+        return rng.choice(digits, (rows, K)), s
+    (xq, xs), (wq, ws) = side(M, bytes_[0]), side(N, bytes_[1])
+    if bytes_ == (254, 127):  # sums of several would be infinite
+        xq[:, 1:] = 0
+    y, st = torch.empty(M, N, dtype=F32 if f32 else BF16, device="cuda"), status()
+    uep.ultraep_expert_matmul_fp8(dev(xq), dev(xs), M, dev(wq), dev(ws), 1, N, K, dev(np.array([0, M])), None, 1,
+                                  uep.ULTRAEP_NO_ACT, y, st)
+    want = pe.dequantised(xq, xs) @ pe.dequantised(wq, ws).T
+    if not f32:
+        want = p64.bf16(want.astype(np.float32)).astype(np.float64)
+    assert want.any() and np.array_equal(y.double().cpu().numpy(), want)
+
+
 def test_fp8_products_offsets_past_32_bits():
     n_w, N, K = 5, 32768, 32768
     g = torch.Generator(device="cuda").manual_seed(2)
