@@ -536,7 +536,8 @@ enum {
  *   pre        SWIGLU: [M][N] bf16, written, or null; SWIGLU_GRAD: [M][2 N]
  *              bf16, read; NO_ACT: null
  *   y          rows of N, N / 2 (SWIGLU) or 2 N (SWIGLU_GRAD) elements; with
- *              SWIGLU_GRAD and bf16 it may be pre itself, else it aliases nothing
+ *              SWIGLU_GRAD and bf16 it may be pre itself; otherwise neither y nor a
+ *              written pre overlaps another buffer
  * Blocks that are not in rising order within [0, M], and a nonempty block
  * whose weight is outside [0, n_w), raise ULTRAEP_EDATA; then no row is written.
  * 1 <= n_block <= 2048, n_w >= 1, M < 2^31; K, N % 8 == 0 (N % 16 == 0 with
@@ -559,7 +560,8 @@ int ultraep_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_t *w, 
  *   dy         [M][N] bf16, x [M][K] bf16 (they may be the same)
  *   block_off, block_w, n_block  as for ultraep_expert_matmul_bf16
  *   dw         n_w gradients of N * K elements of `type`, dw_stride elements
- *              apart; what lies between them is not written
+ *              apart; what lies between them is not written; dw overlaps neither
+ *              dy nor x
  *   ws         workspace of ws_bytes >= ultraep_expert_weight_grad_ws_bytes,
  *              16-byte aligned, or null: where the weights are few and small,
  *              their rows are summed in parts, side by side, with it (the
@@ -590,7 +592,7 @@ size_t ultraep_expert_weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int3
  *   x      rows of K elements of `type`, ld elements apart
  *   q      rows of ldq bytes, ldq >= K: K values, then zeros
  *   scale  rows of 4 * ceil(K / 512) bytes: ceil(K / 128) scales, then zeros;
- *          4-byte aligned
+ *          4-byte aligned; q and scale do not overlap x
  * K, ld % 8 == 0, ldq % 16 == 0, ld, ldq <= 2^20, rows < 2^31, 16-byte aligned x
  * and q. */
 int ultraep_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, int64_t ld,

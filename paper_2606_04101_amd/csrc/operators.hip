@@ -162,6 +162,9 @@ int ultraep_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_t *w, 
   if (M == 0) return ULTRAEP_OK;
   if (act == ULTRAEP_SWIGLU_GRAD && !pre) return ULTRAEP_EINVAL;
   if (!x || !aligned16(x) || !y || !aligned16(y)) return ULTRAEP_EINVAL;
+  // only a bf16 gradient may take its pre's place
+  if (y == pre && !(act == ULTRAEP_SWIGLU_GRAD && type == ULTRAEP_BF16)) return ULTRAEP_EINVAL;
+  if (y == x || y == w || (pre && (pre == x || pre == w))) return ULTRAEP_EINVAL;
   return rc(uep::launch_expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans, block_off, block_w,
                                            n_block, act, pre, y, type, status, stream));
 }
@@ -182,6 +185,7 @@ int ultraep_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M,
   if (ws && (!aligned16(ws) || ws_bytes < uep::weight_grad_ws_bytes(M, N, K, n_w)))
     return ULTRAEP_EINVAL;
   if (M > 0 && (!dy || !aligned16(dy) || !x || !aligned16(x))) return ULTRAEP_EINVAL;
+  if (dw == dy || dw == x || (ws && (ws == dw || ws == dy || ws == x))) return ULTRAEP_EINVAL;
   return rc(uep::launch_expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block, n_w,
                                            dw_stride, accumulate, dw, type, ws, status, stream));
 }
@@ -192,7 +196,7 @@ int ultraep_quant_blocks(const void *x, int32_t type, int64_t rows, int64_t K, i
   if (K < 8 || K % 8 != 0 || ld < K || ld % 8 != 0 || ld > 1 << 20) return ULTRAEP_EINVAL;
   if (ldq < K || ldq % 16 != 0 || ldq > 1 << 20) return ULTRAEP_EINVAL;
   if (rows == 0) return ULTRAEP_OK;
-  if (!x || !q || !scale || !aligned16(x) || !aligned16(q) || !aligned4(scale))
+  if (!x || !q || !scale || !aligned16(x) || !aligned16(q) || !aligned4(scale) || q == x || scale == x || scale == q)
     return ULTRAEP_EINVAL;
   return rc(uep::launch_quant_blocks(x, type, rows, K, ld, q, ldq, scale, stream));
 }
@@ -210,6 +214,7 @@ int ultraep_expert_matmul_fp8(const uint8_t *xq, const uint8_t *x_scale, int64_t
   if (M == 0) return ULTRAEP_OK;
   if (!xq || !aligned16(xq) || !x_scale || !aligned4(x_scale) || !y || !aligned16(y))
     return ULTRAEP_EINVAL;
+  if (y == xq || y == wq || y == x_scale || y == w_scale) return ULTRAEP_EINVAL;
   return rc(uep::launch_expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off,
                                           block_w, n_block, act, y, type, status, stream));
 }

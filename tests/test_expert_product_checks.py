@@ -143,6 +143,27 @@ def test_bad_arguments_are_refused():
     assert m8(M=0) == uep.ULTRAEP_OK
 
 
+def test_outputs_in_the_place_of_inputs_are_refused():
+    L = uep.lib()
+    a, b, c, d, off, st = (ctypes.c_void_p(4096 * i) for i in range(1, 7))  # never dereferenced
+
+    def mm(x, w, pre, y, act, type_):
+        return L.ultraep_expert_matmul_bf16(x, 4, w, 1, 512, 16, 32, 0, off, None, 1, act, pre, y, type_, st, None)
+    none, glu, grad = uep.ULTRAEP_NO_ACT, uep.ULTRAEP_SWIGLU, uep.ULTRAEP_SWIGLU_GRAD
+    for args in [(a, b, None, a, none, 1), (a, b, None, b, none, 1), (a, b, c, c, glu, 1), (a, b, a, c, glu, 1),
+                 (a, b, b, c, glu, 1), (a, b, c, c, grad, 0), (a, b, c, a, grad, 1)]:
+        assert mm(*args) == E_, args
+
+    def wg(dy, x, dw, ws):
+        return L.ultraep_expert_weight_grad(dy, x, 4, 16, 32, off, None, 1, 1, 512, 0, dw, 0, ws, 1 << 20, st, None)
+    for args in [(a, b, a, None), (a, b, b, None), (a, b, c, a), (a, b, c, b), (a, b, c, c)]:
+        assert wg(*args) == E_, args
+    for x, q, s in [(a, a, b), (a, b, a), (a, b, b)]:
+        assert L.ultraep_quant_blocks(x, 1, 4, 16, 16, q, 16, s, None) == E_
+    for y in (a, b, c, d):
+        assert L.ultraep_expert_matmul_fp8(a, b, 4, c, d, 1, 16, 32, off, None, 1, 0, y, 1, st, None) == E_
+
+
 def t(n, dtype=torch.int32):
     return torch.zeros(n, dtype=dtype)
 
