@@ -55,15 +55,13 @@ struct Tile {
   // from one of a wave's loads of a transposed side to the next are whole groups of 8 of
   // the common index
   static_assert(!(TransA || TransB) || kWaves * 512 / (N > M ? N : M) % 8 == 0, "");
+  static_assert((!TransA || N >= 128) && (!TransB || M >= 128), "the exchange of chunks takes 8 of them and more");
 };
 
-// A transposed side of kW channels lies in LDS as the rows of its memory, kW * 2 bytes
+// A transposed side of kW >= 128 channels lies in LDS as the rows of its memory, kW * 2 bytes
 // each, chunk c (of 16 bytes) of row r at c ^ flip(r): the reads that half a wave makes, of
 // 32 bytes of the 8 rows r, r + 1, r + 2, r + 3, r + 8 .. r + 11, meet all banks.
-template <int kW>
-__device__ __forceinline__ int flip(int r) {
-  return kW >= 128 ? ((r & 3) | (r >> 3 & 1) << 2) << 1 : ((r >> 1 & 1) | (r >> 3 & 1) << 1) << 1;
-}
+__device__ __forceinline__ int flip(int r) { return ((r & 3) | (r >> 3 & 1) << 2) << 1; }
 
 // (kMathWide) 8 elements of 8 bits with their scale as bf16.  An e4m3 times a power of two
 // is one exactly, from 2^-126 on.
@@ -142,7 +140,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       const int r = wave * kRowsA + l / (S::kN / 8);
       uint32_t at_a[2];  // of the lane's chunk in row 0, by load % 2
 #pragma unroll
-      for (int i = 0; i < 2; ++i) at_a[i] = work.chunk_a((l % (S::kN / 8)) ^ flip<S::kN>(r + i * kWaves * kRowsA));
+      for (int i = 0; i < 2; ++i) at_a[i] = work.chunk_a((l % (S::kN / 8)) ^ flip(r + i * kWaves * kRowsA));
 #pragma unroll
       for (int i = 0; i < kLoadsA; ++i) off[i] = at_a[i & 1] + (i * kWaves * kRowsA + r) * work.pitch_a;
     } else {
@@ -154,7 +152,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
       const int r = wave * kRowsB + l / (S::kM / 8);
       uint32_t at_b[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) at_b[i] = work.chunk_b((l % (S::kM / 8)) ^ flip<S::kM>(r + i * kWaves * kRowsB));
+      for (int i = 0; i < 2; ++i) at_b[i] = work.chunk_b((l % (S::kM / 8)) ^ flip(r + i * kWaves * kRowsB));
 #pragma unroll
       for (int i = kLoadsA; i < kLoads; ++i)
         off[i] = at_b[(i - kLoadsA) & 1] + ((i - kLoadsA) * kWaves * kRowsB + r) * work.pitch_b;
@@ -227,7 +225,7 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
   auto lane_at = [&](auto width, bool trans, int part) {
     constexpr int kW = decltype(width)::value;
     if (trans)
-      return tr_row * kW * 2 + (((lane >> 1 & 1) * 16 + (lane & 1) * 8) ^ flip<kW>(tr_row) * 16 ^ part * 32);
+      return tr_row * kW * 2 + (((lane >> 1 & 1) * 16 + (lane & 1) * 8) ^ flip(tr_row) * 16 ^ part * 32);
     return (part * 16 + lr) * kBk + (lc ^ (lr >> 1 & 7)) * 16;
   };
   using WidthA = std::integral_constant<int, S::kN>;
