@@ -1,5 +1,7 @@
 // The gradient of the experts' weights: for each weight the sum, over its blocks' rows, of
 // the outer products of the two sides' rows.
+#include <algorithm>
+
 #include "products.hpp"
 
 namespace uep {
@@ -12,7 +14,7 @@ struct GradArgs {
   int32_t *status;
   int64_t M, dw_stride;  // (dw_stride in elements)
   int32_t n_w, N, K, n_block;
-  int32_t parts;  // a weight's rows in so many parts, dw_stride * n_w elements apart
+  int32_t slots;  // in all so many parts of the weights' rows, dw_stride apart; 0: one a weight
 };
 
 // Items item, item + stride, .. below n_item: tiles of a weight's gradient, kM of its rows
@@ -33,7 +35,8 @@ struct GradWork {
   int64_t lo;
   int rows, w, run;
   uint64_t mask;  // of the run's blocks of the item's weight that are still to come
-  int weight, part, n0, k0;
+  int weight, slot, n0, k0;
+  const int *const first_slot;  // of each weight
   int64_t row;    // of the next step
   int remaining;  // rows of its block from there on
   int budget;     // steps of the item's part that are still to come
@@ -42,11 +45,11 @@ struct GradWork {
   int left;
   uint32_t pitch_a, pitch_b;
 
-  __device__ GradWork(const GradArgs &g, int first, int step, int n_tile_n, int n_tile_k, int n)
+  __device__ GradWork(const GradArgs &g, const int *slots, int first, int step, int n_tile_n, int n_tile_k, int n)
       : a(g), N(__builtin_amdgcn_readfirstlane(g.N)), K(__builtin_amdgcn_readfirstlane(g.K)),
         n_block(__builtin_amdgcn_readfirstlane(g.n_block)), n_run((n_block + kWave - 1) / kWave),
         tn(n_tile_n), tk(n_tile_k), stride(step), n_item(n), block_off(uniform(g.block_off)),
-        block_w(uniform(g.block_w)), dy(uniform(g.dy)), x(uniform(g.x)), item(first) {
+        block_w(uniform(g.block_w)), dy(uniform(g.dy)), x(uniform(g.x)), item(first), first_slot(slots) {
     pitch_a = K * 2;
     pitch_b = N * 2;
     if (n_run == 1) load(0);
@@ -82,14 +85,27 @@ struct GradWork {
     next_block();
   }
   __device__ bool next_item() {
-    if (item >= n_item) return false;
-    int it = item;
-    item += stride;
-    const int of_weight = tn * tk, all = of_weight * a.parts;
-    weight = it / all;
-    it -= weight * all;
-    part = it / of_weight;
-    it -= part * of_weight;
+    const int of_weight = tn * tk;
+    auto first_of = [&](int u) { return __builtin_amdgcn_readfirstlane(first_slot[u]); };
+    int it, part = 0, parts = 1;
+    while (true) {
+      if (item >= n_item) return false;
+      slot = item / of_weight;
+      it = item - slot * of_weight;
+      item += stride;
+      weight = slot;
+      if (a.slots == 0) break;
+      if (slot >= first_of(a.n_w)) continue;
+      weight = 0;
+      for (int end = a.n_w; end - weight > 1;) {
+        const int mid = (weight + end) / 2;
+        if (first_of(mid) <= slot) weight = mid;
+        else end = mid;
+      }
+      part = slot - first_of(weight);
+      parts = first_of(weight + 1) - first_of(weight);
+      break;
+    }
     // 4 row tiles by all columns at a time (32768 rows of 5, 4096 x 7168: 2 1675 us, 4 1682, 6
     // 1683, 8 1730, 16 1785; 4096 x 8192: 1775, 1740, 1780, 1890, 1925)
     constexpr int kGroup = 4;
@@ -99,11 +115,11 @@ struct GradWork {
     k0 = rest / high * S::kN;
     first_block();
     budget = 1 << 30;
-    if (a.parts > 1) {
+    if (parts > 1) {
       int steps = 0;
       for (; remaining > 0; next_block()) steps += (remaining + S::kStep - 1) / S::kStep;
-      int skip = static_cast<int>(static_cast<int64_t>(steps) * part / a.parts);
-      budget = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / a.parts) - skip;
+      int skip = static_cast<int>(static_cast<int64_t>(steps) * part / parts);
+      budget = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / parts) - skip;
       first_block();
       while (budget > 0 && skip >= (remaining + S::kStep - 1) / S::kStep) {
         skip -= (remaining + S::kStep - 1) / S::kStep;
@@ -135,10 +151,10 @@ struct GradWork {
   __device__ uint32_t chunk_b(int c) const { return 2 * min(c * 8, N - 8 - n0); }
 
   struct Out {
-    int weight, part, n0, k0;
+    int slot, n0, k0;
     bool skip;
   };
-  __device__ Out out() const { return {weight, part, n0, k0, kAdd && empty}; }
+  __device__ Out out() const { return {slot, n0, k0, kAdd && empty}; }
   // Added to what is there the sums leave LDS in fp32, 4 channels a lane; a bf16 gradient
   // that is not added to leaves as such, 8.
   static constexpr bool kPacked = kBf16 && !kAdd;
@@ -156,7 +172,7 @@ struct GradWork {
     const int r = o.n0 + (wm * kBands + n / kParts) * 32 + p * 8 + el / 8;
     const int c = o.k0 + wn * S::kFn * 16 + (n % kParts * 8 + (el & 7)) * kLane;
     if (r >= N || c >= K || o.skip) return nullptr;
-    const int64_t at = (static_cast<int64_t>(o.part) * a.n_w + o.weight) * a.dw_stride + static_cast<int64_t>(r) * K + c;
+    const int64_t at = o.slot * a.dw_stride + static_cast<int64_t>(r) * K + c;
     return static_cast<char *>(a.dw) + at * kSize;
   }
   __device__ void keep(const Out &o, Early &k, int n, int wn, int wm) const {
@@ -239,6 +255,33 @@ __device__ __forceinline__ bool sound_blocks(const GradArgs &a, int *s_sound) {
   return __builtin_amdgcn_readfirstlane(every);
 }
 
+constexpr int kMostParted = 256;  // weights whose rows are in parts
+
+// The first of each weight's slots (parts of its rows), and the first that nobody has: one a
+// weight and the rest by their rows, in steps of 64, so that a part's steps differ little however
+// the rows are spread.  256 threads, with the same result in every workgroup.
+__device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int *s_of) {
+  const int tid = threadIdx.x;
+  s_of[tid] = 0;
+  __syncthreads();
+  for (int g = tid; g < a.n_block; g += 256) {
+    const int rows = static_cast<int>(a.block_off[g + 1] - a.block_off[g]);
+    if (rows > 0) atomicAdd(&s_of[a.block_w ? a.block_w[g] : g], (rows + 63) / 64);
+  }
+  __syncthreads();
+  int total = 0, before = 0;
+  for (int u = 0; u < a.n_w; ++u) total += s_of[u];
+  // (the shares' roundings, 2^-22 of 2^14 in all, cannot make one more than there are)
+  const int mine = 1 + (total ? static_cast<int>(static_cast<float>(a.slots - a.n_w) * s_of[tid] / total) : 0);
+  __syncthreads();
+  s_of[tid] = mine;
+  __syncthreads();
+  for (int u = 0; u < tid && u < a.n_w; ++u) before += s_of[u];
+  if (tid < a.n_w) s_first[tid] = before;
+  if (tid == a.n_w - 1) s_first[a.n_w] = before + mine;
+  __syncthreads();
+}
+
 // dw = dy^T x, a weight's tiles of kM rows x kN columns.  As the products bound by the matrix
 // units' power, with two transposing reads more a part: 780 us at 8192^3 (1.41 PFLOP/s), 32768
 // rows of 5 weights of 4096 x 7168 to fp32 in 1622 to 1722 us by the card (1.12 to 1.19): 2240 tiles are 8.75
@@ -248,12 +291,14 @@ template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
   using S = Tile<kN, kM, kWn, kWm, kAhead, 2, kMath16, true, true>;
   __shared__ __align__(1024) int8_t s_lds[S::kLds];
-  __shared__ int s_sound[S::kWaves];
+  static_assert(S::kThreads == 256, "slots are counted by 256 threads");
+  __shared__ int s_sound[S::kWaves], s_first[kMostParted + 1];
   if (!sound_blocks<S::kWaves>(a, s_sound)) return;
+  if (a.slots) count_slots(a, s_first, reinterpret_cast<int *>(s_lds));
   constexpr int kXcd = 8;  // the workgroups of one XCD take neighbouring items
   const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
   const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
-  GradWork<S, kBf16, kAdd> work(a, slot, grid, tn, tk, a.n_w * a.parts * tn * tk);
+  GradWork<S, kBf16, kAdd> work(a, s_first, slot, grid, tn, tk, (a.slots ? a.slots : a.n_w) * tn * tk);
   tile_items<S>(work, s_lds);
 }
 
@@ -261,13 +306,16 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int3
 template <bool kBf16>
 __global__ void __launch_bounds__(256)
 k_weight_grad_sum(GradArgs a, const v4f *from, int64_t of_weight, int32_t accumulate) {
-  __shared__ int s_sound[4];
+  __shared__ int s_sound[4], s_first[kMostParted + 1], s_of[256];
   if (!sound_blocks<4>(a, s_sound)) return;
+  count_slots(a, s_first, s_of);
   const int64_t all = of_weight * a.n_w, step = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
-    v4f v = from[i];
-    for (int p = 1; p < a.parts; ++p) v += from[p * all + i];
-    const int64_t at = i / of_weight * a.dw_stride + i % of_weight * 4;
+    const int weight = static_cast<int>(i / of_weight), last = s_first[weight + 1];
+    const int64_t e = i % of_weight;
+    v4f v = from[s_first[weight] * of_weight + e];
+    for (int p = s_first[weight] + 1; p < last; ++p) v += from[p * of_weight + e];
+    const int64_t at = weight * a.dw_stride + e * 4;
     if (kBf16) {
       v2u *to = reinterpret_cast<v2u *>(static_cast<uint16_t *>(a.dw) + at);
       if (accumulate) {
@@ -282,24 +330,27 @@ k_weight_grad_sum(GradArgs a, const v4f *from, int64_t of_weight, int32_t accumu
   }
 }
 
-// Parts of the rows: where the weights' tiles would not fill the card, so many that they
-// do, of 512 rows of a weight at least.  It does not fall with M.
-static int32_t row_parts(int64_t M, int32_t N, int32_t K, int32_t n_w) {
-  const int64_t tiles = int64_t(n_w) * ((N + 127) / 128) * ((K + 127) / 128);
-  const int64_t fill = 512 / tiles, rows = M / (int64_t(n_w) * 512);
-  const int64_t parts = fill < rows ? fill : rows;
-  return static_cast<int32_t>(parts < 2 ? 1 : parts > 64 ? 64 : parts);
+// Slots, over all weights: where the weights' tiles would not fill the card, so many that they
+// do, of 512 rows at least; and, where they would fill little more than that, of 2048 rows, so that
+// one weight with most of the rows does not hold up the call.  No more with fewer rows.
+static int32_t row_slots(int64_t M, int32_t N, int32_t K, int32_t n_w) {
+  const int64_t of_weight = int64_t((N + 127) / 128) * ((K + 127) / 128), tiles = n_w * of_weight;
+  if (n_w > kMostParted || tiles > 384) return 0;
+  const int64_t fill = std::min({512 / tiles, M / (int64_t(n_w) * 512), int64_t(64)}) * n_w;
+  const int64_t spread = std::min({1024 / of_weight, M / 2048, int64_t(64) * n_w});
+  const int64_t slots = std::max(fill, spread);
+  return static_cast<int32_t>(slots > n_w ? slots : 0);
 }
 
 size_t weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w) {
-  const int64_t parts = row_parts(M, N, K, n_w);
-  return parts > 1 ? static_cast<size_t>(parts) * n_w * N * K * 4 : 16;
+  const int64_t slots = row_slots(M, N, K, n_w);
+  return slots ? static_cast<size_t>(slots) * N * K * 4 : 16;
 }
 
 template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
 static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
   const int32_t tn = (a.N + kM - 1) / kM, tk = (a.K + kN - 1) / kN;
-  const int64_t items = int64_t(a.n_w) * a.parts * tn * tk;
+  const int64_t items = int64_t(a.slots ? a.slots : a.n_w) * tn * tk;
   const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
   hipLaunchKernelGGL((k_weight_grad<kN, kM, kWn, kWm, kAhead, kBf16, kAdd>), grid, block, 0, stream, a, tn, tk);
 }
@@ -317,7 +368,7 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 template <bool kBf16, bool kAdd>
 static void choose_grad(const GradArgs &a, hipStream_t stream) {
   auto tiles = [&](int64_t n, int64_t k) {
-    return int64_t(a.n_w) * a.parts * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
+    return int64_t(a.slots ? a.slots : a.n_w) * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
   };
   const int64_t big = (tiles(256, 256) + 255) / 256 * 20, mid = (tiles(128, 128) + 511) / 512 * 13;
   const bool few = a.M < int64_t(768) * a.n_w && tiles(128, 128) < 4 * tiles(256, 256);
@@ -331,15 +382,15 @@ hipError_t launch_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int6
                                      int32_t accumulate, void *dw, int32_t type, void *ws,
                                      int32_t *status, hipStream_t stream) {
   GradArgs a{reinterpret_cast<const int8_t *>(dy), reinterpret_cast<const int8_t *>(x), block_off, block_w, dw, status,
-             M, dw_stride, n_w, N, K, n_block, 1};
+             M, dw_stride, n_w, N, K, n_block, 0};
   const bool bf16 = type == ULTRAEP_BF16;
-  const int32_t parts = ws ? row_parts(M, N, K, n_w) : 1;
-  if (parts > 1) {
+  const int32_t slots = ws ? row_slots(M, N, K, n_w) : 0;
+  if (slots) {
     GradArgs part = a;
     const int64_t of_weight = int64_t(N) * K;
     part.dw = ws;
     part.dw_stride = of_weight;
-    a.parts = part.parts = parts;
+    a.slots = part.slots = slots;
     choose_grad<false, false>(part, stream);
     const int64_t wg = (of_weight / 4 * n_w + 255) / 256;
     const dim3 grid(static_cast<unsigned>(wg < 2048 ? wg : 2048));

@@ -346,6 +346,24 @@ def test_weight_grad_of_parts_over_many_blocks():
     check_weight_grad(sizes.tolist(), 72, 136, True, of=of.tolist(), n_w=3, ws=False)
 
 
+@pytest.mark.parametrize("accumulate", [True, False])
+@pytest.mark.parametrize("sizes,of,n_w,N,K", [
+    ([3000, 5, 0, 40, 9000], [0, 1, 2, 3, 4], 5, 200, 72), ([3000, 5, 0, 40, 9000, 64], [3, 1, 0, 3, 1, 0], 4, 136, 264),
+    ([12000, 1, 0, 4400, 100], [0, 1, 2, 3, 4], 5, 2568, 264), ([2, 6000, 1], [0, 1, 2], 3, 8, 8)])
+def test_weight_grad_of_parts_by_their_rows(sizes, of, n_w, N, K, accumulate):
+    """Weights with nearly all rows, with a few and with none, in parts by their rows."""
+    check_weight_grad(sizes, N, K, accumulate, of=of, n_w=n_w, gap=8, start=3, tail=70, spoil=True, accumulate=accumulate)
+
+
+def test_weight_grad_of_parts_of_many_weights():
+    rng = np.random.default_rng(9)
+    sizes = rng.integers(0, 900, 600)
+    sizes[7] = 20000
+    of = rng.integers(0, 256, 600)
+    of[sizes == 0] = -1
+    check_weight_grad(sizes.tolist(), 64, 64, True, of=of.tolist(), n_w=256)
+
+
 @pytest.mark.parametrize("f32", [True, False])
 @pytest.mark.parametrize("ws", [True, False])
 def test_weight_grad_accumulates(f32, ws):
