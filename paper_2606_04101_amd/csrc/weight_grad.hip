@@ -225,7 +225,7 @@ struct GradWork {
           } else {
             word = st.get<v4u>(p);
           }
-          if (at) __builtin_nontemporal_store(word, reinterpret_cast<Word *>(at));
+          if (at) store_result<S>(word, reinterpret_cast<Word *>(at));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -357,7 +357,7 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 
 // Tiles of 256 x 256 or, two a compute unit, of 128 x 128, by the rounds that either takes, in
 // twentieths of a round of the first; the second where a weight has few rows, so that the
-// results' bytes bound the call, and it pads less.  Measured, us (256 / 128; fp32 results):
+// results' bytes bound the call, and it pads less or its stores fill lines together.  Measured, us (256 / 128; fp32 results):
 //   5 weights, N = 4096, K = 7168: M = 16384 855 / 1004; N = 7168, K = 2048: M = 16384 441 / 504,
 //   1024 79 / 74; 4 weights, N = K = 2048: M = 32768 197 / 247, 8192 60 / 67, 1024 20.5 / 20.6; 2
 //   weights, K = 2048, M = 8192: N = 2048 94 / 64, 1024 67 / 49, 512 43 / 32; 8 weights, K = 1024,
@@ -365,13 +365,15 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 //   weights, N = 2880, K = 1440: M = 2000 69 / 56 (bf16 results 48 / 40)
 //   Out of a cache that holds no results yet: 16 weights, N = 2880, K = 1440: M = 8192 113 / 104, 2991
 //   to bf16 76 / 57; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
+//   Rows of no whole lines: 6 weights, N = 5584, K = 3048, M = 277 to bf16 130 / 63
 template <bool kBf16, bool kAdd>
 static void choose_grad(const GradArgs &a, hipStream_t stream) {
   auto tiles = [&](int64_t n, int64_t k) {
     return int64_t(a.slots ? a.slots : a.n_w) * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
   };
   const int64_t big = (tiles(256, 256) + 255) / 256 * 20, mid = (tiles(128, 128) + 511) / 512 * 13;
-  const bool few = a.M < int64_t(768) * a.n_w && tiles(128, 128) < 4 * tiles(256, 256);
+  const bool lines = a.K * (kBf16 ? 2 : 4) % 128 == 0;  // the smaller tiles' stores may fill them together
+  const bool few = a.M < int64_t(768) * a.n_w && (!lines || tiles(128, 128) < 4 * tiles(256, 256));
   if (big < mid && !few) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
   else start_grad<128, 128, 2, 2, false, kBf16, kAdd>(a, 512, stream);
 }
