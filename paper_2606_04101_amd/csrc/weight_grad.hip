@@ -259,8 +259,9 @@ constexpr int kMostParted = 256;  // weights whose rows are in parts
 
 // The first of each weight's slots (parts of its rows), and the first that nobody has: one a
 // weight and the rest by their rows, in steps of 64, so that a part's steps differ little however
-// the rows are spread.  256 threads, with the same result in every workgroup.
-__device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int *s_of) {
+// the rows are spread.  256 threads, with the same result in every workgroup.  s_steps: left with
+// each weight's rows in steps of 64.
+__device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int *s_of, int *s_steps = nullptr) {
   const int tid = threadIdx.x;
   s_of[tid] = 0;
   __syncthreads();
@@ -272,6 +273,7 @@ __device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int
   int total = 0, before = 0;
   for (int u = 0; u < a.n_w; ++u) total += s_of[u];
   // (the shares' roundings, 2^-22 of 2^14 in all, cannot make one more than there are)
+  if (s_steps) s_steps[tid] = s_of[tid];
   const int mine = 1 + (total ? static_cast<int>(static_cast<float>(a.slots - a.n_w) * s_of[tid] / total) : 0);
   __syncthreads();
   s_of[tid] = mine;
@@ -302,16 +304,18 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int3
   tile_items<S>(work, s_lds);
 }
 
-// The parts' sums, in order: 4 elements a thread.
+// The parts' sums, in order: 4 elements a thread.  (Added to what is there: a weight without
+// rows is not touched, -0 + 0 would be 0.)
 template <bool kBf16>
 __global__ void __launch_bounds__(256)
 k_weight_grad_sum(GradArgs a, const v4f *from, int64_t of_weight, int32_t accumulate) {
-  __shared__ int s_sound[4], s_first[kMostParted + 1], s_of[256];
+  __shared__ int s_sound[4], s_first[kMostParted + 1], s_of[256], s_steps[256];
   if (!sound_blocks<4>(a, s_sound)) return;
-  count_slots(a, s_first, s_of);
+  count_slots(a, s_first, s_of, s_steps);
   const int64_t all = of_weight * a.n_w, step = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
     const int weight = static_cast<int>(i / of_weight), last = s_first[weight + 1];
+    if (accumulate && s_steps[weight] == 0) continue;
     const int64_t e = i % of_weight;
     v4f v = from[s_first[weight] * of_weight + e];
     for (int p = s_first[weight] + 1; p < last; ++p) v += from[p * of_weight + e];
