@@ -1,10 +1,12 @@
 """The weights' gradient of few small weights, whose rows are summed in parts with a workspace
-and joined by a second kernel: weights without rows.  Needs an MI355X."""
+and joined by a second kernel: its binding, guards around outputs and workspace, captures,
+streams, unsound lists, and weights without rows.  Needs an MI355X."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_expert_products import dev, dev16, normal, status
+from test_gpu_expert_binding import Declines
+from test_gpu_expert_products import BAD_LISTS, dev, dev16, normal, status
 
 pytestmark = pytest.mark.gpu
 
@@ -27,6 +29,100 @@ def arguments(seed=0, type=F32, accumulate=False, sizes=(2500, 0, 2400), ws=None
     dw = torch.full((G, N, K), 0.5, dtype=type, device="cuda")
     return [dev16(normal(rng, M, N)), dev16(normal(rng, M, K)), M, N, K, dev(off), dev(np.array([2, 0, 1], np.int32)), 3, G,
             N * K, accumulate, dw, workspace() if ws is None else ws, status()]
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_native_and_ctypes_halves_agree(accumulate, monkeypatch):
+    a = arguments(accumulate=accumulate)
+    uep.ultraep_expert_weight_grad(*a)
+    torch.cuda.synchronize()
+    first = a[11].clone()
+    assert first.any()
+    a[11].fill_(0.5)
+    a[12].fill_(0xC1)
+    monkeypatch.setattr(uep, "_native", Declines())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    uep.ultraep_expert_weight_grad(*a, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(a[11], first)
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_guards_around_outputs_and_workspace(type, accumulate):
+    a = arguments(type=type, accumulate=accumulate)
+    uep.ultraep_expert_weight_grad(*a)
+    want = a[11].clone()
+    buf = torch.full((G * N * K + 128,), 77.0, dtype=type, device="cuda")
+    a[11] = buf[64:-64].view(G, N, K)
+    a[11].fill_(0.5)
+    ws = workspace(guard=256)
+    a[12] = ws[256:-256]
+    uep.ultraep_expert_weight_grad(*a)
+    torch.cuda.synchronize()
+    assert torch.equal(a[11], want)
+    assert (buf[:64] == 77).all() and (buf[-64:] == 77).all()
+    assert (ws[:256] == 0x3F).all() and (ws[-256:] == 0x3F).all()
+
+
+def test_a_workspace_one_byte_short_is_refused():
+    a = arguments()
+    a[12] = a[12][:-1]
+    with pytest.raises(uep.UltraEPError):
+        uep.ultraep_expert_weight_grad(*a)
+
+
+def test_captured_and_replayed():
+    a = arguments()
+    wants = []
+    for src in (a[0].clone(), a[0].flip(0).contiguous()):
+        a[0].copy_(src)
+        uep.ultraep_expert_weight_grad(*a)
+        wants.append((src, a[11].clone()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        uep.ultraep_expert_weight_grad(*a)
+    for src, want in wants * 3:
+        a[0].copy_(src)
+        a[11].zero_()
+        a[12].fill_(0x7F)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a[11], want)
+        uep.ultraep_expert_weight_grad(*a)
+        assert torch.equal(a[11], want)
+
+
+def test_two_streams_at_once():
+    sets = [arguments(seed=1), arguments(seed=2)]
+    wants = []
+    for a in sets:
+        uep.ultraep_expert_weight_grad(*a)
+        wants.append(a[11].clone())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for a in sets:
+            a[11].zero_()
+        torch.cuda.synchronize()
+        for a, s in zip(sets, streams):
+            for _ in range(3):
+                uep.ultraep_expert_weight_grad(*a, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[11], w) for a, w in zip(sets, wants))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("off,of", BAD_LISTS)
+def test_unsound_blocks_write_nothing(off, of, accumulate):
+    """Neither the sums of the parts nor what the workspace holds reach dw."""
+    a = arguments(accumulate=accumulate)
+    assert max(off) <= M
+    if max(off) == 21:  # (the list that ends behind its rows)
+        off = off[:-1] + [M + 1]
+    a[5], a[6] = dev(np.array(off, np.int64)), None if of is None else dev(np.array(of, np.int32))
+    uep.ultraep_expert_weight_grad(*a)
+    assert int(a[13].item()) == uep.ULTRAEP_EDATA and (a[11] == 0.5).all()
 
 
 @pytest.mark.parametrize("type", [F32, BF16])
