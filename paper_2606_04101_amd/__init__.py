@@ -625,6 +625,20 @@ def ultraep_expert_matmul(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, blo
         "ultraep_expert_matmul")
 
 
+_BF16 = 2, "torch.bfloat16", ("torch.int16", "torch.uint16")
+_E4M3 = 1, "torch.float8_e4m3fn", ("torch.uint8", "torch.int8")
+_E8M0 = 1, "torch.float8_e8m0fnu", ("torch.uint8", "torch.int8")
+
+
+def _need_values(t, n, format_, name):
+    """Raises unless t holds n elements of the format, as its own type or as raw integers:
+    those of another of the same size would be taken for other values."""
+    esize, own, raw = format_
+    if n > 0 and t is not None and t.element_size() == esize and str(t.dtype) not in (own, *raw):
+        raise ValueError(f"{name}: expected {own[6:]} elements (or raw integers), got {t.dtype}")
+    _need(t, n, esize, name)
+
+
 def _need_blocks(block_off, block_w, n_block, status):
     _need(block_off, n_block + 1, 8, "block_off")
     _need(block_w, n_block if block_w is not None else 0, 4, "block_w")
@@ -634,18 +648,19 @@ def _need_blocks(block_off, block_w, n_block, status):
 def ultraep_expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans, block_off, block_w, n_block, act,
                                pre, y, status, stream=None):
     """act: ULTRAEP_NO_ACT, ULTRAEP_SWIGLU or ULTRAEP_SWIGLU_GRAD.  block_w may be None
-    (block g takes weight g), pre where act does not read it; y is float32 or bfloat16."""
+    (block g takes weight g), pre where act does not read it; x, w and pre are bfloat16 (or raw
+    16-bit integers), y is float32 or bfloat16."""
     rc = (_native or _load_native()).expert_matmul_bf16(x, M, w, n_w, w_stride, N, K, trans,
                                                        block_off, block_w, n_block, act, pre, y,
                                                        status, stream)
     if rc is not None:
         return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_matmul_bf16")
     type_ = _row_type(y, "y") if M > 0 else ULTRAEP_BF16
-    _need(x, M * K, 2, "x")
-    _need(w, (n_w - 1) * w_stride + N * K if n_w > 0 else 0, 2, "w")
+    _need_values(x, M * K, _BF16, "x")
+    _need_values(w, (n_w - 1) * w_stride + N * K if n_w > 0 else 0, _BF16, "w")
     _need_blocks(block_off, block_w, n_block, status)
     grad = act == ULTRAEP_SWIGLU_GRAD
-    _need(pre, M * (2 * N if grad else N) if grad or pre is not None else 0, 2, "pre")
+    _need_values(pre, M * (2 * N if grad else N) if grad or pre is not None else 0, _BF16, "pre")
     _need(y, M * (2 * N if grad else N // 2 if act == ULTRAEP_SWIGLU else N),
           4 if type_ == ULTRAEP_F32 else 2, "y")
     return _check(lib().ultraep_expert_matmul_bf16(
@@ -660,15 +675,16 @@ def ultraep_expert_weight_grad_ws_bytes(M, N, K, n_w) -> int:
 
 def ultraep_expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block, n_w, dw_stride,
                                accumulate, dw, ws, status, stream=None):
-    """block_w and ws may be None; dw is float32 or bfloat16."""
+    """block_w and ws may be None; dy and x are bfloat16 (or raw 16-bit integers), dw is float32
+    or bfloat16."""
     rc = (_native or _load_native()).expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block,
                                                        n_w, dw_stride, accumulate, dw, ws, status,
                                                        stream)
     if rc is not None:
         return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_weight_grad")
     type_ = _row_type(dw, "dw")
-    _need(dy, M * N, 2, "dy")
-    _need(x, M * K, 2, "x")
+    _need_values(dy, M * N, _BF16, "dy")
+    _need_values(x, M * K, _BF16, "x")
     _need_blocks(block_off, block_w, n_block, status)
     _need(dw, (n_w - 1) * dw_stride + N * K if n_w > 0 else 0, 4 if type_ == ULTRAEP_F32 else 2,
           "dw")
@@ -680,14 +696,14 @@ def ultraep_expert_weight_grad(dy, x, M, N, K, block_off, block_w, n_block, n_w,
 
 
 def ultraep_quant_blocks(x, rows, K, ld, q, ldq, scale, stream=None):
-    """q and scale have one-byte elements (uint8, or torch's float8 types)."""
+    """q is float8_e4m3fn, scale float8_e8m0fnu, or either raw bytes."""
     rc = (_native or _load_native()).quant_blocks(x, rows, K, ld, q, ldq, scale, stream)
     if rc is not None:
         return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_quant_blocks")
     type_ = _row_type(x, "x") if rows > 0 else ULTRAEP_BF16
     _need_rows(x, rows, K, ld, type_, "x")
-    _need(q, rows * ldq, 1, "q")
-    _need(scale, rows * scale_pitch(K), 1, "scale")
+    _need_values(q, rows * ldq, _E4M3, "q")
+    _need_values(scale, rows * scale_pitch(K), _E8M0, "scale")
     return _check(lib().ultraep_quant_blocks(_ptr(x), type_, rows, K, ld, _ptr(q), ldq, _ptr(scale),
                                              _stream(stream)), "ultraep_quant_blocks")
 
@@ -700,18 +716,19 @@ def scale_pitch(K):
 
 def ultraep_expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K, block_off, block_w, n_block, act,
                               y, status, stream=None):
-    """xq, wq and the scales have one-byte elements; block_w may be None (block g takes
-    weight g); act: ULTRAEP_NO_ACT or ULTRAEP_SWIGLU; y is float32 or bfloat16."""
+    """xq and wq are float8_e4m3fn, their scales float8_e8m0fnu, or any of them raw bytes;
+    block_w may be None (block g takes weight g); act: ULTRAEP_NO_ACT or ULTRAEP_SWIGLU; y is
+    float32 or bfloat16."""
     rc = (_native or _load_native()).expert_matmul_fp8(xq, x_scale, M, wq, w_scale, n_w, N, K,
                                                       block_off, block_w, n_block, act, y, status,
                                                       stream)
     if rc is not None:
         return rc if rc == ULTRAEP_OK else _check(rc, "ultraep_expert_matmul_fp8")
     type_ = _row_type(y, "y") if M > 0 else ULTRAEP_BF16
-    _need(xq, M * K, 1, "xq")
-    _need(x_scale, M * scale_pitch(K), 1, "x_scale")
-    _need(wq, n_w * N * K, 1, "wq")
-    _need(w_scale, n_w * N * scale_pitch(K), 1, "w_scale")
+    _need_values(xq, M * K, _E4M3, "xq")
+    _need_values(x_scale, M * scale_pitch(K), _E8M0, "x_scale")
+    _need_values(wq, n_w * N * K, _E4M3, "wq")
+    _need_values(w_scale, n_w * N * scale_pitch(K), _E8M0, "w_scale")
     _need_blocks(block_off, block_w, n_block, status)
     _need(y, M * (N // 2 if act else N), 4 if type_ == ULTRAEP_F32 else 2, "y")
     return _check(lib().ultraep_expert_matmul_fp8(

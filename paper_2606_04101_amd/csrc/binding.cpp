@@ -103,6 +103,22 @@ struct Args {
     type = d == at::kFloat ? ULTRAEP_F32 : ULTRAEP_BF16;
     return tensor(a[i], n, d == at::kFloat ? 4 : 2);
   }
+  // values whose format the element size does not tell: their own type or raw integers
+  static bool is_bf16(at::ScalarType d) { return d == at::kBFloat16 || d == at::kShort || d == at::kUInt16; }
+  static bool is_e4m3(at::ScalarType d) { return d == at::kFloat8_e4m3fn || d == at::kByte || d == at::kChar; }
+  static bool is_e8m0(at::ScalarType d) { return d == at::kFloat8_e8m0fnu || d == at::kByte || d == at::kChar; }
+  template <class T>
+  T *values(int i, wide n, bool (*is)(at::ScalarType)) {
+    if (ok && n > 0) {
+      if (!THPVariable_CheckExact(a[i])) return fail(), nullptr;
+      const at::Tensor &t = THPVariable_Unpack(a[i]);
+      if (!t.defined() || !is(t.scalar_type())) return fail(), nullptr;
+    }
+    return tensor<T>(i, n);
+  }
+  uint16_t *bf16(int i, wide n) { return values<uint16_t>(i, n, is_bf16); }
+  uint8_t *e4m3(int i, wide n) { return values<uint8_t>(i, n, is_e4m3); }
+  uint8_t *e8m0(int i, wide n) { return values<uint8_t>(i, n, is_e8m0); }
   // a float, or an int
   float number(int i) {
     if (!ok || !(PyFloat_CheckExact(a[i]) || PyLong_CheckExact(a[i]))) return fail(), 0.f;
@@ -518,11 +534,12 @@ ENTRY(expert_matmul_bf16, 16, {
   const int32_t n_w = v.i32(3), N = v.i32(5), K = v.i32(6), trans = v.flag(7), n = v.i32(10);
   const int32_t act = v.flag(11);
   const bool grad = act == ULTRAEP_SWIGLU_GRAD;
-  auto *x = v.tensor<uint16_t>(0, wide(M) * K);
-  auto *w = v.tensor<uint16_t>(2, n_w > 0 ? (wide(n_w) - 1) * stride + wide(N) * K : 0);
+  auto *x = v.bf16(0, wide(M) * K);
+  auto *w = v.bf16(2, n_w > 0 ? (wide(n_w) - 1) * stride + wide(N) * K : 0);
   auto *off = v.tensor<int64_t>(8, wide(n) + 1);
   auto *bw = v.maybe<int32_t>(9, n);
-  auto *pre = grad ? v.tensor<uint16_t>(12, wide(M) * 2 * N) : v.maybe<uint16_t>(12, wide(M) * N);
+  const bool left_out = !grad && v.ok && argv[12] == Py_None;
+  auto *pre = left_out ? nullptr : v.bf16(12, wide(M) * (grad ? 2 * wide(N) : N));
   int32_t type;
   void *y = v.rows(13, wide(M) * (grad ? 2 * wide(N) : act == ULTRAEP_SWIGLU ? N / 2 : N), type);
   auto *status = v.tensor<int32_t>(14, 1);
@@ -537,8 +554,8 @@ ENTRY(expert_matmul_bf16, 16, {
 ENTRY(expert_weight_grad, 15, {
   const int64_t M = v.i64(2), stride = v.i64(9);
   const int32_t N = v.i32(3), K = v.i32(4), n = v.i32(7), n_w = v.i32(8), acc = v.flag(10);
-  auto *dy = v.tensor<uint16_t>(0, wide(M) * N);
-  auto *x = v.tensor<uint16_t>(1, wide(M) * K);
+  auto *dy = v.bf16(0, wide(M) * N);
+  auto *x = v.bf16(1, wide(M) * K);
   auto *off = v.tensor<int64_t>(5, wide(n) + 1);
   auto *bw = v.maybe<int32_t>(6, n);
   int32_t type;
@@ -558,8 +575,8 @@ ENTRY(quant_blocks, 8, {
   const int64_t rows = v.i64(1), K = v.i64(2), ld = v.i64(3), ldq = v.i64(5);
   int32_t type;
   void *x = v.rows(0, strided(rows, K, ld), type);
-  auto *q = v.tensor<uint8_t>(4, wide(rows) * ldq);
-  auto *scale = v.tensor<uint8_t>(6, wide(rows) * scale_pitch(K));
+  auto *q = v.e4m3(4, wide(rows) * ldq);
+  auto *scale = v.e8m0(6, wide(rows) * scale_pitch(K));
   hipStream_t s = v.stream(7);
   return finish(v, [&] { return lib.quant_blocks(x, type, rows, K, ld, q, ldq, scale, s); });
 })
@@ -568,10 +585,10 @@ ENTRY(quant_blocks, 8, {
 ENTRY(expert_matmul_fp8, 15, {
   const int64_t M = v.i64(2);
   const int32_t n_w = v.i32(5), N = v.i32(6), K = v.i32(7), n = v.i32(10), act = v.flag(11);
-  auto *xq = v.tensor<uint8_t>(0, wide(M) * K);
-  auto *xs = v.tensor<uint8_t>(1, wide(M) * scale_pitch(K));
-  auto *wq = v.tensor<uint8_t>(3, wide(n_w) * N * K);
-  auto *ws = v.tensor<uint8_t>(4, wide(n_w) * N * scale_pitch(K));
+  auto *xq = v.e4m3(0, wide(M) * K);
+  auto *xs = v.e8m0(1, wide(M) * scale_pitch(K));
+  auto *wq = v.e4m3(3, wide(n_w) * N * K);
+  auto *ws = v.e8m0(4, wide(n_w) * N * scale_pitch(K));
   auto *off = v.tensor<int64_t>(8, wide(n) + 1);
   auto *bw = v.maybe<int32_t>(9, n);
   int32_t type;
