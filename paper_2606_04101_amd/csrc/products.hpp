@@ -378,13 +378,32 @@ __device__ __forceinline__ void tile_items(Work &work, int8_t *s_lds) {
 }
 
 // The results of the largest tiles leave past the caches: rows of 8192 bytes (32768 rows, K =
-// 1408, 8 bits) in 210 us, through them 230.  The smaller tiles' leave through them, so that the
-// parts of a line that two tiles or rows write meet there: rows of 3680 bytes (weights' gradient
-// of 22 rows, 4 of 6176 x 920 to fp32) in 26 us, past them 46; whole lines take the same.
-template <class S, class V>
-__device__ __forceinline__ void store_result(V v, V *p) {
-  if constexpr (S::kAhead) __builtin_nontemporal_store(v, p);
-  else *p = v;
+// 1408, 8 bits) in 210 us, through them 230.  So do the smaller tiles' whose rows are whole halves
+// of lines, 64 bytes: rows of 2880 bytes (weights' gradient of 2991 rows, 16 of 2880 x 1440 to
+// bf16) in 54 us, through them 73; 8192 bytes (2048 rows, 4 of 4096 x 1024 with SwiGLU) in 34, 35.
+// Others leave through the caches, so that the parts of a half that two tiles or rows write meet
+// there: rows of 3680 bytes (22 rows, 4 of 6176 x 920 to fp32) in 22 us, past them 42; 12192 bytes
+// (1000 rows, 4 of 3048 x 512 to fp32) in 10.4, 10.9.  (Among calls on other buffers: where one
+// is made over and over its results lie in the caches already, and both take the same.)
+template <class V>
+__device__ __forceinline__ void store_result(V v, V *p, std::true_type) {
+  asm volatile("");  // (else the compiler makes one store of both kinds, through the caches)
+  __builtin_nontemporal_store(v, p);
+  asm volatile("");
+}
+template <class V>
+__device__ __forceinline__ void store_result(V v, V *p, std::false_type) {
+  *p = v;
+}
+// stores(std::true_type()) past the caches, stores(std::false_type()) through them
+template <class S, class F>
+__device__ __forceinline__ void by_halves(bool halves, F stores) {
+  if (S::kAhead || halves) stores(std::true_type());
+  else stores(std::false_type());
+}
+// whether rows of so many bytes from `at` on begin and end with halves of lines
+__device__ __forceinline__ bool whole_halves(const void *at, int64_t row_bytes) {
+  return (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at)) | static_cast<uint32_t>(row_bytes)) % 64 == 0;
 }
 
 // Results of 32 rows x 64 channels (32 in fp32) leave through 4 KiB of LDS a wave, so that
@@ -577,6 +596,8 @@ struct ProductWork {
     constexpr int kSize = kBf16 ? 2 : 4;
     const int nw = o.n0 + wn * kOutW, limit = min(n_out, nw + kOutW);
     char *const y = static_cast<char *>(a.y);
+    // (the gradient of SwiGLU is rows of N and N channels, what SwiGLU keeps of half and half)
+    const bool y_halves = whole_halves(y, static_cast<int64_t>(n_out) * kSize), pre_halves = whole_halves(a.pre, N);
 #pragma unroll
     for (int b = 0; b < kBands; ++b) {
       const int r0 = (wm * kBands + b) * 32;
@@ -590,15 +611,17 @@ struct ProductWork {
       if (S::kAhead && b == kBands - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       else asm volatile("" : : : "memory");
       // the stage's channels to rows of ld elements, from channel c0 on, below `end`
-      auto leave = [&](char *dst, int64_t ld, int size, int c0, int end) {
+      auto leave = [&](char *dst, int64_t ld, int size, int c0, int end, bool halves) {
         const int c = c0 + (st.el & 7) * (16 / size);
+        by_halves<S>(halves, [&](auto past) {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          const int r = r0 + st.row(p);
-          const v4u v = st.get<v4u>(p);
-          if (r < o.rows && c < end)
-            store_result<S>(v, reinterpret_cast<v4u *>(dst + ((o.row + r) * ld + c) * size));
-        }
+          for (int p = 0; p < 4; ++p) {
+            const int r = r0 + st.row(p);
+            const v4u v = st.get<v4u>(p);
+            if (r < o.rows && c < end)
+              store_result(v, reinterpret_cast<v4u *>(dst + ((o.row + r) * ld + c) * size), past);
+          }
+        });
         __builtin_amdgcn_sched_barrier(0);
       };
       // the channels' 16s from `from` on, as many as the stage takes and there are
@@ -628,13 +651,15 @@ struct ProductWork {
                           e % 2 ? bf16_at_high(u[e / 2]) : bf16_at_low(u[e / 2]), da[e], db[e]);
             if (r < o.rows && c < limit) {
               char *at = y + ((o.row + r) * 2 * N + c) * kSize, *at2 = at + static_cast<int64_t>(N) * kSize;
-              if (kBf16) {
-                store_result<S>(v2u{pack_bf16(da[0], da[1]), pack_bf16(da[2], da[3])}, reinterpret_cast<v2u *>(at));
-                store_result<S>(v2u{pack_bf16(db[0], db[1]), pack_bf16(db[2], db[3])}, reinterpret_cast<v2u *>(at2));
-              } else {
-                store_result<S>(v4f{da[0], da[1], da[2], da[3]}, reinterpret_cast<v4f *>(at));
-                store_result<S>(v4f{db[0], db[1], db[2], db[3]}, reinterpret_cast<v4f *>(at2));
-              }
+              by_halves<S>(y_halves, [&](auto past) {
+                if constexpr (kBf16) {
+                  store_result(v2u{pack_bf16(da[0], da[1]), pack_bf16(da[2], da[3])}, reinterpret_cast<v2u *>(at), past);
+                  store_result(v2u{pack_bf16(db[0], db[1]), pack_bf16(db[2], db[3])}, reinterpret_cast<v2u *>(at2), past);
+                } else {
+                  store_result(v4f{da[0], da[1], da[2], da[3]}, reinterpret_cast<v4f *>(at), past);
+                  store_result(v4f{db[0], db[1], db[2], db[3]}, reinterpret_cast<v4f *>(at2), past);
+                }
+              });
             }
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -648,7 +673,7 @@ struct ProductWork {
 #pragma unroll
             for (int i = 0; i < kCols; i += 2) {
               put(std::true_type(), 2 * i, [&](int f, int j) { return acc[gate(f) + 2 * s][j]; });
-              leave(reinterpret_cast<char *>(a.pre), N, 2, s * half + nw + i * 32, s * half + limit);
+              leave(reinterpret_cast<char *>(a.pre), N, 2, s * half + nw + i * 32, s * half + limit, pre_halves);
             }
         }
       }
@@ -662,7 +687,7 @@ struct ProductWork {
             return acc[f][j];
           }
         });
-        leave(y, n_out, kSize, nw + i * 32, limit);
+        leave(y, n_out, kSize, nw + i * 32, limit, y_halves);
       }
     }
   }

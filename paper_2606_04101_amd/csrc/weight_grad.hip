@@ -190,6 +190,7 @@ struct GradWork {
   template <class Acc>
   __device__ void results(const Out &o, Early &old, Acc &acc, int8_t *lds, int wn, int wm) const {
     const Stage st(lds);
+    const bool halves = whole_halves(a.dw, (static_cast<int64_t>(K) | a.dw_stride) * kSize);
 #pragma unroll
     for (int b = 0; b < kBands; ++b) {
 #pragma unroll
@@ -225,7 +226,7 @@ struct GradWork {
           } else {
             word = st.get<v4u>(p);
           }
-          if (at) store_result<S>(word, reinterpret_cast<Word *>(at));
+          if (at) by_halves<S>(halves, [&](auto past) { store_result(word, reinterpret_cast<Word *>(at), past); });
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -368,8 +369,9 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 //   M = 8192: N = 2048 37 / 37, 1024 31 / 21; 64 weights, N = 1024, K = 2048: M = 4096 91 / 104; 16
 //   weights, N = 2880, K = 1440: M = 2000 69 / 56 (bf16 results 48 / 40)
 //   Out of a cache that holds no results yet: 16 weights, N = 2880, K = 1440: M = 8192 113 / 104, 2991
-//   to bf16 76 / 57; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
-//   Rows of no whole lines: 6 weights, N = 5584, K = 3048, M = 277 to bf16 130 / 63
+//   to bf16 76 / 54; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
+//   Rows of no whole lines, to bf16: 6 weights, N = 5584, K = 3048, M = 277 127 / 64; K = 3040, M = 1024
+//   77 / 71; 6 of 4096 x 1440, M = 2048 46 / 43
 template <bool kBf16, bool kAdd>
 static void choose_grad(const GradArgs &a, hipStream_t stream) {
   auto tiles = [&](int64_t n, int64_t k) {
