@@ -86,7 +86,8 @@ __device__ __forceinline__ float scale_value(int byte) {
 // kTied: the wave's sums take all 256 accumulation registers, where the compiler, left to
 // choose another register for a product's result than for its addend, copies sums about.
 // It does not know these instructions' latencies: `settle` stands between what writes their
-// operands with the vector ALU and them, and between them and the reading of the sums.
+// operands with the vector ALU and them, and between them and the reading of the sums.  What the
+// compiler puts around them is checked in the built code, by tests/test_written_out.py.
 template <Math kKind, bool kTied>
 __device__ __forceinline__ void multiply(const v4i &a, int, const v4i &b, int, v4f &c) {
   if constexpr (kTied)

@@ -108,7 +108,9 @@ struct RowTiles {
 };
 
 // 16 bytes a lane from base + off straight into LDS, lane l's at lds + 16 l.
-// The wait for it is the caller's (vmcnt).
+// The wait for it is the caller's (vmcnt).  A scalar register that the vector ALU wrote may be an
+// address 5 instructions later, which the compiler does not see to here; in the built code
+// they lie further apart (tests/test_written_out.py).
 __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
