@@ -21,3 +21,10 @@ hipError_t launch_expert_matmul_bf16(const uint16_t *x, int64_t M, const uint16_
 }
 
 }  // namespace uep
+
+// Which of product_tile's tiles a call takes, for the tests (host only): eight, whether of 8 bits
+extern "C" int uep_product_tile(int64_t M, int32_t n_block, int32_t N, int32_t K, int32_t eight, int32_t trans,
+                                int32_t act, int32_t type) {
+  const uep::Math kind = !eight ? uep::kMath16 : type == ULTRAEP_BF16 ? uep::kMath8 : uep::kMathWide;
+  return uep::product_tile(kind, trans, act, M, n_block, N, K);
+}

@@ -227,6 +227,9 @@ void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
   hipLaunchKernelGGL((k_product<kN, kM, kWn, kWm, kAhead, kRing, kKind, kTrans, kAct, kBf16>), grid, block, 0, stream, a, n_col);
 }
 
+// four waves' worth of steps
+inline bool deep_k(Math kind, int32_t K) { return static_cast<int64_t>(K) * (kind == kMath16 ? 2 : 1) >= 4096; }
+
 // The tiles by the rounds that they would take: a round is 256 of them, one a compute unit (of
 // 128 x 128 two a compute unit, 512), and its time is in thousandths of a round of 256 x 256,
 // bf16 / 8 bits.  `rows`: M over the blocks, of which the host cannot know how many are empty
@@ -259,36 +262,44 @@ void start_product(const ProductArgs &a, int n_wg, hipStream_t stream) {
 //   (Where the weights' bytes bound the call the choice misses the best by up to an eighth: 10
 //   blocks of 6 rows, weights [K][N], take 130 us of 128 x 64 where two tiles of 128 x 128 a
 //   compute unit take 114.)
-template <Math kKind, bool kTrans, int kAct, bool kBf16>
-void choose_product(const ProductArgs &a, hipStream_t stream) {
-  const int64_t blocks = a.M < a.n_block ? a.M : a.n_block;
+// 0: 256 x 256, 1: 128 x 128, two buffers, 2: four, 3: 128 x 64, 4 to 6: thin of 64, 32, 16 rows
+inline int product_tile(Math kind, bool trans, int act, int64_t M, int32_t n_block, int32_t N, int32_t K) {
+  const int64_t blocks = M < n_block ? M : n_block;
   auto items = [&](int64_t tile_rows, int64_t channels) {
-    const double whole = static_cast<double>((a.M + tile_rows - 1) / tile_rows);
-    const double several = static_cast<double>(a.M) / tile_rows + blocks / 3.;
-    return (blocks == 1 ? whole : several > blocks ? several : blocks) * ((a.N + channels - 1) / channels);
+    const double whole = static_cast<double>((M + tile_rows - 1) / tile_rows);
+    const double several = static_cast<double>(M) / tile_rows + blocks / 3.;
+    return (blocks == 1 ? whole : several > blocks ? several : blocks) * ((N + channels - 1) / channels);
   };
   auto time = [&](double n, int of, int cost, double more) {
     const double rounds = n / of;
     if (blocks > 1) return cost * (rounds + more > 1 ? rounds + more : 1);
     return cost * std::ceil(rounds);
   };
-  constexpr bool k8 = kKind == kMath8, kBig = kKind != kMathWide;
-  constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
-  const bool deep = static_cast<int64_t>(a.K) * (kKind == kMath16 ? 2 : 1) >= 4096;  // four waves' worth of steps
+  const bool k8 = kind == kMath8, large = kind != kMathWide, thin = !trans && act != ULTRAEP_SWIGLU_GRAD;
+  const bool deep = deep_k(kind, K);
   const double big = items(256, 256), last = std::fmod(big, 256);
   constexpr double kNever = 1e30;
   const double times[] = {
-      !kBig ? kNever : blocks == 1 && big > 256 && last > 0 && last <= 64 ? (big - last) / 256 * 1000 + 350 : time(big, 256, 1000, 0.175),
+      !large ? kNever : blocks == 1 && big > 256 && last > 0 && last <= 64 ? (big - last) / 256 * 1000 + 350 : time(big, 256, 1000, 0.175),
       k8 ? kNever : time(items(128, 128), 512, 600, 0.5),  // (8 bits: 1050 to 1100 of two of the next's)
       time(items(128, 128), 256, k8 ? 550 : 360, 0.5),
       time(items(64, 128), 256, k8 ? 370 : 250, 0.5),
-      kThin ? time(items(64, 64), 256, k8 ? 190 : 155, 0.5) : kNever,
-      kThin ? time(items(32, 64), 256, k8 ? 135 : 115, 0.5) : kNever,
-      kThin ? time(items(16, deep ? 32 : 64), 256, deep ? 70 : 80, 0.5) : kNever,
+      thin ? time(items(64, 64), 256, k8 ? 190 : 155, 0.5) : kNever,
+      thin ? time(items(32, 64), 256, k8 ? 135 : 115, 0.5) : kNever,
+      thin ? time(items(16, deep ? 32 : 64), 256, deep ? 70 : 80, 0.5) : kNever,
   };
   int best = 0;
   for (int i = 1; i < 7; ++i)
     if (times[i] < times[best]) best = i;
+  return best;
+}
+
+template <Math kKind, bool kTrans, int kAct, bool kBf16>
+void choose_product(const ProductArgs &a, hipStream_t stream) {
+  constexpr bool k8 = kKind == kMath8, kBig = kKind != kMathWide;
+  constexpr bool kThin = !kTrans && kAct != ULTRAEP_SWIGLU_GRAD;
+  const bool deep = deep_k(kKind, a.K);
+  const int best = product_tile(kKind, kTrans, kAct, a.M, a.n_block, a.N, a.K);
   if constexpr (kBig) {
     if (best == 0) start_product<256, 256, 2, 2, true, 2, kKind, kTrans, kAct, kBf16>(a, 256, stream);
   }

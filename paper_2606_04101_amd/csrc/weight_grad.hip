@@ -372,15 +372,18 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 //   to bf16 76 / 54; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
 //   Rows of no whole lines, to bf16: 6 weights, N = 5584, K = 3048, M = 277 127 / 64; K = 3040, M = 1024
 //   77 / 71; 6 of 4096 x 1440, M = 2048 46 / 43
-template <bool kBf16, bool kAdd>
-static void choose_grad(const GradArgs &a, hipStream_t stream) {
+static bool large_tiles(const GradArgs &a, bool bf16) {
   auto tiles = [&](int64_t n, int64_t k) {
     return int64_t(a.slots ? a.slots : a.n_w) * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
   };
   const int64_t big = (tiles(256, 256) + 255) / 256 * 20, mid = (tiles(128, 128) + 511) / 512 * 13;
-  const bool lines = a.K * (kBf16 ? 2 : 4) % 128 == 0;  // the smaller tiles' stores may fill them together
+  const bool lines = a.K * (bf16 ? 2 : 4) % 128 == 0;  // the smaller tiles' stores may fill them together
   const bool few = a.M < int64_t(768) * a.n_w && (!lines || tiles(128, 128) < 4 * tiles(256, 256));
-  if (big < mid && !few) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
+  return big < mid && !few;
+}
+template <bool kBf16, bool kAdd>
+static void choose_grad(const GradArgs &a, hipStream_t stream) {
+  if (large_tiles(a, kBf16)) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
   else start_grad<128, 128, 2, 2, false, kBf16, kAdd>(a, 512, stream);
 }
 
@@ -415,3 +418,12 @@ hipError_t launch_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int6
 }
 
 }  // namespace uep
+
+// Whether a call takes tiles of 256 x 256, for the tests (host only): parts, whether it has a
+// workspace
+extern "C" int uep_weight_grad_large(int64_t M, int32_t N, int32_t K, int32_t n_w, int32_t type, int32_t parts) {
+  const int32_t slots = parts ? uep::row_slots(M, N, K, n_w) : 0;
+  uep::GradArgs a{};
+  a.M = M, a.N = N, a.K = K, a.n_w = n_w, a.slots = slots;
+  return uep::large_tiles(a, type == ULTRAEP_BF16 && !slots);
+}
