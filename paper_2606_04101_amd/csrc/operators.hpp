@@ -138,8 +138,9 @@ __device__ __forceinline__ int lanes_max(int v) {
 }
 __device__ __forceinline__ float wave_sum_f(float v) { return lanes_sum<kWave>(v); }
 
-// exp by the hardware's exp2, 1 ulp.  The product with log2(e) is rounded before it, so a
-// result between 2^-126 and infinity is (|x| + 2) 2^-24 off at most, relatively; below it is 0.
+// exp by the hardware's exp2, 1 ulp.  The product with log2(e) is rounded before it, and fp32's
+// log2(e) is 0.23 x 2^-24 off, so a result between 2^-126 and infinity is (1.23 |x| + 2) 2^-24 off at
+// most, relatively; below it is 0.
 __device__ __forceinline__ float fast_exp(float x) {
   return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
 }

@@ -155,10 +155,10 @@ __device__ __forceinline__ uint32_t lds_address(T *p) {
 }
 
 // v / (1 + exp(-v)) by the hardware's exp2 and reciprocal: a relative error of
-// (|v| + 5) 2^-24 at most for v >= -87; below, where it is under 2e-36 in magnitude, it
-// becomes 0.  |v| 2^-24 is far below the rounding of 8-bit operands or of a bf16 result;
-// with expf and a division the epilogue's arithmetic costs 65 us of 3350 at
-// 131072 x 4096 x 7168 in 8-bit integers.
+// (1.23 |v| + 6) 2^-24 at most (exp's, 1 of the sum, 2 of the reciprocal, 1 of the product) for
+// v >= -87.3; below, where it is under 2e-36 in magnitude, it becomes 0.  |v| 2^-24 is far below the
+// rounding of 8-bit operands or of a bf16 result, and fp32 results are held to it; with expf and
+// a division the epilogue's arithmetic costs 65 us of 3350 at 131072 x 4096 x 7168 in 8-bit integers.
 __device__ __forceinline__ float silu(float v) { return v * fast_rcp(1.f + fast_exp(-v)); }
 
 }  // namespace uep
