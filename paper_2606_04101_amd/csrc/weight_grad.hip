@@ -190,7 +190,8 @@ struct GradWork {
   template <class Acc>
   __device__ void results(const Out &o, Early &old, Acc &acc, int8_t *lds, int wn, int wm) const {
     const Stage st(lds);
-    const bool halves = whole_halves(a.dw, (static_cast<int64_t>(K) | a.dw_stride) * kSize);
+    // (the lines of what is added to have just been read: either kind of store takes the same)
+    const bool halves = !kAdd && whole_halves(a.dw, (static_cast<int64_t>(K) | a.dw_stride) * kSize);
 #pragma unroll
     for (int b = 0; b < kBands; ++b) {
 #pragma unroll
