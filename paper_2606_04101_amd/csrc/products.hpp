@@ -396,14 +396,15 @@ template <class V>
 __device__ __forceinline__ void store_result(V v, V *p, std::false_type) {
   *p = v;
 }
-// stores(std::true_type()) past the caches, stores(std::false_type()) through them
+// stores(std::true_type()) past the caches, stores(std::false_type()) through them (as all of the
+// few rows of the smallest tiles: 8 rows, N = 256, K = 3688 20.3 us, with both kinds 20.9)
 template <class S, class F>
 __device__ __forceinline__ void by_halves(bool halves, F stores) {
-  if (S::kAhead || halves) stores(std::true_type());
+  if (S::kAhead || (S::kM >= 128 && halves)) stores(std::true_type());
   else stores(std::false_type());
 }
 // whether rows of so many bytes from `at` on begin and end with halves of lines
-__device__ __forceinline__ bool whole_halves(const void *at, int64_t row_bytes) {
+__host__ __device__ inline bool whole_halves(const void *at, int64_t row_bytes) {
   return (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at)) | static_cast<uint32_t>(row_bytes)) % 64 == 0;
 }
 

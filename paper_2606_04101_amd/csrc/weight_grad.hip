@@ -22,7 +22,7 @@ struct GradArgs {
 // that are summed over.  Both sides are transposed on their way from LDS.  The steps of an
 // item are its blocks' rows by 64; a block's last may have fewer.  Blocks are looked at in
 // runs of 64, one a lane.
-template <class S, bool kBf16, bool kAdd>
+template <class S, bool kBf16, bool kAdd, bool kPast>
 struct GradWork {
   static constexpr uint32_t pitch = 0;
   const GradArgs &a;
@@ -190,8 +190,6 @@ struct GradWork {
   template <class Acc>
   __device__ void results(const Out &o, Early &old, Acc &acc, int8_t *lds, int wn, int wm) const {
     const Stage st(lds);
-    // (the lines of what is added to have just been read: either kind of store takes the same)
-    const bool halves = !kAdd && whole_halves(a.dw, (static_cast<int64_t>(K) | a.dw_stride) * kSize);
 #pragma unroll
     for (int b = 0; b < kBands; ++b) {
 #pragma unroll
@@ -227,7 +225,7 @@ struct GradWork {
           } else {
             word = st.get<v4u>(p);
           }
-          if (at) by_halves<S>(halves, [&](auto past) { store_result(word, reinterpret_cast<Word *>(at), past); });
+          if (at) store_result(word, reinterpret_cast<Word *>(at), std::bool_constant<kPast>());
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -291,7 +289,7 @@ __device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int
 // rows of 5 weights of 4096 x 7168 to fp32 in 1622 to 1722 us by the card (1.12 to 1.19): 2240 tiles are 8.75
 // rounds of 256 and the fp32 results 587 MB.  Few rows a weight are bound by the results' bytes
 // (2991 rows over 16 weights of 2880 x 1440, bf16: 53 us, of which the bytes take 30).
-template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd, bool kPast>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
   using S = Tile<kN, kM, kWn, kWm, kAhead, 2, kMath16, true, true>;
   __shared__ __align__(1024) int8_t s_lds[S::kLds];
@@ -302,7 +300,7 @@ __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int3
   constexpr int kXcd = 8;  // the workgroups of one XCD take neighbouring items
   const int grid = gridDim.x, per_xcd = grid / kXcd;  // the grid is a multiple
   const int slot = blockIdx.x % kXcd * per_xcd + blockIdx.x / kXcd;
-  GradWork<S, kBf16, kAdd> work(a, s_first, slot, grid, tn, tk, (a.slots ? a.slots : a.n_w) * tn * tk);
+  GradWork<S, kBf16, kAdd, kPast> work(a, s_first, slot, grid, tn, tk, (a.slots ? a.slots : a.n_w) * tn * tk);
   tile_items<S>(work, s_lds);
 }
 
@@ -353,12 +351,12 @@ size_t weight_grad_ws_bytes(int64_t M, int32_t N, int32_t K, int32_t n_w) {
   return slots ? static_cast<size_t>(slots) * N * K * 4 : 16;
 }
 
-template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd>
+template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd, bool kPast>
 static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
   const int32_t tn = (a.N + kM - 1) / kM, tk = (a.K + kN - 1) / kN;
   const int64_t items = int64_t(a.slots ? a.slots : a.n_w) * tn * tk;
   const dim3 grid(static_cast<unsigned>(items < n_wg ? (items + 7) / 8 * 8 : n_wg)), block(64 * kWn * kWm);
-  hipLaunchKernelGGL((k_weight_grad<kN, kM, kWn, kWm, kAhead, kBf16, kAdd>), grid, block, 0, stream, a, tn, tk);
+  hipLaunchKernelGGL((k_weight_grad<kN, kM, kWn, kWm, kAhead, kBf16, kAdd, kPast>), grid, block, 0, stream, a, tn, tk);
 }
 
 // Tiles of 256 x 256 or, two a compute unit, of 128 x 128, by the rounds that either takes, in
@@ -371,8 +369,8 @@ static void start_grad(const GradArgs &a, int n_wg, hipStream_t stream) {
 //   weights, N = 2880, K = 1440: M = 2000 69 / 56 (bf16 results 48 / 40)
 //   Out of a cache that holds no results yet: 16 weights, N = 2880, K = 1440: M = 8192 113 / 104, 2991
 //   to bf16 76 / 54; 6 of 4096 x 1408, M = 2048 to bf16 46 / 40; 10 of 4096 x 7168, M = 4096 353 / 391
-//   Rows of no whole lines, to bf16: 6 weights, N = 5584, K = 3048, M = 277 127 / 64; K = 3040, M = 1024
-//   77 / 71; 6 of 4096 x 1440, M = 2048 46 / 43
+//   Rows of no whole lines, to bf16: 6 weights, N = 5584, K = 3048, M = 277 127 / 63; K = 3040, M = 1024
+//   77 / 70; 6 of 4096 x 1440, M = 2048 46 / 41
 static bool large_tiles(const GradArgs &a, bool bf16) {
   auto tiles = [&](int64_t n, int64_t k) {
     return int64_t(a.slots ? a.slots : a.n_w) * ((a.N + n - 1) / n) * ((a.K + k - 1) / k);
@@ -384,8 +382,15 @@ static bool large_tiles(const GradArgs &a, bool bf16) {
 }
 template <bool kBf16, bool kAdd>
 static void choose_grad(const GradArgs &a, hipStream_t stream) {
-  if (large_tiles(a, kBf16)) start_grad<256, 256, 2, 2, true, kBf16, kAdd>(a, 256, stream);
-  else start_grad<128, 128, 2, 2, false, kBf16, kAdd>(a, 512, stream);
+  if (large_tiles(a, kBf16)) return start_grad<256, 256, 2, 2, true, kBf16, kAdd, true>(a, 256, stream);
+  // Stores as by_halves chooses them; here by instances, since small calls feel the longer
+  // code (31 rows, 160 x 160 5.0 us, with both kinds 5.2).  What is added to has just been read, and
+  // parts are read again at once: through the caches (added to, either takes the same; 2535 rows,
+  // 96 x 224 in parts 14.2, past them 15.0).
+  if constexpr (!kAdd)
+    if (a.slots == 0 && whole_halves(a.dw, (a.K | a.dw_stride) * (kBf16 ? 2 : 4)))
+      return start_grad<128, 128, 2, 2, false, kBf16, kAdd, true>(a, 512, stream);
+  start_grad<128, 128, 2, 2, false, kBf16, kAdd, false>(a, 512, stream);
 }
 
 hipError_t launch_expert_weight_grad(const uint16_t *dy, const uint16_t *x, int64_t M, int32_t N,
