@@ -697,7 +697,7 @@ struct ProductWork {
 
 // y = act(x w^T) by tiles of kN channels x kM rows.  Of 256 x 256 (4 waves of 128 x 128, 64
 // parts of 16 x 16 each) a step of 64 KiB feeds 16.8 MFLOP, so the matrix units bound it, and
-// before their issue rate their power: 8192^3 takes 785 us (1.40 PFLOP/s) where registers
+// before their issue rate their power: 8192^3 takes 769 to 785 us (1.40 to 1.43 PFLOP/s) where registers
 // alone, fed with random data, reach 1.95, and fewer stalls no longer shorten it;
 // products of 32 x 32 reach 1.57 in registers and were slower here by a tenth.  Results leave
 // in a burst, all compute units in step, of 9 to 13 us a round of tiles; the next tile's loads

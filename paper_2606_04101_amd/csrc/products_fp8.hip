@@ -50,7 +50,8 @@ struct Eight {
 // nearest-even is the only one.
 //   Bound by memory: 131072 rows of 7168 bf16 (2.8 GB) take 486 us, 5.8 TB/s, with 7 words
 // at a time (one word 518 to 543, four 506, loads that stay in the caches 543); 131072 rows
-// of 2048 126 us with 4 (two 148); 40960 of 520 15 us with 2 (7 28).  Where there are few
+// of 2048 126 us with 4 (two 148); 40960 of 520 15 us with 2 (7 28).  Of other lengths the last 7
+// are filled in part: 131072 rows of 4096 305 us, 5.3 TB/s (the least), 5120 340, 5.9, 8192 573, 5.6.  Where there are few
 // waves, or a row is one word, each takes one, with loads that may stay: 2999 rows of 2888
 // 7.1 us (7.9 past the caches).
 template <bool kBf16, int kWords>

@@ -10,8 +10,8 @@ namespace uep {
 // Few rows a block: the weight's bytes bound the call.  A workgroup takes kRows weight
 // rows (with SwiGLU half of them gates, then their partners) and up to kTok rows; its waves
 // share K in steps of 128 bytes in turn, each through an LDS ring of its own that kDeep
-// steps fill, so no wave waits for another until they add their sums.  16 rows over 10 experts,
-// N = 4096, K = 7168 in 8 bits take 48 us, 6.1 TB/s of the weights' 294 MB; one row in bf16,
+// steps fill, so no wave waits for another until they add their sums.  16 rows over 9 experts,
+// N = 4096, K = 7168 in 8 bits take 48 us, 5.5 TB/s of the weights' 264 MB; one row in bf16,
 // N = 4096, K = 7168: 11.4 us, 5.1 TB/s.
 template <int kTok, int kRows, int kWaves, int kDeep, Math kKind, int kAct, bool kBf16>
 __global__ void __launch_bounds__(64 * kWaves) k_product_thin(ProductArgs a, int32_t n_col) {

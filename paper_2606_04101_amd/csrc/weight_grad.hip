@@ -286,9 +286,9 @@ __device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int
 
 // dw = dy^T x, a weight's tiles of kM rows x kN columns.  As the products bound by the matrix
 // units' power, with two transposing reads more a part: 780 us at 8192^3 (1.41 PFLOP/s), 32768
-// rows of 5 weights of 4096 x 7168 to fp32 in 1622 to 1722 us by the card (1.12 to 1.19): 2240 tiles are 8.75
+// rows of 5 weights of 4096 x 7168 to fp32 in 1577 to 1722 us by the card (1.12 to 1.22): 2240 tiles are 8.75
 // rounds of 256 and the fp32 results 587 MB.  Few rows a weight are bound by the results' bytes
-// (2991 rows over 16 weights of 2880 x 1440, bf16: 53 us, of which the bytes take 30).
+// (2991 rows over 16 weights of 2880 x 1440, bf16: 54 us, of which the bytes take 25).
 template <int kN, int kM, int kWn, int kWm, bool kAhead, bool kBf16, bool kAdd, bool kPast>
 __global__ void __launch_bounds__(64 * kWn * kWm) k_weight_grad(GradArgs a, int32_t tn, int32_t tk) {
   using S = Tile<kN, kM, kWn, kWm, kAhead, 2, kMath16, true, true>;
