@@ -17,6 +17,9 @@ struct GradArgs {
   int32_t slots;  // in all so many parts of the weights' rows, dw_stride apart; 0: one a weight
 };
 
+// steps of 64 that `rows` take; a block may have 2^31 - 1
+__device__ __forceinline__ int steps_of(int rows) { return rows / 64 + (rows % 64 != 0); }
+
 // Items item, item + stride, .. below n_item: tiles of a weight's gradient, kM of its rows
 // (channels n of dy) by kN of its columns (channels k of x), and of each a part of the rows
 // that are summed over.  Both sides are transposed on their way from LDS.  The steps of an
@@ -117,12 +120,13 @@ struct GradWork {
     budget = 1 << 30;
     if (parts > 1) {
       int steps = 0;
-      for (; remaining > 0; next_block()) steps += (remaining + S::kStep - 1) / S::kStep;
+      static_assert(S::kStep == 64, "steps_of");
+      for (; remaining > 0; next_block()) steps += steps_of(remaining);
       int skip = static_cast<int>(static_cast<int64_t>(steps) * part / parts);
       budget = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / parts) - skip;
       first_block();
-      while (budget > 0 && skip >= (remaining + S::kStep - 1) / S::kStep) {
-        skip -= (remaining + S::kStep - 1) / S::kStep;
+      while (budget > 0 && skip >= steps_of(remaining)) {
+        skip -= steps_of(remaining);
         next_block();
       }
       if (budget > 0) {
@@ -267,7 +271,7 @@ __device__ __forceinline__ void count_slots(const GradArgs &a, int *s_first, int
   __syncthreads();
   for (int g = tid; g < a.n_block; g += 256) {
     const int rows = static_cast<int>(a.block_off[g + 1] - a.block_off[g]);
-    if (rows > 0) atomicAdd(&s_of[a.block_w ? a.block_w[g] : g], (rows + 63) / 64);
+    if (rows > 0) atomicAdd(&s_of[a.block_w ? a.block_w[g] : g], steps_of(rows));
   }
   __syncthreads();
   int total = 0, before = 0;

@@ -144,3 +144,19 @@ def test_a_weight_without_rows_stays_as_it_is(type, parts):
     assert int(a[13].item()) == 0
     assert torch.equal(a[11][0].view(words), bits[0])
     assert not torch.equal(a[11][1].view(words), bits[1])
+
+
+def test_the_most_rows():
+    """2^31 - 1 rows in one block, all zero but for some from one end to the other: the steps
+    of 64 that they take, 2^25, were counted by a sum past 2^31."""
+    rows, N, K = (1 << 31) - 1, 8, 8
+    dy, x = (torch.zeros(rows, n, dtype=BF16, device="cuda") for n in (N, K))
+    at = torch.tensor([0, 63, 64, (1 << 30) - 1, (1 << 30) + 5, rows - 65, rows - 64, rows - 1], device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for t in (dy, x):
+        t[at] = torch.randint(-3, 4, (len(at), 8), device="cuda", generator=g).to(BF16)  # exact sums
+    dw, st = torch.full((N, K), 7.0, device="cuda"), status()
+    uep.ultraep_expert_weight_grad(dy, x, rows, N, K, torch.tensor([0, rows], device="cuda"), None, 1, 1, N * K, False, dw,
+                                   workspace(rows, N, K, 1), st)
+    assert int(st.item()) == 0
+    assert torch.equal(dw.double(), dy[at].double().t().contiguous() @ x[at].double())
